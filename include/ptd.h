@@ -11,7 +11,12 @@
  *                        (ptd_tree_attention_ragged: trees of different sizes
  *                        in one padded batch; ptd_tree_attention_paged: the
  *                        same on paged caches; ptd_tree_attention_fp8kv: on
- *                        8-bit E4M3 key/value caches; _paged_fp8kv: both)
+ *                        8-bit E4M3 key/value caches; _paged_fp8kv: both;
+ *                        _paged_fp8blk: pages with a scale per block of rows)
+ *   ptd_prompt_attention causal attention over packed prompts (the pass that
+ *                        fills the caches before the first step)
+ *   ptd_page_plan        page tables and slot maps from the sequences' lengths
+ *   ptd_kv_write_fp8blk  key/value rows into 8-bit pages (block scales)
  *   ptd_topk_argmax      per-row argmax / top-k of the verification logits
  *   ptd_verify           greedy longest accepted path (+ bonus token)
  *   ptd_expand           progressive expansion with top-k children
@@ -73,8 +78,13 @@ typedef enum {
   PTD_ERR_BAD_PATH = 9,  /* device-detected: accepted path not strictly increasing
                             node ids in [0, T), or its length outside [0, T] */
   PTD_ERR_PAGE = 10,     /* device-detected: a page id outside [0, num_pages) */
-  PTD_ERR_SCRATCH = 11   /* the problem needs more scratch than the fixed array of
+  PTD_ERR_SCRATCH = 11,  /* the problem needs more scratch than the fixed array of
                             ptd_tree_attention_noalloc (PTD_NOALLOC_SCRATCH_BYTES) */
+  PTD_ERR_NO_PAGES = 12, /* device-detected: the free list has too few pages */
+  PTD_ERR_ROWS = 13,     /* device-detected: row starts not ascending within [0, N], more
+                            rows than there is room for, a source row or slot order that
+                            the call does not allow */
+  PTD_ERR_VALUE = 14     /* device-detected: a key or value that is not finite */
 } ptd_status;
 
 /* Dimension pairs turned together by the rotary embedding. */
@@ -279,6 +289,174 @@ int ptd_tree_attention_paged_fp8kv(const void* q, const ptd_kv_pages* kv, const 
                                    const int32_t* tree_len, const int32_t* parent, int32_t T,
                                    void* out, const ptd_attn_shape* shape, void* workspace,
                                    size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+/*
+ * 8-bit pages with a scale per block (host struct, read during the call only).
+ * Keys and values are OCP FP8 E4M3 codes as in ptd_tree_attention_paged_fp8kv,
+ * but every block of scale_rows consecutive rows of a page and head has one
+ * scale for its keys and one for its values: a power of two 2^(e - 127), held
+ * as its biased exponent e (the OCP microscaling E8M0 format, 1 <= e <= 254;
+ * ptd_kv_write_fp8blk writes 10 <= e <= 246).  A power of two costs the codes
+ * no precision, and gfx950's converters apply it while widening to bf16.
+ */
+typedef struct {
+  uint8_t* k_pages;           /* [num_pages][Hkv][page_size][128] E4M3 codes */
+  uint8_t* v_pages;           /* likewise */
+  uint8_t* scales;            /* [num_pages][Hkv][page_size / scale_rows][2]: e of the
+                                 block's keys, e of its values; 4-byte aligned */
+  const int32_t* page_table;  /* [B][max_pages] as in ptd_kv_pages (not read by
+                                 ptd_kv_write_fp8blk, where it may be NULL) */
+  int32_t page_size;          /* rows per page: a power of two >= 32 */
+  int32_t max_pages;          /* page-table entries per sequence */
+  int32_t num_pages;          /* pages in k_pages / v_pages */
+  int32_t scale_rows;         /* rows per scale: 32, 64 or 128, <= page_size */
+} ptd_kv_pages_fp8blk;
+
+/*
+ * ptd_tree_attention_paged_fp8blk -- ptd_tree_attention_paged_fp8kv on pages
+ * with block scales: key row j = e4m3(code) * 2^(e - 127) with e of its block,
+ * values likewise.  Codes and scale widen to bf16 exactly wherever the product
+ * is a normal bf16 number, so the arithmetic is that of the bf16 path on the
+ * decoded pages (bit for bit).  A tree of one node is the decoding step of a
+ * single token; a chain of up to PTD_MAX_T nodes continues a prompt whose
+ * beginning is cached.  Blocks without a live row (committed, or of a live
+ * node) are not read beyond the sub-tile of 32 rows that holds the last one.
+ * Other arguments, workspace, dev_status and errors as
+ * ptd_tree_attention_paged_fp8kv; PTD_ERR_SHAPE for scale_rows.
+ */
+int ptd_tree_attention_paged_fp8blk(const void* q, const ptd_kv_pages_fp8blk* kv,
+                                    const int32_t* kv_len, const int32_t* tree_len,
+                                    const int32_t* parent, int32_t T, void* out,
+                                    const ptd_attn_shape* shape, void* workspace,
+                                    size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+/*
+ * ptd_kv_write_fp8blk -- rows of keys and values into 8-bit pages with block
+ * scales: prompts, a step's tree rows, or (with src) the accepted ones of them.
+ *   k, v       [N][Hkv][128] of dtype; row r starts at element r * ldk (r * ldv),
+ *              so views of a wider projection are taken as they are; ldk, ldv >=
+ *              Hkv * 128 and multiples of 16 bytes
+ *   slots      int32 [N]: row i goes to page slots[i] / page_size, row
+ *              slots[i] % page_size of it; -1: row i is not written.  The rows of
+ *              one block are adjacent in i and their slots ascend by one (as
+ *              ptd_page_plan writes them); a row that breaks this inside a block
+ *              is reported and not written, and a block that is reached from two
+ *              places of the same call holds unspecified codes
+ *   src        int32 [N] or NULL.  Row i's key and value are row i of k and v; with
+ *              src, row (i / rows_per_seq) * rows_per_seq + src[i] (accept_nodes of
+ *              ptd_verify with rows_per_seq = T: the commit of the accepted
+ *              path).  Read only where slots[i] >= 0.  N % rows_per_seq == 0
+ * For every block that receives a row: the rows before its first new one are
+ * live and keep their values, the rows after its last new one are dead.  The
+ * block's scale becomes the least power of two s (2^-117 <= s <= 2^119) with
+ * |x| <= 448 s over its live and new rows (1 if all of them are zero), and both
+ * are coded with it, rounded to nearest even; live rows whose scale does not
+ * change keep their codes.  A code is within max(2^-4 |x|, 2^-10 s) of x; a live
+ * row that is coded anew under a larger scale adds at most 2^-10 s.  Codes of dead
+ * rows stay as they are.  Values beyond 448 * 2^119 and infinities saturate, a
+ * NaN becomes 0; whatever is not finite is reported and does not enter s.
+ * k_pages and v_pages 16-byte, scales 4-byte aligned; D must be 128.
+ * dev_status: PTD_ERR_PAGE (a slot outside the pages: not written), PTD_ERR_ROWS
+ * (slot order; src outside [0, rows_per_seq)), PTD_ERR_VALUE.
+ * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_DTYPE, PTD_ERR_ALIGN, PTD_ERR_HIP.
+ * N = 0 does nothing.
+ */
+int ptd_kv_write_fp8blk(const void* k, const void* v, ptd_dtype dtype, int64_t ldk, int64_t ldv,
+                        int32_t N, const int32_t* slots, const int32_t* src,
+                        int32_t rows_per_seq, const ptd_kv_pages_fp8blk* kv, int32_t Hkv,
+                        int32_t D, int32_t* dev_status, void* stream);
+
+/*
+ * Page tables of B sequences over one set of pages (host struct, read during
+ * the call only; the arrays are device memory and hold the state).
+ */
+typedef struct {
+  int32_t* page_table;  /* [B][max_pages]: a sequence's pages first, then -1 or old ids */
+  int32_t* num_held;    /* [B]: pages of the sequence */
+  int32_t* free_pages;  /* [num_pages]: free page ids in [0, num_free) */
+  int32_t* num_free;    /* [1] */
+  int32_t B;            /* 1 .. 65536 */
+  int32_t page_size;    /* a power of two, 1 .. 2^20 */
+  int32_t max_pages;    /* page-table entries per sequence; max_pages * page_size < 2^31 */
+  int32_t num_pages;    /* num_pages * page_size < 2^31 */
+} ptd_page_state;
+
+/* Every page free (page 0 is handed out first), no sequence holds any. */
+int ptd_page_init(const ptd_page_state* state, void* stream);
+
+/*
+ * ptd_page_plan -- pages and places for new rows, from the requests' lengths.
+ *   kv_len, new_len  int32 [B]: rows that a sequence has, rows that it is about to
+ *                    get (a prompt, a step's tree; 0 to keep kv_len rows; both 0:
+ *                    the sequence is finished).  >= 0, kv_len + new_len <=
+ *                    max_pages * page_size
+ * Each sequence then holds exactly ceil((kv_len + new_len) / page_size) pages:
+ *   1. surplus pages go back to the free list, in the reverse of the order in
+ *      which they would have been taken (last sequence first, last page first);
+ *   2. missing pages are taken from the free list's end, sequence by sequence.
+ *      From the first sequence on that does not find enough, no sequence of
+ *      the call takes any (PTD_ERR_NO_PAGES): those keep what they hold.
+ * So a call that trims what the one before took restores the free list, and
+ * the result depends on the lengths and the state alone.  Row r < new_len[b]
+ * of sequence b is row kv_len[b] + r of its cache:
+ *   rows_per_seq     0: the new rows of all sequences are packed one after the
+ *                    other, row_start[b] + r; otherwise sequence b's are the
+ *                    rows b * rows_per_seq + r, and N == B * rows_per_seq
+ *   N                rows of slots and positions
+ *   row_start        int32 [B + 1]: start of each sequence's rows, their total
+ *                    last (as ptd_prompt_attention reads it); nullable where
+ *                    rows_per_seq > 0, and not written there
+ *   slots            int32 [N]: page_table[b][p / page_size] * page_size + p %
+ *                    page_size of each row's place p = kv_len[b] + r; -1 for
+ *                    places without a row, or rows without a page
+ *   positions        int32 [N] or NULL: p; -1 for places without a row
+ * A sequence whose lengths or held pages are out of range keeps its pages and
+ * gets no rows.  The state's arrays, lengths and outputs must not overlap; calls
+ * on one state must not overlap.
+ * dev_status: PTD_ERR_KV_LEN (lengths), PTD_ERR_NO_PAGES, PTD_ERR_ROWS (more
+ * rows than N, or than rows_per_seq: the rest are left out), PTD_ERR_PAGE
+ * (num_held or num_free out of range, a page id outside the pages: slot -1).
+ * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_HIP.
+ */
+int ptd_page_plan(const ptd_page_state* state, const int32_t* kv_len, const int32_t* new_len,
+                  int32_t N, int32_t rows_per_seq, int32_t* row_start, int32_t* slots,
+                  int32_t* positions, int32_t* dev_status, void* stream);
+
+/* Packed prompts (host struct, read during the call only). */
+typedef struct {
+  int32_t B;           /* sequences, 1 .. 65536 */
+  int32_t N;           /* rows of q, k, v and out */
+  int32_t Hq, Hkv;     /* heads; Hq % Hkv == 0 */
+  int32_t D;           /* head dim: 64 or 128 */
+  int64_t ldq, ldk, ldv; /* elements from one row to the next: at least heads * D and
+                            a multiple of 16 bytes; 0 selects heads * D */
+  ptd_dtype in_dtype;  /* of q, k, v */
+  ptd_dtype out_dtype; /* of out */
+  float scale;         /* softmax scale; 0 selects 1/sqrt(D) */
+} ptd_prompt_shape;
+
+/*
+ * ptd_prompt_attention -- causal attention over whole prompts, packed one
+ * after the other:
+ *   for row i of sequence b and query head h (KV head g = h / (Hq/Hkv)),
+ *     out[i][h] = sum_{row_start[b] <= j <= i} softmax_j(scale * q_i . k_j) v_j
+ *   q          [N][Hq][D], rows ldq apart;  k, v  [N][Hkv][D], rows ldk, ldv apart
+ *   row_start  int32 [B + 1]: sequence b's rows are row_start[b] ..
+ *              row_start[b + 1] - 1 (none: an empty prompt); ascending, in [0, N]
+ *   out        [N][Hq][D]; rows outside the sequences are left as they were
+ * What a row may not see does not reach it, infinities and NaN included.  bf16
+ * inputs run on v_mfma_f32_32x32x16_bf16 with the softmax weights rounded to bf16
+ * above and below the line (out within 2^-7 of the largest value it averages,
+ * before its own rounding); fp32 inputs on v_mfma_f32_32x32x2_f32, fp32 throughout.  q, k, v and out must be
+ * 16-byte aligned.  Outputs do not depend on the other sequences of the call.
+ * dev_status: PTD_ERR_ROWS (a sequence whose start and end are not in order within
+ * [0, N] is not computed).
+ * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_DTYPE, PTD_ERR_ALIGN, PTD_ERR_HIP.
+ * N = 0 does nothing.
+ */
+int ptd_prompt_attention(const void* q, const void* k, const void* v, const int32_t* row_start,
+                         void* out, const ptd_prompt_shape* shape, int32_t* dev_status,
+                         void* stream);
 
 /* Workspace bytes ptd_topk_argmax needs (0 on invalid arguments). */
 size_t ptd_topk_workspace_bytes(int32_t R, int32_t V, int32_t k);

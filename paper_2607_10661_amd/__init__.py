@@ -10,8 +10,9 @@ device memory and the stream.  There is no CPU fallback: without a built
 
 The lower-case helpers (``tree_mask``, ``tree_attention``, ``topk_argmax``,
 ``verify``, ``expand``, ``verify_expand``, ``tree_rope``, ``kv_commit``,
-``verify_sample``, ``step_prune``, the ``Pool`` class) allocate outputs with
-torch and call the entry points.
+``verify_sample``, ``step_prune``, ``prompt_attention``, the ``Pool``,
+``PageTables`` and ``BlockKV`` classes) allocate outputs with torch and call the
+entry points.
 """
 from __future__ import annotations
 
@@ -30,7 +31,8 @@ PTD_MAX_T, PTD_MAX_K, PTD_MAX_DEPTH = 1024, 16, 64
 STATUS = {0: "PTD_OK", 1: "PTD_ERR_NULL", 2: "PTD_ERR_SHAPE", 3: "PTD_ERR_DTYPE",
           4: "PTD_ERR_ALIGN", 5: "PTD_ERR_WORKSPACE", 6: "PTD_ERR_HIP",
           7: "PTD_ERR_BAD_TREE", 8: "PTD_ERR_KV_LEN", 9: "PTD_ERR_BAD_PATH",
-          10: "PTD_ERR_PAGE", 11: "PTD_ERR_SCRATCH"}
+          10: "PTD_ERR_PAGE", 11: "PTD_ERR_SCRATCH", 12: "PTD_ERR_NO_PAGES",
+          13: "PTD_ERR_ROWS", 14: "PTD_ERR_VALUE"}
 PTD_NOALLOC_SCRATCH_BYTES = 64 << 20
 
 
@@ -54,6 +56,30 @@ class KVPages(ctypes.Structure):
     _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
                 ("page_table", ctypes.c_void_p), ("page_size", ctypes.c_int32),
                 ("max_pages", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
+class KVPagesFp8Blk(ctypes.Structure):
+    """ptd_kv_pages_fp8blk"""
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("scale_rows", ctypes.c_int32)]
+
+
+class PageState(ctypes.Structure):
+    """ptd_page_state"""
+    _fields_ = [("page_table", ctypes.c_void_p), ("num_held", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("num_free", ctypes.c_void_p),
+                ("B", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
+class PromptShape(ctypes.Structure):
+    """ptd_prompt_shape"""
+    _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("Hq", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32), ("ldq", ctypes.c_int64),
+                ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64), ("in_dtype", ctypes.c_int),
+                ("out_dtype", ctypes.c_int), ("scale", ctypes.c_float)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -103,6 +129,16 @@ _SIGS = {
                        ctypes.c_int),
     "ptd_pool_retrieve": ([_vp, _sz, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp],
                           ctypes.c_int),
+    "ptd_tree_attention_paged_fp8blk": ([_vp, ctypes.POINTER(KVPagesFp8Blk), _vp, _vp, _vp, _i32,
+                                         _vp, ctypes.POINTER(AttnShape), _vp, _sz, _vp, _vp],
+                                        ctypes.c_int),
+    "ptd_kv_write_fp8blk": ([_vp, _vp, ctypes.c_int, _i64, _i64, _i32, _vp, _vp, _i32,
+                             ctypes.POINTER(KVPagesFp8Blk), _i32, _i32, _vp, _vp], ctypes.c_int),
+    "ptd_page_init": ([ctypes.POINTER(PageState), _vp], ctypes.c_int),
+    "ptd_page_plan": ([ctypes.POINTER(PageState), _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp,
+                       _vp], ctypes.c_int),
+    "ptd_prompt_attention": ([_vp, _vp, _vp, _vp, _vp, ctypes.POINTER(PromptShape), _vp, _vp],
+                             ctypes.c_int),
     "ptd_verify_sample": ([_vp, ctypes.c_int, _i32, _i64, _vp, _vp, _vp, _i32, _i32,
                            ctypes.c_double, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp],
                           ctypes.c_int),
@@ -218,6 +254,44 @@ def ptd_tree_attention_paged(q, kv: KVPages, kv_len, tree_len, parent, T, out, s
                                          _ptr(mask), _ptr(workspace), workspace_bytes,
                                          _ptr(dev_status), _stream(stream)),
            "ptd_tree_attention_paged")
+
+
+def ptd_tree_attention_paged_fp8blk(q, kv: KVPagesFp8Blk, kv_len, tree_len, parent, T, out,
+                                    shape: AttnShape, workspace=None, workspace_bytes=0,
+                                    dev_status=None, stream=None):
+    _check(_lib.ptd_tree_attention_paged_fp8blk(_ptr(q), ctypes.byref(kv), _ptr(kv_len),
+                                                _ptr(tree_len), _ptr(parent), T, _ptr(out),
+                                                ctypes.byref(shape), _ptr(workspace),
+                                                workspace_bytes, _ptr(dev_status),
+                                                _stream(stream)),
+           "ptd_tree_attention_paged_fp8blk")
+
+
+def ptd_kv_write_fp8blk(k, v, dtype, ldk, ldv, N, slots, src, rows_per_seq, kv: KVPagesFp8Blk,
+                        Hkv, D, dev_status=None, stream=None):
+    _check(_lib.ptd_kv_write_fp8blk(_ptr(k), _ptr(v), dtype, ldk, ldv, N, _ptr(slots), _ptr(src),
+                                    rows_per_seq, ctypes.byref(kv), Hkv, D, _ptr(dev_status),
+                                    _stream(stream)),
+           "ptd_kv_write_fp8blk")
+
+
+def ptd_page_init(state: PageState, stream=None):
+    _check(_lib.ptd_page_init(ctypes.byref(state), _stream(stream)), "ptd_page_init")
+
+
+def ptd_page_plan(state: PageState, kv_len, new_len, N, rows_per_seq, row_start, slots,
+                  positions=None, dev_status=None, stream=None):
+    _check(_lib.ptd_page_plan(ctypes.byref(state), _ptr(kv_len), _ptr(new_len), N, rows_per_seq,
+                              _ptr(row_start), _ptr(slots), _ptr(positions), _ptr(dev_status),
+                              _stream(stream)),
+           "ptd_page_plan")
+
+
+def ptd_prompt_attention(q, k, v, row_start, out, shape: PromptShape, dev_status=None,
+                         stream=None):
+    _check(_lib.ptd_prompt_attention(_ptr(q), _ptr(k), _ptr(v), _ptr(row_start), _ptr(out),
+                                     ctypes.byref(shape), _ptr(dev_status), _stream(stream)),
+           "ptd_prompt_attention")
 
 
 def ptd_topk_workspace_bytes(R: int, V: int, k: int) -> int:
@@ -621,3 +695,147 @@ class Pool:
         ptd_pool_retrieve(self.buf, self.nbytes, self.B, self.e_max, self.n_cap, last_token,
                           T_max, po, to, ln)
         return po, to, ln
+
+
+# ---------------------------------------------------------------------------
+# prompts, page tables and 8-bit pages with block scales
+# ---------------------------------------------------------------------------
+def _need_here(*ts):
+    """Tensors on the current device: the calls run on its current stream."""
+    for t in ts:
+        if t is not None and (not isinstance(t, torch.Tensor) or not t.is_cuda
+                              or t.device.index != torch.cuda.current_device()):
+            raise ValueError("expected tensors on the current GPU")
+
+
+def _need_i32(*ts):
+    _need_here(*ts)
+    for t in ts:
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+            raise ValueError("expected contiguous int32 tensors")
+
+
+def _rows(t, heads=None):
+    """Row stride of [N][heads][D] rows whose heads are dense."""
+    if t.dim() != 3 or (t.shape[0] and (t.stride(2) != 1 or
+                                        (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
+        raise ValueError("expected [N][heads][D] rows with dense heads")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def prompt_attention(q, k, v, row_start, out=None, out_dtype=None, scale: float = 0.0,
+                     dev_status=None):
+    """Causal attention over packed prompts: q [N][Hq][D], k, v [N][Hkv][D] (views of
+    a wider projection are taken as they are), row_start int32 [B + 1].  Returns
+    out [N][Hq][D]; rows outside the sequences are left as they are (a new out:
+    zero)."""
+    _need_here(q, k, v)
+    _need_i32(row_start, dev_status)
+    N, Hq, D = q.shape
+    if k.shape != v.shape or k.shape[0] != N or k.shape[2] != D or k.dtype != q.dtype \
+            or v.dtype != q.dtype or row_start.dim() != 1 or row_start.numel() < 2:
+        raise ValueError("expected q [N][Hq][D], k and v [N][Hkv][D] of one dtype, row_start [B+1]")
+    code = _dtype_code(q)
+    if out is None:
+        out = torch.zeros((N, Hq, D), dtype=out_dtype or q.dtype, device=q.device)
+    elif out.shape != q.shape or not out.is_contiguous():
+        raise ValueError("expected contiguous out of q's shape")
+    _need_here(out)
+    shape = PromptShape(row_start.numel() - 1, N, Hq, k.shape[1], D, _rows(q), _rows(k), _rows(v),
+                        code, _dtype_code(out), float(scale))
+    ptd_prompt_attention(q, k, v, row_start, out, shape, dev_status)
+    return out
+
+
+class PageTables:
+    """Page tables of B sequences over num_pages pages of page_size rows, on the
+    GPU: plan() gives every sequence the pages its lengths ask for."""
+
+    def __init__(self, B: int, page_size: int, max_pages: int, num_pages: int, device="cuda"):
+        def i32(*shape):
+            return torch.empty(shape, dtype=torch.int32, device=device)
+
+        self.page_table, self.num_held = i32(B, max_pages), i32(B)
+        self.free_pages, self.num_free = i32(num_pages), i32(1)
+        self.B, self.page_size = B, page_size
+        self.max_pages, self.num_pages = max_pages, num_pages
+        _need_here(self.page_table)
+        ptd_page_init(self.state())
+
+    def state(self) -> PageState:
+        return PageState(self.page_table.data_ptr(), self.num_held.data_ptr(),
+                         self.free_pages.data_ptr(), self.num_free.data_ptr(), self.B,
+                         self.page_size, self.max_pages, self.num_pages)
+
+    def plan(self, kv_len, new_len, N: int, rows_per_seq: int = 0, dev_status=None):
+        """Returns (row_start [B + 1], or None with rows_per_seq; slots [N];
+        positions [N])."""
+        _need_i32(kv_len, new_len, dev_status, self.page_table)
+        if kv_len.numel() != self.B or new_len.numel() != self.B:
+            raise ValueError("expected lengths of B sequences")
+        dev = self.page_table.device
+        start = None if rows_per_seq else torch.empty(self.B + 1, dtype=torch.int32, device=dev)
+        slots, pos = (torch.empty(N, dtype=torch.int32, device=dev) for _ in range(2))
+        ptd_page_plan(self.state(), kv_len, new_len, N, rows_per_seq, start, slots, pos, dev_status)
+        return start, slots, pos
+
+
+class BlockKV:
+    """One layer's keys and values in 8-bit pages with a scale per scale_rows rows
+    and head (head dimension 128)."""
+
+    def __init__(self, num_pages: int, Hkv: int, page_size: int, scale_rows: int = 32,
+                 device="cuda"):
+        if scale_rows not in (32, 64, 128) or page_size % scale_rows:
+            raise ValueError("scale_rows is 32, 64 or 128 and divides page_size")
+        shape = (num_pages, Hkv, page_size, 128)
+        self.k_pages = torch.zeros(shape, dtype=torch.uint8, device=device)
+        self.v_pages = torch.zeros(shape, dtype=torch.uint8, device=device)
+        blocks = page_size // scale_rows
+        n = num_pages * Hkv * blocks * 2
+        # (the kernels read the exponents in 4-byte words)
+        self._words = torch.full(((n + 3) // 4 * 4,), 127, dtype=torch.uint8, device=device)
+        self.scales = self._words[:n].view(num_pages, Hkv, blocks, 2)
+        self.num_pages, self.Hkv, self.page_size, self.scale_rows = num_pages, Hkv, page_size, scale_rows
+
+    def pages(self, page_table=None) -> KVPagesFp8Blk:
+        return KVPagesFp8Blk(self.k_pages.data_ptr(), self.v_pages.data_ptr(),
+                             self.scales.data_ptr(),
+                             None if page_table is None else page_table.data_ptr(),
+                             self.page_size, 0 if page_table is None else page_table.shape[1],
+                             self.num_pages, self.scale_rows)
+
+    def write(self, k, v, slots, src=None, rows_per_seq: int = 0, dev_status=None):
+        """Rows of k, v [N][Hkv][128] (bf16 or fp32) to the slots int32 [N] (any shape
+        of N elements); src: rows within each sequence's rows_per_seq."""
+        _need_here(k, v, self.k_pages)
+        _need_i32(slots, src, dev_status)
+        N = slots.numel()
+        if k.shape != v.shape or k.shape[0] != N or k.shape[1:] != (self.Hkv, 128) \
+                or k.dtype != v.dtype or (src is not None and src.numel() != N):
+            raise ValueError("expected k and v [N][Hkv][128] and N slots")
+        ptd_kv_write_fp8blk(k, v, _dtype_code(k), _rows(k), _rows(v), N, slots, src, rows_per_seq,
+                            self.pages(), self.Hkv, 128, dev_status)
+
+    def tree_attention(self, q, page_table, kv_len, parent, out=None, out_dtype=None,
+                       scale: float = 0.0, workspace=None, dev_status=None, tree_len=None):
+        """q bf16 [B][T][Hq][128], page_table int32 [B][max_pages]; otherwise as
+        tree_attention_paged."""
+        _need_gpu(q, page_table, kv_len, parent, tree_len)
+        _need_here(q, self.k_pages)
+        _need_i32(page_table, kv_len, parent, tree_len, dev_status)
+        B, T, Hq, D = q.shape
+        if page_table.shape[0] != B or kv_len.numel() != B or parent.shape != (B, T):
+            raise ValueError("expected page_table [B][max_pages], kv_len [B], parent [B][T]")
+        od = out_dtype or (q.dtype if out is None else out.dtype)
+        if out is None:
+            out = torch.empty((B, T, Hq, D), dtype=od, device=q.device)
+        shape = AttnShape(B, Hq, self.Hkv, D, page_table.shape[1] * self.page_size, _dtype_code(q),
+                          _dtype_code(out), float(scale))
+        nbytes = ptd_tree_attention_workspace_bytes(shape, T)
+        if workspace is None and nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        ptd_tree_attention_paged_fp8blk(q, self.pages(page_table), kv_len, tree_len, parent, T, out,
+                                        shape, workspace,
+                                        0 if workspace is None else workspace.numel(), dev_status)
+        return out

@@ -15,6 +15,9 @@ extern "C" const char* ptd_status_string(int status) {
     case PTD_ERR_BAD_PATH: return "accepted path: length outside [0, T] or node ids not strictly increasing in [0, T)";
     case PTD_ERR_PAGE: return "page id outside [0, num_pages)";
     case PTD_ERR_SCRATCH: return "problem needs more than the 64 MiB scratch of ptd_tree_attention_noalloc";
+    case PTD_ERR_NO_PAGES: return "the free list has too few pages";
+    case PTD_ERR_ROWS: return "row starts, row counts, source rows or slot order out of range";
+    case PTD_ERR_VALUE: return "a key or value that is not finite";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,621 @@
+// Pages of the key/value caches: page tables and slot maps from the sequences'
+// lengths (ptd_page_init, ptd_page_plan), and rows into 8-bit pages with block
+// scales (ptd_kv_write_fp8blk).
+#include <algorithm>
+
+#include "ptd_common.hpp"
+
+namespace {
+
+// ===========================================================================
+// page tables and slot maps
+// ===========================================================================
+struct PlanParams {
+  ptd_page_state s;
+  const int32_t* kv_len;
+  const int32_t* new_len;
+  int32_t* row_start;
+  int32_t* slots;
+  int32_t* positions;
+  int32_t* dev_status;
+  int N, rows_per_seq, page_shift;
+};
+
+constexpr int kPlanThreads = 512;
+constexpr int kPlanWaves = kPlanThreads / PTD_WAVE;
+// Rows whose slots the planning workgroup writes itself; more take a launch of
+// their own, over the whole chip.
+constexpr int kPlanRows = 16 * kPlanThreads;
+
+// A sequence's lengths and pages, checked.  rows: new rows (0 where refused).
+struct Want {
+  int kv, rows, held, need;
+};
+__device__ inline Want want_of(const PlanParams& p, int b, int32_t* report_to) {
+  Want w;
+  w.kv = p.kv_len[b];
+  w.rows = p.new_len[b];
+  w.held = p.s.num_held[b];
+  const long long cap = static_cast<long long>(p.s.max_pages) << p.page_shift;
+  const bool bad_len = w.kv < 0 || w.rows < 0 || static_cast<long long>(w.kv) + w.rows > cap;
+  const bool bad_held = w.held < 0 || w.held > p.s.max_pages;
+  if (bad_len) ptd::report(report_to, PTD_ERR_KV_LEN);
+  if (bad_held) ptd::report(report_to, PTD_ERR_PAGE);
+  if (bad_len || bad_held) {
+    w.rows = 0;
+    w.held = bad_held ? 0 : w.held;
+    w.need = w.held;
+  } else {
+    // (the sum fits an int: it is at most cap < 2^31)
+    w.need = static_cast<int>((static_cast<unsigned>(w.kv + w.rows) + (1u << p.page_shift) - 1u) >> p.page_shift);
+  }
+  return w;
+}
+
+__device__ __forceinline__ long long wave_scan(long long v) {  // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < PTD_WAVE; o <<= 1) {
+    const long long u = __shfl_up(v, o, PTD_WAVE);
+    v += lane >= o ? u : 0;
+  }
+  return v;
+}
+
+// Exclusive sum over the workgroup; total to every thread.
+__device__ __forceinline__ long long block_scan(long long v, long long* lds, long long* total) {
+  const int wave = threadIdx.x >> 6;
+  const long long in = wave_scan(v);
+  __syncthreads();  // lds of the call before is read
+  if ((threadIdx.x & 63) == 63) lds[wave] = in;
+  __syncthreads();
+  long long base = 0, all = 0;
+  for (int w = 0; w < kPlanWaves; ++w) {
+    base += w < wave ? lds[w] : 0;
+    all += lds[w];
+  }
+  *total = all;
+  return base + in - v;
+}
+
+// Last index x of [0, n) with a[x] <= v (a ascending, a[0] <= v).
+template <typename A>
+__device__ __forceinline__ int upper(const A& a, int n, long long v) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Slot and position of row i: row r of sequence b (r < rows: a live one).
+__device__ __forceinline__ void put_row(const PlanParams& p, int i, int b, int r, int rows, int kv, int held) {
+  int slot = -1, pos = -1;
+  if (r < rows) {
+    pos = kv + r;
+    const int pg = pos >> p.page_shift;
+    if (pg < held) {
+      const int id = p.s.page_table[static_cast<size_t>(b) * p.s.max_pages + pg];
+      if (static_cast<uint32_t>(id) < static_cast<uint32_t>(p.s.num_pages))
+        slot = (id << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+      else
+        ptd::report(p.dev_status, PTD_ERR_PAGE);
+    }
+  }
+  p.slots[i] = slot;
+  if (p.positions) p.positions[i] = pos;
+}
+
+// Both kernels' row loop: rows [i0, i1) by `step`.  Sequences of packed rows come
+// from row_start (in LDS where they fit, else in memory).
+template <typename Starts>
+__device__ __forceinline__ void put_rows(const PlanParams& p, const Starts& starts, int i0, int i1, int step) {
+  for (int i = i0; i < i1; i += step) {
+    int b, r;
+    if (p.rows_per_seq > 0) {
+      b = i / p.rows_per_seq;
+      r = i - b * p.rows_per_seq;
+    } else {
+      b = upper(starts, p.s.B, i);  // (the last of sequences that start at one place has the rows)
+      r = i - starts[b];
+    }
+    const Want w = want_of(p, b, nullptr);
+    put_row(p, i, b, r, w.rows, w.kv, w.held);
+  }
+}
+
+// One workgroup: a thread per sequence (in rounds of 512) counts pages, sums over
+// the workgroup give every sequence its places on the free list and in the rows,
+// then a thread per page moves ids.  Bound by latency: about seven dependent
+// accesses to memory, whatever the lengths (16 sequences that take and trim 17
+// pages each).  Outputs depend on nothing but the inputs: no atomics.
+__global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanParams p) {
+  __shared__ long long s_scan[kPlanWaves];
+  __shared__ int s_off[kPlanThreads], s_need[kPlanThreads], s_held[kPlanThreads], s_start[kPlanThreads + 1];
+  const int tid = threadIdx.x;
+  const int B = p.s.B;
+  int count = p.s.num_free[0];
+  if (count < 0 || count > p.s.num_pages) {  // uniform
+    if (tid == 0) ptd::report(p.dev_status, PTD_ERR_PAGE);
+    count = min(max(count, 0), p.s.num_pages);
+  }
+  // ---- pages that go back: their number first, as the first sequence's lie deepest
+  long long total = 0;
+  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+    Want w = {0, 0, 0, 0};
+    if (b0 + tid < B) w = want_of(p, b0 + tid, nullptr);
+    long long t;
+    block_scan(max(w.held - w.need, 0), s_scan, &t);
+    total += t;
+  }
+  if (total > p.s.num_pages - count) {  // pages held twice: the list cannot take them
+    if (tid == 0) ptd::report(p.dev_status, PTD_ERR_PAGE);
+    total = p.s.num_pages - count;
+  }
+  const int count1 = count + static_cast<int>(total);
+  long long done = 0;
+  for (int b0 = 0; b0 < B && total > 0; b0 += kPlanThreads) {  // uniform
+    Want w = {0, 0, 0, 0};
+    if (b0 + tid < B) w = want_of(p, b0 + tid, nullptr);
+    long long t;
+    const long long off = block_scan(max(w.held - w.need, 0), s_scan, &t);
+    s_off[tid] = static_cast<int>(off);
+    s_need[tid] = w.need;
+    __syncthreads();
+    const int n = min(B - b0, kPlanThreads);
+    for (int j = tid; j < t; j += kPlanThreads) {
+      const int x = upper(s_off, n, j);
+      const long long at = count1 - 1 - (done + j);
+      if (at >= count)
+        p.s.free_pages[at] = p.s.page_table[static_cast<size_t>(b0 + x) * p.s.max_pages + s_need[x] + (j - s_off[x])];
+    }
+    done += t;
+    __syncthreads();
+  }
+  // ---- pages that are taken, in order while the list lasts; starts of the rows
+  long long taken = 0, rows = 0;
+  bool short_of = false;
+  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+    Want w = {0, 0, 0, 0};
+    const bool live = b0 + tid < B;
+    if (live) w = want_of(p, b0 + tid, p.dev_status);
+    if (p.rows_per_seq > 0 && w.rows > p.rows_per_seq) ptd::report(p.dev_status, PTD_ERR_ROWS);
+    const int grow = max(w.need - w.held, 0);
+    long long t, tr;
+    const long long off = block_scan(grow, s_scan, &t);
+    const long long at = rows + block_scan(w.rows, s_scan, &tr);
+    const bool ok = grow == 0 || taken + off + grow <= count1;
+    if (!ok) ptd::report(p.dev_status, PTD_ERR_NO_PAGES);
+    const int now = ok ? w.need : w.held;
+    s_off[tid] = static_cast<int>(min(off, static_cast<long long>(p.s.num_pages)));
+    s_need[tid] = ok ? grow : 0;
+    s_held[tid] = w.held;
+    if (p.rows_per_seq == 0) {
+      const int start = static_cast<int>(min(at, static_cast<long long>(0x7FFFFFFF)));
+      if (live) p.row_start[b0 + tid] = start;
+      s_start[tid] = start;
+    }
+    __syncthreads();
+    const int n = min(B - b0, kPlanThreads);
+    const long long room = min(t, static_cast<long long>(count1) - taken);
+    for (int j = tid; j < room; j += kPlanThreads) {
+      const int x = upper(s_off, n, j);
+      const int k = j - s_off[x];
+      if (k < s_need[x])
+        p.s.page_table[static_cast<size_t>(b0 + x) * p.s.max_pages + s_held[x] + k] =
+            p.s.free_pages[count1 - 1 - (taken + j)];
+    }
+    // (a sequence refused above keeps num_held as it is, whatever it says)
+    if (live && now != w.held) p.s.num_held[b0 + tid] = now;
+    // sequences after the first that was refused took none
+    const bool any_bad = __syncthreads_or(!ok);
+    if (any_bad && !short_of) {
+      long long mx = ok && grow > 0 ? off + grow : 0;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const long long u = __shfl_xor(mx, o, PTD_WAVE);
+        mx = u > mx ? u : mx;
+      }
+      if ((tid & 63) == 0) s_scan[tid >> 6] = mx;
+      __syncthreads();
+      mx = 0;
+      for (int w2 = 0; w2 < kPlanWaves; ++w2) mx = max(mx, s_scan[w2]);
+      __syncthreads();
+      if (tid == 0) p.s.num_free[0] = count1 - static_cast<int>(taken + mx);
+      short_of = true;
+    }
+    taken += t;
+    rows += tr;
+  }
+  if (tid == 0) {
+    if (!short_of) p.s.num_free[0] = count1 - static_cast<int>(taken);
+    if (p.rows_per_seq == 0) {
+      p.row_start[B] = static_cast<int>(min(rows, static_cast<long long>(0x7FFFFFFF)));
+      if (rows > p.N) ptd::report(p.dev_status, PTD_ERR_ROWS);
+    }
+  }
+  if (p.N > kPlanRows) return;
+  __syncthreads();
+  if (p.rows_per_seq > 0 || B <= kPlanThreads) put_rows(p, s_start, tid, p.N, kPlanThreads);
+  else put_rows(p, p.row_start, tid, p.N, kPlanThreads);
+}
+
+constexpr int kSlotThreads = 256;
+constexpr int kSlotRows = 4 * kSlotThreads;  // rows per workgroup
+
+__global__ void __launch_bounds__(kSlotThreads) k_page_slots(PlanParams p) {
+  __shared__ int s_start[kPlanThreads];
+  const int i0 = blockIdx.x * kSlotRows + threadIdx.x;
+  const int i1 = static_cast<int>(min(static_cast<long long>(p.N), (blockIdx.x + 1LL) * kSlotRows));
+  if (p.rows_per_seq == 0 && p.s.B <= kPlanThreads) {
+    for (int x = threadIdx.x; x < p.s.B; x += kSlotThreads) s_start[x] = p.row_start[x];
+    __syncthreads();
+    put_rows(p, s_start, i0, i1, kSlotThreads);
+  } else {
+    put_rows(p, p.row_start, i0, i1, kSlotThreads);
+  }
+}
+
+__global__ void __launch_bounds__(256) k_page_init(ptd_page_state s) {
+  const long long n = static_cast<long long>(s.B) * s.max_pages;
+  const long long step = static_cast<long long>(gridDim.x) * 256;
+  const long long first = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+  for (long long i = first; i < n; i += step) s.page_table[i] = -1;
+  for (long long i = first; i < s.num_pages; i += step) s.free_pages[i] = s.num_pages - 1 - static_cast<int>(i);
+  for (long long i = first; i < s.B; i += step) s.num_held[i] = 0;
+  if (first == 0) s.num_free[0] = s.num_pages;
+}
+
+int check_state(const ptd_page_state* s, int* shift) {
+  PTD_RETURN_IF(!s || !s->page_table || !s->num_held || !s->free_pages || !s->num_free, PTD_ERR_NULL);
+  const int ps = s->page_size;
+  PTD_RETURN_IF(ps < 1 || ps > (1 << 20) || (ps & (ps - 1)) != 0, PTD_ERR_SHAPE);
+  PTD_RETURN_IF(s->B < 1 || s->B > 65536 || s->max_pages < 1 || s->num_pages < 1, PTD_ERR_SHAPE);
+  PTD_RETURN_IF(static_cast<long long>(s->max_pages) * ps > 0x7FFFFFFFLL ||
+                    static_cast<long long>(s->num_pages) * ps > 0x7FFFFFFFLL,
+                PTD_ERR_SHAPE);
+  int sh = 0;
+  while ((1 << sh) < ps) ++sh;
+  *shift = sh;
+  return PTD_OK;
+}
+
+// ===========================================================================
+// rows into 8-bit pages
+// ===========================================================================
+struct WriteParams {
+  const void* src[2];      // keys, values
+  int64_t ld[2];           // elements
+  uint8_t* pages[2];
+  uint8_t* scales;
+  const int32_t* slots;
+  const int32_t* from;     // source rows within a sequence, or null
+  int32_t* dev_status;
+  int N, rows_per_seq, Hkv, chunk, page_shift, scale_shift;
+  long long slot_end;      // num_pages * page_size
+};
+
+constexpr int kWriteThreads = 256;
+constexpr int kHeadDim = 128;
+constexpr int kExpMin = -117, kExpMax = 119;  // of the scales
+
+// Eight elements of a row as they are loaded.  top(): largest magnitude's bits of
+// each half or word, ordered as integers; at(j): element j.
+template <typename T>
+struct Row8;
+template <>
+struct Row8<uint16_t> {
+  uint32_t w[4];
+  __device__ void load(const uint16_t* s) {
+    const uint4 v = *reinterpret_cast<const uint4*>(s);
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  }
+  __device__ void clear() { w[0] = w[1] = w[2] = w[3] = 0u; }
+  // (the compiler would keep the floats of one use for the next: twice the registers)
+  __device__ void forget() { asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3])); }
+  __device__ float at(int j) const { return (j & 1) ? ptd::bf16_hi(w[j >> 1]) : ptd::bf16_lo(w[j >> 1]); }
+  __device__ uint32_t top() const {
+    using u16x2 = unsigned short __attribute__((ext_vector_type(2)));
+    u16x2 m = __builtin_bit_cast(u16x2, w[0] & 0x7FFF7FFFu);
+#pragma unroll
+    for (int j = 1; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[j] & 0x7FFF7FFFu));
+    const uint32_t r = __builtin_bit_cast(uint32_t, m);
+    return max(r << 16, r & 0xFFFF0000u);
+  }
+};
+template <>
+struct Row8<float> {
+  uint32_t w[8];
+  __device__ void load(const float* s) {
+    const uint4 a = *reinterpret_cast<const uint4*>(s), b = *reinterpret_cast<const uint4*>(s + 4);
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+    w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+  }
+  __device__ void clear() {
+    for (int j = 0; j < 8; ++j) w[j] = 0u;
+  }
+  __device__ void forget() {
+    asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]), "+v"(w[4]), "+v"(w[5]), "+v"(w[6]), "+v"(w[7]));
+  }
+  __device__ float at(int j) const { return __uint_as_float(w[j]); }
+  __device__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, w[j] & 0x7FFFFFFFu);
+    return m;
+  }
+};
+
+constexpr uint32_t kInfBits = 0x7F800000u;
+
+// Eight E4M3 codes of x * 2^e, nearest even (v_cvt_pk_fp8_f32: OCP on gfx950).  x *
+// 2^e is exact or far below the least code; 448 is the largest.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true));
+}
+__device__ __forceinline__ float to_range(float x, float f) {
+  const float y = x * f;
+  return __builtin_amdgcn_fmed3f(y != y ? 0.f : y, -448.f, 448.f);
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+
+// One wave per (block of S rows, head, keys or values): 16 lanes hold a row of 128
+// elements, eight each; a lane's S / 4 loads are all in flight before the first is
+// used, and the largest magnitude is the only thing that passes between lanes.
+//
+// The block's scale is 2^e, e least with amax <= 448 * 2^e: with amax = m * 2^x, 1 <=
+// m < 2, that is x - 8, or x - 7 where m > 1.75.  A power of two leaves the
+// codes' three mantissa bits untouched, so a live row is coded anew without
+// loss while it stays a normal number of the format.
+template <typename T, int S>
+__global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
+  constexpr int R = S / 4;  // rows per lane
+  // registers hold the block's rows (up to 64 registers of them), or 32 rows at a
+  // time that the second pass reads again
+  constexpr bool HOLD = R * sizeof(T) * 2 <= 64;
+  constexpr int RH = HOLD ? R : 8;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kind = wave & 1;
+  const int g = blockIdx.y * 2 + (wave >> 1);
+  if (g >= p.Hkv) return;
+  const int sub = lane >> 4, d8 = (lane & 15) * 8;
+  const T* src = static_cast<const T*>(p.src[kind]) + static_cast<size_t>(g) * kHeadDim + d8;
+  const int64_t ld = p.ld[kind];
+  const int end = static_cast<int>(min(static_cast<long long>(p.N), (blockIdx.x + 1LL) * p.chunk));
+  // slot of row i, or -1 (off the rows, not to be written, outside the pages)
+  auto slot_of = [&](int i) __attribute__((always_inline)) {
+    int s = i >= 0 && i < p.N ? p.slots[i] : -1;
+    if (s < -1 || s >= p.slot_end) {
+      ptd::report(p.dev_status, PTD_ERR_PAGE);
+      s = -1;
+    }
+    return s;
+  };
+  for (int i = blockIdx.x * p.chunk; i < end;) {
+    // next row of the chunk that opens a block: one whose row before it is not in
+    // the same block
+    const int cur = slot_of(i + lane), prev = slot_of(i + lane - 1);
+    const bool same = cur >= 0 && prev >= 0 && (cur >> p.scale_shift) == (prev >> p.scale_shift);
+    if (same && cur != prev + 1) ptd::report(p.dev_status, PTD_ERR_ROWS);
+    const uint64_t heads = __ballot(cur >= 0 && !same && i + lane < end);
+    if (heads == 0) {
+      i += PTD_WAVE;
+      continue;
+    }
+    i += __builtin_ctzll(heads);
+    // the run: rows whose slots go on by one inside the block
+    const int slot0 = __builtin_amdgcn_readfirstlane(slot_of(i));
+    const int off0 = slot0 & (S - 1);
+    int n = 0;
+#pragma unroll
+    for (int h = 0; h < (S + 63) / 64; ++h) {
+      const int j = h * 64 + lane;
+      const bool in = j < S - off0 && slot_of(i + j) == slot0 + j;
+      const uint64_t m = ~__ballot(in);
+      if (n == h * 64) n += m ? __builtin_ctzll(m) : 64;
+    }
+    const size_t block = (((static_cast<size_t>(slot0) >> p.page_shift) * p.Hkv + g) << (p.page_shift - p.scale_shift)) +
+                         ((slot0 & ((1 << p.page_shift) - 1)) >> p.scale_shift);
+    uint8_t* page = p.pages[kind] + block * (S * kHeadDim) + d8;
+    uint8_t* scale = p.scales + block * 2 + kind;
+    Row8<T> x[RH];
+    auto is_new = [&](int r) __attribute__((always_inline)) { return r >= off0 && r < off0 + n; };
+    auto load = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int t = 0; t < RH; ++t) {
+        const int r = 4 * (t0 + t) + sub;
+        x[t].clear();
+        if (is_new(r)) {
+          int row = i + r - off0;
+          if (p.from) {
+            const int f = p.from[row];
+            if (f < 0 || f >= p.rows_per_seq) ptd::report(p.dev_status, PTD_ERR_ROWS);
+            row = row / p.rows_per_seq * p.rows_per_seq + min(max(f, 0), p.rows_per_seq - 1);
+          }
+          x[t].load(src + row * ld);
+        }
+      }
+    };
+    // ---- largest magnitude
+    uint32_t top = 0;
+    bool odd = false;  // something not finite
+    for (int t0 = 0; t0 < R; t0 += RH) {
+      load(t0);
+      uint32_t m = 0;
+#pragma unroll
+      for (int t = 0; t < RH; ++t) m = max(m, x[t].top());
+      if (__any(m >= kInfBits)) {  // rare: the finite elements only
+        odd |= m >= kInfBits;
+        m = 0;
+#pragma unroll
+        for (int t = 0; t < RH; ++t)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t u = __float_as_uint(x[t].at(j)) & 0x7FFFFFFFu;
+            m = max(m, u >= kInfBits ? 0u : u);
+          }
+      }
+      top = max(top, m);
+    }
+    if (odd) ptd::report(p.dev_status, PTD_ERR_VALUE);
+    int e_old = 0;
+    if (off0 > 0) {  // uniform: live rows
+      e_old = __builtin_amdgcn_readfirstlane(*scale) - 127;
+      uint32_t code = 0;
+      for (int r = sub; r < off0; r += 4) {
+        const uint2 c = *reinterpret_cast<const uint2*>(page + r * kHeadDim);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) code = max(code, max((c.x >> (8 * j)) & 0x7Fu, (c.y >> (8 * j)) & 0x7Fu));
+      }
+      // its value, times the scale it was coded with (both in normal range)
+      const float v = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(min(code, 0x7Eu)), 0) * pow2(min(max(e_old, -126), kExpMax));
+      top = max(top, __float_as_uint(v));
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o, PTD_WAVE)));
+    int e = static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    e = top == 0 ? 0 : min(max(e, kExpMin), kExpMax);
+    // ---- codes
+    const float f = pow2(-e);
+    for (int t0 = 0; t0 < R; t0 += RH) {
+      if constexpr (!HOLD) load(t0);
+#pragma unroll
+      for (int t = 0; t < RH; ++t) {
+        const int r = 4 * (t0 + t) + sub;
+        x[t].forget();
+        if (is_new(r)) {
+          float y[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = to_range(x[t].at(j), f);
+          *reinterpret_cast<uint2*>(page + r * kHeadDim) = make_uint2(codes4(y[0], y[1], y[2], y[3]), codes4(y[4], y[5], y[6], y[7]));
+        }
+      }
+    }
+    if (off0 > 0 && e != e_old) {  // uniform
+      const float fo = pow2(min(max(e_old - e, -126), 127));
+      for (int r = sub; r < off0; r += 4) {
+        const uint2 c = *reinterpret_cast<const uint2*>(page + r * kHeadDim);
+        float y[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int w = static_cast<int>(h ? c.y : c.x);
+          y[4 * h + 0] = __builtin_amdgcn_cvt_f32_fp8(w, 0);
+          y[4 * h + 1] = __builtin_amdgcn_cvt_f32_fp8(w, 1);
+          y[4 * h + 2] = __builtin_amdgcn_cvt_f32_fp8(w, 2);
+          y[4 * h + 3] = __builtin_amdgcn_cvt_f32_fp8(w, 3);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = to_range(y[j], fo);
+        *reinterpret_cast<uint2*>(page + r * kHeadDim) =
+            make_uint2(codes4(y[0], y[1], y[2], y[3]), codes4(y[4], y[5], y[6], y[7]));
+      }
+    }
+    if (lane == 0) *scale = static_cast<uint8_t>(e + 127);
+    i += n;
+  }
+}
+
+template <typename T>
+void launch_write(const WriteParams& prm, int scale_rows, dim3 grid, hipStream_t st) {
+  if (scale_rows == 32) hipLaunchKernelGGL((k_kv_write<T, 32>), grid, dim3(kWriteThreads), 0, st, prm);
+  else if (scale_rows == 64) hipLaunchKernelGGL((k_kv_write<T, 64>), grid, dim3(kWriteThreads), 0, st, prm);
+  else hipLaunchKernelGGL((k_kv_write<T, 128>), grid, dim3(kWriteThreads), 0, st, prm);
+}
+
+}  // namespace
+
+extern "C" int ptd_page_init(const ptd_page_state* state, void* stream) {
+  int shift = 0;
+  const int rc = check_state(state, &shift);
+  if (rc != PTD_OK) return rc;
+  const long long n = std::max(static_cast<long long>(state->B) * state->max_pages,
+                               static_cast<long long>(state->num_pages));
+  const unsigned grid = static_cast<unsigned>(std::min<long long>((n + 255) / 256, 2048));
+  hipLaunchKernelGGL(k_page_init, dim3(grid), dim3(256), 0, static_cast<hipStream_t>(stream), *state);
+  return ptd_launch_status();
+}
+
+extern "C" int ptd_page_plan(const ptd_page_state* state, const int32_t* kv_len,
+                             const int32_t* new_len, int32_t N, int32_t rows_per_seq,
+                             int32_t* row_start, int32_t* slots, int32_t* positions,
+                             int32_t* dev_status, void* stream) {
+  PlanParams prm;
+  const int rc = check_state(state, &prm.page_shift);
+  if (rc != PTD_OK) return rc;
+  PTD_RETURN_IF(!kv_len || !new_len || (N > 0 && !slots) || (rows_per_seq == 0 && !row_start), PTD_ERR_NULL);
+  PTD_RETURN_IF(N < 0 || rows_per_seq < 0, PTD_ERR_SHAPE);
+  PTD_RETURN_IF(rows_per_seq > 0 && static_cast<long long>(state->B) * rows_per_seq != N, PTD_ERR_SHAPE);
+  prm.s = *state;
+  prm.kv_len = kv_len;
+  prm.new_len = new_len;
+  prm.row_start = row_start;
+  prm.slots = slots;
+  prm.positions = positions;
+  prm.dev_status = dev_status;
+  prm.N = N;
+  prm.rows_per_seq = rows_per_seq;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(k_page_plan, dim3(1), dim3(kPlanThreads), 0, st, prm);
+  if (N > kPlanRows) {
+    const unsigned grid = static_cast<unsigned>((static_cast<long long>(N) + kSlotRows - 1) / kSlotRows);
+    hipLaunchKernelGGL(k_page_slots, dim3(grid), dim3(kSlotThreads), 0, st, prm);
+  }
+  return ptd_launch_status();
+}
+
+extern "C" int ptd_kv_write_fp8blk(const void* k, const void* v, ptd_dtype dtype, int64_t ldk,
+                                   int64_t ldv, int32_t N, const int32_t* slots,
+                                   const int32_t* src, int32_t rows_per_seq,
+                                   const ptd_kv_pages_fp8blk* kv, int32_t Hkv, int32_t D,
+                                   int32_t* dev_status, void* stream) {
+  PTD_RETURN_IF(!kv || !kv->k_pages || !kv->v_pages || !kv->scales, PTD_ERR_NULL);
+  PTD_RETURN_IF(N > 0 && (!k || !v || !slots), PTD_ERR_NULL);
+  PTD_RETURN_IF(dtype != PTD_F32 && dtype != PTD_BF16, PTD_ERR_DTYPE);
+  const int ps = kv->page_size, sr = kv->scale_rows;
+  PTD_RETURN_IF(ps < 32 || ps > (1 << 20) || (ps & (ps - 1)) != 0 || kv->num_pages < 1, PTD_ERR_SHAPE);
+  PTD_RETURN_IF((sr != 32 && sr != 64 && sr != 128) || sr > ps, PTD_ERR_SHAPE);
+  PTD_RETURN_IF(static_cast<long long>(kv->num_pages) * ps > 0x7FFFFFFFLL, PTD_ERR_SHAPE);
+  PTD_RETURN_IF(N < 0 || Hkv < 1 || Hkv > 65535 || D != kHeadDim, PTD_ERR_SHAPE);
+  PTD_RETURN_IF(src && (rows_per_seq < 1 || N % rows_per_seq != 0), PTD_ERR_SHAPE);
+  const int64_t row = static_cast<int64_t>(Hkv) * kHeadDim;
+  PTD_RETURN_IF(ldk < row || ldv < row, PTD_ERR_SHAPE);
+  const int per16 = dtype == PTD_F32 ? 4 : 8;
+  PTD_RETURN_IF(ldk % per16 != 0 || ldv % per16 != 0 || !ptd_aligned(k, 16) || !ptd_aligned(v, 16) ||
+                    !ptd_aligned(kv->k_pages, 16) || !ptd_aligned(kv->v_pages, 16) ||
+                    !ptd_aligned(kv->scales, 4),
+                PTD_ERR_ALIGN);
+  if (N == 0) return PTD_OK;
+  WriteParams prm;
+  prm.src[0] = k;
+  prm.src[1] = v;
+  prm.ld[0] = ldk;
+  prm.ld[1] = ldv;
+  prm.pages[0] = kv->k_pages;
+  prm.pages[1] = kv->v_pages;
+  prm.scales = kv->scales;
+  prm.slots = slots;
+  prm.from = src;
+  prm.dev_status = dev_status;
+  prm.N = N;
+  prm.rows_per_seq = src ? rows_per_seq : 1;
+  prm.Hkv = Hkv;
+  prm.slot_end = static_cast<long long>(kv->num_pages) * ps;
+  prm.page_shift = 0;
+  while ((1 << prm.page_shift) < ps) ++prm.page_shift;
+  prm.scale_shift = sr == 32 ? 5 : sr == 64 ? 6 : 7;
+  // Rows per workgroup: a block's rows (one run each for prompts), halved while
+  // workgroups are too few to fill the chip -- a step's rows open several blocks
+  // within that many rows, which a wave would code one after the other.
+  const int pairs = (Hkv + 1) / 2;
+  prm.chunk = sr;
+  while (prm.chunk > 1 && (static_cast<long long>(N) + prm.chunk - 1) / prm.chunk * pairs < 1024) prm.chunk /= 2;
+  const dim3 grid(static_cast<unsigned>((static_cast<long long>(N) + prm.chunk - 1) / prm.chunk), pairs);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (dtype == PTD_F32) launch_write<float>(prm, sr, grid, st);
+  else launch_write<uint16_t>(prm, sr, grid, st);
+  return ptd_launch_status();
+}

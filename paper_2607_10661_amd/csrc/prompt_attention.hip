@@ -1,0 +1,563 @@
+// Causal attention over packed prompts (ptd_prompt_attention) on gfx950.
+//
+//   out[i][h] = sum_{j <= i} softmax_j(scale * q_i . k_j) v_j   within a sequence
+//
+// The query heads of a KV head share its keys, so their rows are taken together:
+// row r of (sequence, KV head) is position r / G, head g * G + r % G (G = Hq / Hkv).
+// A tile of consecutive rows then spans few positions, which keeps the part of
+// its keys that the causal mask throws away small.  One workgroup computes one
+// tile over all its keys with a running maximum and sum; keys and values pass
+// through a ring of tiles in LDS, filled by asynchronous copies.
+#include <math.h>
+
+#include <algorithm>
+
+#include "ptd_async.hpp"
+#include "ptd_common.hpp"
+
+namespace {
+
+using ptd::dma16;
+using ptd::dma16_s;
+using ptd::lds_addr;
+using ptd::lds_barrier;
+using ptd::wait_vmcnt;
+using ptd::wait_vmcnt_le;
+
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using f32x16 = float __attribute__((ext_vector_type(16)));
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
+using i16x4 = short __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNegBig = -3.0e38f;  // running-max start: finite, below any score
+
+struct PromptParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  const int32_t* row_start;
+  void* out;
+  int32_t* dev_status;
+  int64_t ldq, ldk, ldv;  // elements
+  int B, N, Hq, Hkv, G;
+  long long items;  // tiles (an upper bound) * Hkv
+  float c;          // scale * log2(e)
+  int out_bf16;
+};
+
+// A tile: rows [r0, r0 + TM) of the M = n * G rows of a sequence that starts at
+// packed row `start`, KV head g.
+struct TileOf {
+  int start, n, r0, g;
+};
+
+// Tile number w of all sequences' tiles, each sequence's last (longest) first; false
+// past the last one.  Every lane of a wave takes part.
+template <int TM>
+__device__ __forceinline__ bool find_tile(const PromptParams& p, long long w, TileOf& t) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < p.B; b0 += PTD_WAVE) {
+    const int b = b0 + lane;
+    int s = 0, n = 0;
+    if (b < p.B) {
+      s = p.row_start[b];
+      const int e = p.row_start[b + 1];
+      if (s < 0 || e < s || e > p.N) {
+        ptd::report(p.dev_status, PTD_ERR_ROWS);
+      } else {
+        n = e - s;
+      }
+    }
+    // (n * G <= N * Hq / Hkv, checked on the host to fit an int)
+    const int nt = (n * p.G + TM - 1) / TM;
+    long long up = nt;
+#pragma unroll
+    for (int o = 1; o < PTD_WAVE; o <<= 1) {
+      const long long u = __shfl_up(up, o, PTD_WAVE);
+      up += lane >= o ? u : 0;
+    }
+    const uint64_t past = __ballot(up > w);
+    if (past) {
+      const int x = __builtin_ctzll(past);
+      t.start = __builtin_amdgcn_readlane(s, x);
+      t.n = __builtin_amdgcn_readlane(n, x);
+      const int after = static_cast<int>(__shfl(up, x, PTD_WAVE) - w);  // 1 .. nt
+      t.r0 = __builtin_amdgcn_readfirstlane(after - 1) * TM;
+      return true;
+    }
+    w -= __shfl(up, 63, PTD_WAVE);
+  }
+  return false;
+}
+
+// Workgroups are dealt round-robin over the 8 XCDs; a KV head's keys stay on as few of
+// them (one L2 each) as its share of the work allows.
+template <int TM>
+__device__ __forceinline__ bool my_tile(const PromptParams& p, TileOf& t) {
+  const long long id = blockIdx.x + static_cast<long long>(gridDim.x) * blockIdx.y;
+  if (id >= p.items) return false;
+  const int H = p.Hkv;
+  long long w;
+  if ((H & 7) == 0) {
+    const long long tiles = p.items / H, j = id >> 3;
+    t.g = static_cast<int>((id & 7) + 8 * (j / tiles));
+    w = j % tiles;
+  } else if ((8 % H) == 0) {
+    t.g = static_cast<int>((id & 7) % H);
+    w = (id >> 3) * (8 / H) + (id & 7) / H;
+  } else {
+    t.g = static_cast<int>(id % H);
+    w = id / H;
+  }
+  return find_tile<TM>(p, w, t);
+}
+
+__device__ __forceinline__ float max_xor32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_xor32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// Sum of a bf16 pair and an fp32 number (v_dot2_f32_bf16 with a pair of ones).
+__device__ __forceinline__ float sum_bf16x2(uint32_t w, float acc) {
+  using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), acc, false);
+}
+__device__ __forceinline__ u32x2 lds_read_tr16(const unsigned char* p) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((PTD_LDS i16x4*)p));
+}
+
+// ===========================================================================
+// bf16: v_mfma_f32_32x32x16_bf16
+// ===========================================================================
+// Scores are computed transposed, S^T = K Q^T, and the output as O^T = V^T P^T: a
+// lane owns query row l % 32 in both accumulators (keys, or columns of V, 8 * (i / 4) +
+// 4 * (l / 32) + i % 4 in element i), so the softmax needs one exchange between
+// two lanes, and only when the reference maximum moves.  V is read transposed from
+// its natural layout (ds_read_b64_tr_b16).
+//
+// LDS: a tile of 64 keys, K rows then V rows, row-major in 16-byte chunks.  Chunk c of row r
+// lies at c ^ swz(r): for K, so that 16 rows x one chunk (a quarter of a ds_read_b128)
+// fall on 16 different places of 256 bytes; for V, so that 4 rows x 4 chunks (half of a
+// transposing read) do.
+template <int D, int NT>
+struct Tiles {
+  static constexpr int KEYS = 64;
+  static constexpr int RB = D * 2;             // bytes per row
+  static constexpr int CH = RB / 16;           // chunks per row
+  static constexpr int PART = KEYS * RB;       // K (or V) bytes
+  static constexpr int SLOT = 2 * PART;
+  static constexpr int CPT = KEYS * CH / NT;   // copies per thread of K (and of V)
+  static constexpr int NS = NT == 512 ? 4 : 2; // tiles in the ring
+  static_assert(CPT * NT == KEYS * CH, "copies divide");
+  __device__ static int swz_k(int r) { return CH == 16 ? r & 15 : (r >> 1) & 7; }
+  __device__ static int swz_v(int r) {
+    return CH == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  }
+};
+
+template <int D, int NT>
+__global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
+  using L = Tiles<D, NT>;
+  constexpr int NW = NT / PTD_WAVE;
+  constexpr int TM = 32 * NW;
+  constexpr int DB = D / 16;  // QK^T steps
+  constexpr int DT = D / 32;  // 32-column parts of O
+  __shared__ __attribute__((aligned(16))) unsigned char smem[L::NS * L::SLOT];
+
+  TileOf t;
+  if (!my_tile<TM>(p, t)) return;
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63;
+  const int l32 = lane & 31, h = lane >> 5;
+  const int M = t.n * p.G;
+
+  // ---- this lane's query row
+  const int row = t.r0 + wave * 32 + l32;
+  const int rc = min(row, M - 1);
+  const int pos = rc / p.G, hq = t.g * p.G + rc % p.G;
+  const uint16_t* qr = static_cast<const uint16_t*>(p.q) + static_cast<size_t>(t.start + pos) * p.ldq +
+                       static_cast<size_t>(hq) * D + 8 * h;
+  bf16x8 qf[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qr + 16 * i));
+
+  // ---- tile copies
+  const uint16_t* kbase = static_cast<const uint16_t*>(p.k) + static_cast<size_t>(t.start) * p.ldk + static_cast<size_t>(t.g) * D;
+  const uint16_t* vbase = static_cast<const uint16_t*>(p.v) + static_cast<size_t>(t.start) * p.ldv + static_cast<size_t>(t.g) * D;
+  const uint32_t ring = lds_addr(smem);
+  int c_row[L::CPT], c_k[L::CPT], c_v[L::CPT];
+#pragma unroll
+  for (int u = 0; u < L::CPT; ++u) {
+    const int c = u * NT + tid;
+    c_row[u] = c / L::CH;
+    c_k[u] = ((c % L::CH) ^ L::swz_k(c_row[u])) * 8;
+    c_v[u] = ((c % L::CH) ^ L::swz_v(c_row[u])) * 8;
+  }
+  auto issue = [&](int tt) __attribute__((always_inline)) {
+    const uint32_t dst = ring + (tt % L::NS) * L::SLOT + wave * PTD_WAVE * 16;
+#pragma unroll
+    for (int u = 0; u < L::CPT; ++u) {
+      const size_t key = min(tt * L::KEYS + c_row[u], t.n - 1);  // past the sequence: its last row again
+      dma16(kbase + key * p.ldk + c_k[u], dst + u * NT * 16);
+      dma16(vbase + key * p.ldv + c_v[u], dst + L::PART + u * NT * 16);
+    }
+  };
+  // keys up to the tile's last position
+  const int last = (min(t.r0 + TM, M) - 1) / p.G;
+  const int ntiles = last / L::KEYS + 1;
+  // positions of the wave's rows
+  const int wave_lo = min(t.r0 + wave * 32, M - 1) / p.G;
+  const int wave_hi = min(t.r0 + wave * 32 + 31, M - 1) / p.G;
+
+  int koff[DB], voff[DT];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) koff[i] = l32 * L::RB + ((2 * i + h) ^ L::swz_k(l32)) * 16;
+  // source lane 4 j + q of a group of 16 points at V[key j][.. + 4 q]; the group's
+  // lane i receives its four keys' values of column i
+  const int l16 = lane & 15, vrow = 4 * h + (l16 >> 2), q4 = l16 & 3, dsub = (lane >> 4) & 1;
+#pragma unroll
+  for (int i = 0; i < DT; ++i) voff[i] = L::PART + vrow * L::RB + (q4 & 1) * 8;
+  auto v_at = [&](int dt, int r8) __attribute__((always_inline)) {  // r8: multiple of 8
+    const int r = vrow + r8;
+    return voff[dt] + r8 * L::RB + ((4 * dt + 2 * dsub + (q4 >> 1)) ^ L::swz_v(r)) * 16;
+  };
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m = kNegBig, nmc = -kNegBig * p.c, l = 0.f;
+
+  const int ninit = min(ntiles, L::NS - 1);
+  for (int tt = 0; tt < ninit; ++tt) issue(tt);
+  for (int tt = 0; tt < ntiles; ++tt) {
+    // tile tt has landed; every wave is done with tile tt - 1, whose place is filled next
+    wait_vmcnt_le((min(ntiles, tt + L::NS - 1) - tt - 1) * 2 * L::CPT);
+    lds_barrier();
+    if (tt + L::NS - 1 < ntiles) issue(tt + L::NS - 1);
+    const int k0 = tt * L::KEYS;
+    if (k0 > wave_hi) continue;  // uniform over the wave
+    const unsigned char* slot = smem + (tt % L::NS) * L::SLOT;
+    f32x16 s[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(slot + kb * 32 * L::RB + koff[i]));
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[kb], 0, 0, 0);
+      }
+    }
+    const bool masked = k0 + L::KEYS - 1 > wave_lo;
+    if (masked) {
+      const int lim = pos - k0 - 4 * h;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          s[kb][e] = 32 * kb + 8 * (e / 4) + e % 4 <= lim ? s[kb][e] : -INFINITY;
+    }
+    // weights 2^((s - m) c) as bf16 pairs, and the sum of what they were rounded to
+    uint32_t pw[2][8];
+    float ps;
+    auto exps = [&]() __attribute__((always_inline)) {
+      ps = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+          pw[kb][w] = ptd::cvt_pk_bf16(__builtin_amdgcn_exp2f(fmaf(s[kb][2 * w], p.c, nmc)),
+                                       __builtin_amdgcn_exp2f(fmaf(s[kb][2 * w + 1], p.c, nmc)));
+          ps = sum_bf16x2(pw[kb][w], ps);
+        }
+    };
+    exps();
+    // A row's reference m stays while its weights are far inside the fp32 range; else it
+    // moves to the row's maximum (always at its first keys), whatever the other rows do.
+    const uint64_t over = __ballot(!(ps <= 65536.f));
+    if (over) {
+      const bool mine = ((static_cast<uint32_t>(over) | static_cast<uint32_t>(over >> 32)) >> l32) & 1u;
+      float mx = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+      mx = max_xor32(mx);
+      const bool up = mine && mx > m;
+      const float alpha = up ? __builtin_amdgcn_exp2f((m - mx) * p.c) : 1.f;
+      m = up ? mx : m;
+      nmc = -m * p.c;
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= alpha;
+      exps();
+    }
+    l += ps;
+    bool odd = false;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pw[kb][4 * st], pw[kb][4 * st + 1], pw[kb][4 * st + 2], pw[kb][4 * st + 3]});
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const u32x2 a = lds_read_tr16(slot + v_at(dt, 32 * kb + 16 * st));
+          const u32x2 b = lds_read_tr16(slot + v_at(dt, 32 * kb + 16 * st + 8));
+          u32x4 vw = {a[0], a[1], b[0], b[1]};
+          if (masked) {  // 0 * inf must not reach the rows that do not see the key
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const bool lo = (vw[w] & 0x7F80u) == 0x7F80u, hi = (vw[w] & 0x7F800000u) == 0x7F800000u;
+              odd |= lo || hi;
+              vw[w] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+            }
+          }
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vw), pf, o[dt], 0, 0, 0);
+        }
+      }
+    if (masked && __any(odd)) {  // rare: what is not finite, to the rows that see it
+      for (int key = 0; key < L::KEYS; ++key) {
+        const bool sees = k0 + key <= pos;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int d = 32 * dt + 8 * (e / 4) + 4 * h + e % 4;
+            const uint32_t x = *reinterpret_cast<const uint16_t*>(slot + L::PART + key * L::RB + (((d >> 3) ^ L::swz_v(key)) * 16) + (d & 7) * 2);
+            const float f = __uint_as_float(x << 16);
+            if (sees && (x & 0x7F80u) == 0x7F80u) o[dt][e] += f;
+          }
+      }
+    }
+  }
+  if (row >= M) return;
+  const float inv = 1.f / sum_xor32(l);
+  const size_t off = (static_cast<size_t>(t.start + pos) * p.Hq + hq) * D + 4 * h;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      const f32x4 v = {o[dt][4 * e4] * inv, o[dt][4 * e4 + 1] * inv, o[dt][4 * e4 + 2] * inv, o[dt][4 * e4 + 3] * inv};
+      const size_t at = off + 32 * dt + 8 * e4;
+      if (p.out_bf16) {
+        const u32x2 w = {ptd::cvt_pk_bf16(v[0], v[1]), ptd::cvt_pk_bf16(v[2], v[3])};
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = w;
+      } else {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = v;
+      }
+    }
+}
+
+// ===========================================================================
+// fp32: v_mfma_f32_32x32x2_f32, the same scheme with tiles of 32 keys
+// ===========================================================================
+// A step of QK^T contracts the columns 8 j + 4 h + e (h: half of the wave) of one
+// 16-byte load; a step of PV the keys 8 * (i / 4) + 4 h + i % 4 whose weights
+// the lane owns in element i.  Bound by the matrix cores: 64 cycles per MFMA.
+constexpr int kF32Threads = 256;
+
+template <int D>
+__global__ void __launch_bounds__(kF32Threads, 2) k_prompt_f32(PromptParams p) {
+  constexpr int NT = kF32Threads, TM = 32 * (NT / PTD_WAVE);
+  constexpr int KEYS = 32, RB = D * 4, CH = RB / 16, PART = KEYS * RB, SLOT = 2 * PART, NS = 2;
+  constexpr int CPT = KEYS * CH / NT, KJ = D / 8, DT = D / 32;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[NS * SLOT];
+  auto swz_k = [](int r) __attribute__((always_inline)) { return r & 15; };
+  auto swz_v = [](int r) __attribute__((always_inline)) { return ((r >> 2) & 1) << 3; };
+
+  TileOf t;
+  if (!my_tile<TM>(p, t)) return;
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63;
+  const int l32 = lane & 31, h = lane >> 5;
+  const int M = t.n * p.G;
+  const int row = t.r0 + wave * 32 + l32;
+  const int rc = min(row, M - 1);
+  const int pos = rc / p.G, hq = t.g * p.G + rc % p.G;
+  const float* qr = static_cast<const float*>(p.q) + static_cast<size_t>(t.start + pos) * p.ldq +
+                    static_cast<size_t>(hq) * D + 4 * h;
+  f32x4 qf[KJ];
+#pragma unroll
+  for (int j = 0; j < KJ; ++j) qf[j] = *reinterpret_cast<const f32x4*>(qr + 8 * j);
+  const float* kbase = static_cast<const float*>(p.k) + static_cast<size_t>(t.start) * p.ldk + static_cast<size_t>(t.g) * D;
+  const float* vbase = static_cast<const float*>(p.v) + static_cast<size_t>(t.start) * p.ldv + static_cast<size_t>(t.g) * D;
+  const uint32_t ring = lds_addr(smem);
+  auto issue = [&](int tt) __attribute__((always_inline)) {
+    const uint32_t dst = ring + (tt % NS) * SLOT + wave * PTD_WAVE * 16;
+#pragma unroll
+    for (int u = 0; u < CPT; ++u) {
+      const int c = u * NT + tid, r = c / CH;
+      const size_t key = min(tt * KEYS + r, t.n - 1);
+      dma16(kbase + key * p.ldk + ((c % CH) ^ swz_k(r)) * 4, dst + u * NT * 16);
+      dma16(vbase + key * p.ldv + ((c % CH) ^ swz_v(r)) * 4, dst + PART + u * NT * 16);
+    }
+  };
+  const int ntiles = (min(t.r0 + TM, M) - 1) / p.G / KEYS + 1;
+  const int wave_lo = min(t.r0 + wave * 32, M - 1) / p.G;
+  const int wave_hi = min(t.r0 + wave * 32 + 31, M - 1) / p.G;
+  f32x16 o[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
+  float m = kNegBig, l = 0.f;
+  issue(0);
+  for (int tt = 0; tt < ntiles; ++tt) {
+    wait_vmcnt<0>();
+    lds_barrier();
+    if (tt + 1 < ntiles) issue(tt + 1);
+    const int k0 = tt * KEYS;
+    if (k0 > wave_hi) continue;
+    const unsigned char* slot = smem + (tt % NS) * SLOT;
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < KJ; ++j) {
+      const f32x4 kf = *reinterpret_cast<const f32x4*>(slot + l32 * RB + ((2 * j + h) ^ swz_k(l32)) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[j][e], s, 0, 0, 0);
+    }
+    const bool masked = k0 + KEYS - 1 > wave_lo;
+    if (masked) {
+      const int lim = pos - k0 - 4 * h;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 8 * (e / 4) + e % 4 <= lim ? s[e] : -INFINITY;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    mx = fmaxf(m, max_xor32(mx));
+    const float alpha = __builtin_amdgcn_exp2f((m - mx) * p.c);
+    m = mx;
+    const float nmc = -m * p.c;
+    float ps = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], p.c, nmc));
+      ps += s[e];
+    }
+    l = fmaf(l, alpha, ps);
+    if (__any(alpha != 1.f)) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= alpha;
+    }
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int r = 8 * (e / 4) + 4 * h + e % 4;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        float v = *reinterpret_cast<const float*>(slot + PART + r * RB + ((8 * dt + (l32 >> 2)) ^ swz_v(r)) * 16 + (l32 & 3) * 4);
+        if (masked) {
+          const bool bad = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u;
+          odd |= bad;
+          v = bad ? 0.f : v;
+        }
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[e], o[dt], 0, 0, 0);
+      }
+    }
+    if (masked && __any(odd)) {
+      for (int key = 0; key < KEYS; ++key) {
+        const bool sees = k0 + key <= pos;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int d = 32 * dt + 8 * (e / 4) + 4 * h + e % 4;
+            const float f = *reinterpret_cast<const float*>(slot + PART + key * RB + ((d >> 2) ^ swz_v(key)) * 16 + (d & 3) * 4);
+            if (sees && (__float_as_uint(f) & 0x7F800000u) == 0x7F800000u) o[dt][e] += f;
+          }
+      }
+    }
+  }
+  if (row >= M) return;
+  const float inv = 1.f / sum_xor32(l);
+  const size_t off = (static_cast<size_t>(t.start + pos) * p.Hq + hq) * D + 4 * h;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      const f32x4 v = {o[dt][4 * e4] * inv, o[dt][4 * e4 + 1] * inv, o[dt][4 * e4 + 2] * inv, o[dt][4 * e4 + 3] * inv};
+      const size_t at = off + 32 * dt + 8 * e4;
+      if (p.out_bf16) {
+        const u32x2 w = {ptd::cvt_pk_bf16(v[0], v[1]), ptd::cvt_pk_bf16(v[2], v[3])};
+        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = w;
+      } else {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = v;
+      }
+    }
+}
+
+}  // namespace
+
+extern "C" int ptd_prompt_attention(const void* q, const void* k, const void* v,
+                                    const int32_t* row_start, void* out,
+                                    const ptd_prompt_shape* shape, int32_t* dev_status,
+                                    void* stream) {
+  PTD_RETURN_IF(!shape || !row_start, PTD_ERR_NULL);
+  const ptd_prompt_shape& s = *shape;
+  PTD_RETURN_IF(s.N > 0 && (!q || !k || !v || !out), PTD_ERR_NULL);
+  PTD_RETURN_IF((s.in_dtype != PTD_F32 && s.in_dtype != PTD_BF16) ||
+                    (s.out_dtype != PTD_F32 && s.out_dtype != PTD_BF16),
+                PTD_ERR_DTYPE);
+  PTD_RETURN_IF(s.B < 1 || s.B > 65536 || s.N < 0 || s.Hq < 1 || s.Hkv < 1 || s.Hq % s.Hkv != 0, PTD_ERR_SHAPE);
+  PTD_RETURN_IF(s.D != 64 && s.D != 128, PTD_ERR_SHAPE);
+  PTD_RETURN_IF(static_cast<long long>(s.N) * s.Hq > 0x7FFFFFFFLL, PTD_ERR_SHAPE);
+  PTD_RETURN_IF(!(s.scale >= 0.f) || !isfinite(s.scale), PTD_ERR_SHAPE);
+  PromptParams prm;
+  const int64_t wq = static_cast<int64_t>(s.Hq) * s.D, wk = static_cast<int64_t>(s.Hkv) * s.D;
+  prm.ldq = s.ldq ? s.ldq : wq;
+  prm.ldk = s.ldk ? s.ldk : wk;
+  prm.ldv = s.ldv ? s.ldv : wk;
+  PTD_RETURN_IF(prm.ldq < wq || prm.ldk < wk || prm.ldv < wk, PTD_ERR_SHAPE);
+  const int per16 = s.in_dtype == PTD_F32 ? 4 : 8;
+  PTD_RETURN_IF(prm.ldq % per16 || prm.ldk % per16 || prm.ldv % per16 || !ptd_aligned(q, 16) ||
+                    !ptd_aligned(k, 16) || !ptd_aligned(v, 16) || !ptd_aligned(out, 16),
+                PTD_ERR_ALIGN);
+  if (s.N == 0) return PTD_OK;
+  prm.q = q;
+  prm.k = k;
+  prm.v = v;
+  prm.row_start = row_start;
+  prm.out = out;
+  prm.dev_status = dev_status;
+  prm.B = s.B;
+  prm.N = s.N;
+  prm.Hq = s.Hq;
+  prm.Hkv = s.Hkv;
+  prm.G = s.Hq / s.Hkv;
+  prm.c = (s.scale > 0.f ? s.scale : 1.0f / sqrtf(static_cast<float>(s.D))) * kLog2e;
+  prm.out_bf16 = s.out_dtype == PTD_BF16;
+  // every sequence has at most one tile that is not full
+  const auto items_of = [&](int tm) {
+    return (static_cast<long long>(s.N) * prm.G / tm + std::min(s.B, s.N)) * s.Hkv;
+  };
+  const auto grid_of = [&](long long items) {  // two dimensions: one holds fewer than 2^32 threads
+    const long long x = std::min<long long>((items + 7) / 8 * 8, 1 << 20);
+    return dim3(static_cast<unsigned>(x), static_cast<unsigned>((items + x - 1) / x));
+  };
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (s.in_dtype == PTD_F32) {
+    prm.items = items_of(128);
+    const dim3 grid = grid_of(prm.items);
+    if (s.D == 128) hipLaunchKernelGGL(k_prompt_f32<128>, grid, dim3(kF32Threads), 0, st, prm);
+    else hipLaunchKernelGGL(k_prompt_f32<64>, grid, dim3(kF32Threads), 0, st, prm);
+  } else {
+    prm.items = items_of(256);
+    const dim3 grid = grid_of(prm.items);
+    if (s.D == 128) hipLaunchKernelGGL((k_prompt_bf16<128, 512>), grid, dim3(512), 0, st, prm);
+    else hipLaunchKernelGGL((k_prompt_bf16<64, 512>), grid, dim3(512), 0, st, prm);
+  }
+  return ptd_launch_status();
+}

@@ -77,6 +77,10 @@ struct AttnParams {
   // sequence b lives in page page_table[b][r >> page_shift]; null: contiguous
   const int32_t* page_table;
   int page_shift, max_pages, num_pages;
+  // block scales: biased exponents [num_pages][Hkv][2^(page_shift - scale_shift)][2]
+  // (keys, values), read as 4-byte words
+  const uint32_t* scales;
+  int scale_shift;
   float scale;  // softmax scale
   float c;      // scale * log2(e)
   float precise;  // kPreciseFrac, or a smaller share
@@ -151,14 +155,14 @@ using i32x2 = int __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u32x2 lds_read_tr8(const unsigned char* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((PTD_LDS i32x2*)p));
 }
-// Eight OCP E4M3 values (bytes 0..7 of w) as eight bf16, exactly (every E4M3
-// value is a bf16 value): gfx950 v_cvt_scalef32_pk_bf16_fp8 with scale 1.
-__device__ __forceinline__ bf16x8 e4m3x8_to_bf16(u32x2 w) {
+// Eight OCP E4M3 values (bytes 0..7 of w) times a power of two as eight bf16,
+// exactly (every E4M3 value is a bf16 value): gfx950 v_cvt_scalef32_pk_bf16_fp8.
+__device__ __forceinline__ bf16x8 e4m3x8_to_bf16(u32x2 w, float scale) {
   const u32x4 r = {
-      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.0f, false)),
-      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], 1.0f, true)),
-      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], 1.0f, false)),
-      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], 1.0f, true))};
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], scale, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], scale, true)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], scale, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], scale, true))};
   return __builtin_bit_cast(bf16x8, r);
 }
 
@@ -195,10 +199,18 @@ struct Ring {
   }
 };
 
-template <int D, int QB, int WR, bool F8, bool PAGED, int NT = kThreads>
+// KIND: bf16 caches, E4M3 codes with one scale per KV head, or E4M3 codes with a
+// power-of-two scale per block of rows
+enum CacheKind { kBf16, kE4m3Head, kE4m3Block };
+
+template <int D, int QB, int WR, CacheKind KIND, bool PAGED, int NT = kThreads>
 __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
-  // F8: keys and values are OCP E4M3 codes (scaled per KV head), widened to
-  // bf16 exactly after the LDS reads; everything else is the bf16 kernel
+  // F8: keys and values are OCP E4M3 codes, widened to bf16 exactly after the
+  // LDS reads (with their block's scale for kE4m3Block); everything else is the
+  // bf16 kernel
+  constexpr bool F8 = KIND != kBf16;
+  constexpr bool BLK = KIND == kE4m3Block;
+  static_assert(!BLK || PAGED, "block scales live in pages");
   using KV = std::conditional_t<F8, uint8_t, uint16_t>;
   constexpr int ES = F8 ? 1 : 2;
   using R = Ring<D, ES, NT>;
@@ -479,8 +491,46 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
   struct KFrag {
     bf16x8 k[DB][2];
   };
+  // Block scales: the two exponents of sub-tile t's block (keys in bits 0..7,
+  // values in bits 8..15), by a scalar load -- a vector load would be waited for
+  // together with the ring copies behind it.  A block is at least a sub-tile, so
+  // one pair serves the wave's 32 keys.  e0 belongs to the wave's sub-tile of the
+  // round, e1 to the next round's; the one after that is requested at the head
+  // of a round, ahead of its wait and barrier.
+  using cu32 = const __attribute__((address_space(4))) uint32_t;
+  auto tile_scales = [&](int t) __attribute__((always_inline)) -> uint32_t {
+    if constexpr (!BLK) return 0u;
+    const int row0 = start + min(t, (end - start - 1) / R::SUB) * R::SUB;
+    const int ti = (row0 >> p.page_shift) - first_page;
+    uint32_t phys;
+    if (ti < 4 * PTD_WAVE) {
+      const uint32_t v0 = __builtin_amdgcn_readlane(pg[0], ti & 63);
+      const uint32_t v1 = __builtin_amdgcn_readlane(pg[1], ti & 63);
+      const uint32_t v2 = __builtin_amdgcn_readlane(pg[2], ti & 63);
+      const uint32_t v3 = __builtin_amdgcn_readlane(pg[3], ti & 63);
+      phys = ti < 64 ? v0 : ti < 128 ? v1 : ti < 192 ? v2 : v3;
+    } else {  // beyond the staged ids (reported by the sub-tile's copy)
+      phys = ((cu32*)p.page_table)[static_cast<size_t>(b) * p.max_pages + (row0 >> p.page_shift)];
+      phys = phys < static_cast<uint32_t>(p.num_pages) ? phys : 0u;
+    }
+    const size_t blk = ((static_cast<size_t>(phys) * p.Hkv + g) << (p.page_shift - p.scale_shift)) +
+                       ((row0 & ((1 << p.page_shift) - 1)) >> p.scale_shift);
+    return ((cu32*)p.scales)[blk >> 1] >> (16 * (blk & 1));
+  };
+  uint32_t e0 = 0, e1 = 0;
+  if constexpr (BLK) {
+    e0 = tile_scales(kg);
+    e1 = tile_scales(kg + WK);
+  }
+  // 2^(e - 127) of a byte
+  auto key_scale = [](uint32_t e) __attribute__((always_inline)) {
+    return BLK ? __uint_as_float((e & 255u) << 23) : 1.0f;
+  };
+  auto value_scale = [](uint32_t e) __attribute__((always_inline)) {
+    return BLK ? __uint_as_float((e << 15) & 0x7F800000u) : 1.0f;
+  };
   // K fragments of the sub-tile in `slot` (A operand: 16 keys x 32 d)
-  auto read_k = [&](int slot) __attribute__((always_inline)) -> KFrag {
+  auto read_k = [&](int slot, float sc) __attribute__((always_inline)) -> KFrag {
     KFrag f;
     const unsigned char* ks = smem + slot * R::SLOT;
 #pragma unroll
@@ -488,7 +538,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         if constexpr (F8)
-          f.k[db][kb] = e4m3x8_to_bf16(*reinterpret_cast<const u32x2*>(ks + kb * 16 * R::RB + koff[db]));
+          f.k[db][kb] = e4m3x8_to_bf16(*reinterpret_cast<const u32x2*>(ks + kb * 16 * R::RB + koff[db]), sc);
         else
           f.k[db][kb] = __builtin_bit_cast(
               bf16x8, *reinterpret_cast<const u32x4*>(ks + kb * 16 * R::RB + koff[db]));
@@ -518,12 +568,12 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
   struct VFrag {
     bf16x8 v[DT];
   };
-  auto read_v = [&](int slot) __attribute__((always_inline)) -> VFrag {
+  auto read_v = [&](int slot, float sc) __attribute__((always_inline)) -> VFrag {
     VFrag f;
     const unsigned char* vs = smem + slot * R::SLOT + R::PART;
     if constexpr (F8) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) f.v[dt] = e4m3x8_to_bf16(lds_read_tr8(vs + voff[dt]));
+      for (int dt = 0; dt < DT; ++dt) f.v[dt] = e4m3x8_to_bf16(lds_read_tr8(vs + voff[dt]), sc);
       return f;
     }
 #pragma unroll
@@ -658,8 +708,8 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
   float m[QB], nmc[QB];
   f32x4 ls[QB];  // row sums of p (all four elements: the lane's query column)
   // score scale in the exp2 domain; 8-bit keys carry their head's scale
-  const float c = F8 && p.k_scale ? p.c * p.k_scale[g] : p.c;
-  const float vsc = F8 && p.v_scale ? p.v_scale[g] : 1.0f;  // value scale
+  const float c = KIND == kE4m3Head && p.k_scale ? p.c * p.k_scale[g] : p.c;
+  const float vsc = KIND == kE4m3Head && p.v_scale ? p.v_scale[g] : 1.0f;  // value scale
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     m[qb] = kNegBig;
@@ -803,12 +853,13 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
   int rs = 0;   // slot refilled next (round rd - 1's slots, in order)
   Tile sc;      // PIPE: scores of the current round's sub-tile
   if (PIPE && wave_live && kg < ntiles) {
-    sc = qk(read_k(cs));
+    sc = qk(read_k(cs, key_scale(e0)));
     mask_tile(sc, kg);
   }
   // a round in general: waits by the count of copies issued so far, refills
   // (whole or last sub-tiles, contiguous or paged caches), masked sub-tiles
   auto round = [&](int rd) __attribute__((always_inline)) {
+      const uint32_t e2 = tile_scales((rd + 2) * WK + kg);
       const bool do_wait = PIPE ? rd + 1 < nrounds : rd >= 1;
       if (do_wait) {
         if (rd >= 1 && rd <= steady_end) {
@@ -840,19 +891,19 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
           // wave's last sub-tile the next-tile QK^T works on whatever the slot
           // holds and its result is dropped: one code path keeps the register
           // allocation of this loop within the two-waves-per-SIMD budget.
-          const KFrag kf = read_k(ns);
+          const KFrag kf = read_k(ns, key_scale(e1));
           exp_tile(sc, pv, pm);
           PFrag pf;
           const unsigned precise = to_p(sc, pv, pm, pf);
           Tile sn = qk(kf);
-          const VFrag vf = read_v(cs);
+          const VFrag vf = read_v(cs, value_scale(e0));
           pv_acc(vf, pf, precise);
           if (j + WK < ntiles) mask_tile(sn, j + WK);
           sc = sn;
         } else {
-          sc = qk(read_k(cs));
+          sc = qk(read_k(cs, key_scale(e0)));
           mask_tile(sc, j);
-          const VFrag vf = read_v(cs);
+          const VFrag vf = read_v(cs, value_scale(e0));
           exp_tile(sc, pv, pm);
           PFrag pf;
           const unsigned precise = to_p(sc, pv, pm, pf);
@@ -860,6 +911,8 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
         }
       }
       cs = ns;
+      e0 = e1;
+      e1 = e2;
   };
   // Steady rounds: every refill of the round is a whole sub-tile below t_mask0, so this round's and the next round's
   // sub-tiles need no masking either; the wait count is the constant, the
@@ -886,6 +939,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
   }
   const int steady_hi = t_steady >= R::NS + WK ? (t_steady - R::NS - WK) / WK + 1 : 0;
   auto round_steady = [&](int rd) __attribute__((always_inline)) {
+    const uint32_t e2 = tile_scales((rd + 2) * WK + kg);
     wait_vmcnt<(R::NS - (2 + (PIPE ? 1 : 0)) * WK) * R::DPS>();
     lds_barrier();
 #pragma unroll
@@ -912,7 +966,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
     if constexpr (PIPE) {
       if (wave_live) {
         float pv[QB][8], pm[QB];
-        const KFrag kf = read_k(ns);
+        const KFrag kf = read_k(ns, key_scale(e1));
         exp_tile(sc, pv, pm);
         Tile sn = qk(kf);
         // the K reads, a few exponentials, then one QK^T MFMA per three
@@ -944,7 +998,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
           for (int w = 0; w < 4; ++w) ph[w] = ptd::cvt_pk_bf16(pv[qb][2 * w], pv[qb][2 * w + 1]);
           pf.hi[qb] = __builtin_bit_cast(bf16x8, ph);
         }
-        const VFrag vf = read_v(cs);
+        const VFrag vf = read_v(cs, value_scale(e0));
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -980,8 +1034,8 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
     } else {
       if (wave_live) {
         float pv[QB][8], pm[QB];
-        sc = qk(read_k(cs));
-        const VFrag vf = read_v(cs);
+        sc = qk(read_k(cs, key_scale(e0)));
+        const VFrag vf = read_v(cs, value_scale(e0));
         exp_tile(sc, pv, pm);
         PFrag pf;
         const unsigned precise = to_p(sc, pv, pm, pf);
@@ -989,6 +1043,8 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
       }
     }
     cs = ns;
+    e0 = e1;
+    e1 = e2;
   };
   int rd0 = 0;
   if (steady_hi >= 1) {
@@ -1035,7 +1091,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
       }
     } else if (r < m_live) {
       const size_t prow = ((static_cast<size_t>(split) * p.B + b) * p.Hkv + g) * p.M + r;
-      *reinterpret_cast<f32x4*>(p.part_o + prow * D + 16 * dt + 4 * l4) = F8 ? acc * vsc : acc;
+      *reinterpret_cast<f32x4*>(p.part_o + prow * D + 16 * dt + 4 * l4) = KIND == kE4m3Head ? acc * vsc : acc;
       if (dt == 0 && l4 == 0) p.part_ml[prow] = make_float2(mc, den);
     }
   };
@@ -1519,16 +1575,16 @@ bool make_plan(const ptd_attn_shape* s, int T, Plan* pl) {
   return true;
 }
 
-template <int D, bool F8, bool PAGED>
+template <int D, CacheKind KIND, bool PAGED>
 void launch_mfma(const Plan& pl, const AttnParams& prm, hipStream_t st) {
   const dim3 grid(prm.B * prm.Hkv * pl.passes * pl.splits);
   if (pl.nt == 256) {
-    hipLaunchKernelGGL((k_attn_mfma<D, 2, 4, F8, PAGED, 256>), grid, dim3(256), 0, st, prm);
+    hipLaunchKernelGGL((k_attn_mfma<D, 2, 4, KIND, PAGED, 256>), grid, dim3(256), 0, st, prm);
     return;
   }
   const dim3 block(kThreads);
 #define PTD_MFMA_CASE(qb_, wr_) \
-  if (pl.QB == qb_ && pl.WR == wr_) { hipLaunchKernelGGL((k_attn_mfma<D, qb_, wr_, F8, PAGED>), grid, block, 0, st, prm); return; }
+  if (pl.QB == qb_ && pl.WR == wr_) { hipLaunchKernelGGL((k_attn_mfma<D, qb_, wr_, KIND, PAGED>), grid, block, 0, st, prm); return; }
   PTD_MFMA_CASE(1, 2) PTD_MFMA_CASE(2, 2) PTD_MFMA_CASE(2, 4)
 #undef PTD_MFMA_CASE
 }
@@ -1582,8 +1638,9 @@ int attention_impl(const void* q, const void* k_cache, const void* v_cache,
                    const ptd_attn_shape* shape, const uint64_t* mask, void* workspace,
                    size_t workspace_bytes, int32_t* dev_status, void* stream,
                    const int32_t* page_table, int page_shift, int max_pages, int num_pages,
-                   bool f8 = false, const float* k_scale = nullptr,
-                   const float* v_scale = nullptr, bool noalloc = false) {
+                   CacheKind kind = kBf16, const float* k_scale = nullptr,
+                   const float* v_scale = nullptr, bool noalloc = false,
+                   const uint8_t* scales = nullptr, int scale_shift = 0) {
   PTD_RETURN_IF(!q || !k_cache || !v_cache || !kv_len || !parent || !out || !shape,
                 PTD_ERR_NULL);
   if (shape->in_dtype != PTD_F32 && shape->in_dtype != PTD_BF16) return PTD_ERR_DTYPE;
@@ -1661,6 +1718,8 @@ int attention_impl(const void* q, const void* k_cache, const void* v_cache,
   prm.page_shift = page_shift;
   prm.max_pages = max_pages;
   prm.num_pages = num_pages;
+  prm.scales = reinterpret_cast<const uint32_t*>(scales);
+  prm.scale_shift = scale_shift;
   if (pl.splits > 1) {
     const size_t rows = static_cast<size_t>(pl.splits) * prm.B * prm.Hkv * prm.M;
     prm.part_ml = reinterpret_cast<float2*>(prm.part_o + rows * shape->D);
@@ -1668,9 +1727,12 @@ int attention_impl(const void* q, const void* k_cache, const void* v_cache,
   if (pl.mfma) {
     const auto launch = [&](auto paged) {
       constexpr bool kPaged = decltype(paged)::value;
-      if (f8) launch_mfma<128, true, kPaged>(pl, prm, st);  // (D = 128 checked by the entry point)
-      else if (shape->D == 128) launch_mfma<128, false, kPaged>(pl, prm, st);
-      else launch_mfma<64, false, kPaged>(pl, prm, st);
+      if constexpr (kPaged) {  // (8-bit caches: D = 128 checked by the entry points)
+        if (kind == kE4m3Block) return launch_mfma<128, kE4m3Block, true>(pl, prm, st);
+      }
+      if (kind == kE4m3Head) launch_mfma<128, kE4m3Head, kPaged>(pl, prm, st);
+      else if (shape->D == 128) launch_mfma<128, kBf16, kPaged>(pl, prm, st);
+      else launch_mfma<64, kBf16, kPaged>(pl, prm, st);
     };
     if (page_table) launch(std::true_type{});
     else launch(std::false_type{});
@@ -1727,7 +1789,7 @@ extern "C" int ptd_tree_attention_noalloc(const void* q, const void* k_cache, co
                                           const ptd_attn_shape* shape, const uint64_t* mask,
                                           int32_t* dev_status, void* stream) {
   return attention_impl(q, k_cache, v_cache, kv_len, tree_len, parent, T, out, shape, mask,
-                        nullptr, 0, dev_status, stream, nullptr, 0, 0, 0, false, nullptr, nullptr,
+                        nullptr, 0, dev_status, stream, nullptr, 0, 0, 0, kBf16, nullptr, nullptr,
                         true);
 }
 
@@ -1744,7 +1806,7 @@ extern "C" int ptd_tree_attention_fp8kv(const void* q, const void* k_cache, cons
   PTD_RETURN_IF((k_scale && !ptd_aligned(k_scale, 4)) || (v_scale && !ptd_aligned(v_scale, 4)),
                 PTD_ERR_ALIGN);
   return attention_impl(q, k_cache, v_cache, kv_len, tree_len, parent, T, out, shape, nullptr,
-                        workspace, workspace_bytes, dev_status, stream, nullptr, 0, 0, 0, true,
+                        workspace, workspace_bytes, dev_status, stream, nullptr, 0, 0, 0, kE4m3Head,
                         k_scale, v_scale);
 }
 
@@ -1797,5 +1859,27 @@ extern "C" int ptd_tree_attention_paged_fp8kv(const void* q, const ptd_kv_pages*
                 PTD_ERR_ALIGN);
   return attention_impl(q, kv->k_pages, kv->v_pages, kv_len, tree_len, parent, T, out, shape,
                         nullptr, workspace, workspace_bytes, dev_status, stream, kv->page_table,
-                        shift, kv->max_pages, kv->num_pages, true, k_scale, v_scale);
+                        shift, kv->max_pages, kv->num_pages, kE4m3Head, k_scale, v_scale);
+}
+
+extern "C" int ptd_tree_attention_paged_fp8blk(const void* q, const ptd_kv_pages_fp8blk* kv,
+                                               const int32_t* kv_len, const int32_t* tree_len,
+                                               const int32_t* parent, int32_t T, void* out,
+                                               const ptd_attn_shape* shape, void* workspace,
+                                               size_t workspace_bytes, int32_t* dev_status,
+                                               void* stream) {
+  PTD_RETURN_IF(!kv || !kv->scales, PTD_ERR_NULL);
+  const ptd_kv_pages pages = {kv->k_pages, kv->v_pages, kv->page_table,
+                              kv->page_size, kv->max_pages, kv->num_pages};
+  int shift = 0;
+  const int rc = paged_args(&pages, shape, &shift);
+  if (rc != PTD_OK) return rc;
+  const int sr = kv->scale_rows;
+  PTD_RETURN_IF(shape->D != 128 || (sr != 32 && sr != 64 && sr != 128) || sr > kv->page_size,
+                PTD_ERR_SHAPE);
+  PTD_RETURN_IF(!ptd_aligned(kv->scales, 4), PTD_ERR_ALIGN);
+  return attention_impl(q, kv->k_pages, kv->v_pages, kv_len, tree_len, parent, T, out, shape,
+                        nullptr, workspace, workspace_bytes, dev_status, stream, kv->page_table,
+                        shift, kv->max_pages, kv->num_pages, kE4m3Block, nullptr, nullptr, false,
+                        kv->scales, sr == 32 ? 5 : sr == 64 ? 6 : 7);
 }

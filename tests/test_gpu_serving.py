@@ -1,0 +1,131 @@
+"""GPU check of the serving path as a whole: prompts are attended to and written into
+8-bit pages that ptd_page_plan hands out, then steps of a draft tree follow (tree rows
+written, attended to, verified, the accepted ones committed), sequences finish and
+new prompts take their pages.  Every output is compared with a plain 64-bit implementation
+on the rows that the cache stands for, the rows with those written."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import oracle as O
+import ref64
+import workloads as W
+
+pytestmark = pytest.mark.gpu
+TOL = 2e-3
+
+
+@pytest.fixture(scope="module")
+def P():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2607_10661_amd as lib
+    return lib
+
+
+def i32(x):
+    return torch.as_tensor(np.ascontiguousarray(x), dtype=torch.int32).cuda()
+
+
+def bits(x):
+    return x.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def cached(kv, tables, b, n):
+    """Rows 0 .. n - 1 of sequence b as bf16 [Hkv][n][128] (exact), for keys and values."""
+    ids = tables.page_table[b, :-(-n // kv.page_size)].long()
+    got = []
+    for kind, x in enumerate((kv.k_pages, kv.v_pages)):
+        y = x[ids].view(torch.float8_e4m3fn).double().unflatten(2, (-1, kv.scale_rows))
+        y = (y * torch.exp2(kv.scales[ids][..., kind].double() - 127)[..., None, None]).flatten(2, 3)
+        got.append(y.transpose(0, 1).reshape(kv.Hkv, -1, 128)[:, :n].bfloat16())
+    return got
+
+
+@pytest.mark.parametrize("Hq,Hkv,page,S", [(8, 2, 64, 32), (4, 4, 128, 128)])
+def test_prompts_steps_and_turnover(P, Hq, Hkv, page, S):
+    B, T, per, steps = 4, 24, 8, 5
+    r, rng = random.Random(Hq), np.random.default_rng(Hq)
+    g = torch.Generator("cuda").manual_seed(Hq)
+    tables = P.PageTables(B, page, per, B * per)
+    kv = P.BlockKV(B * per, Hkv, page, S)
+    st = i32([0])
+    true = [[torch.zeros((0, Hkv, 128)), torch.zeros((0, Hkv, 128))] for _ in range(B)]  # rows as computed
+    lens = [0] * B
+
+    def rows(n):
+        x = torch.randn((n, Hq + 2 * Hkv, 128), generator=g, device="cuda").bfloat16()
+        return x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+
+    def check_rows():
+        for b in range(B):
+            if lens[b]:
+                for got, want in zip(cached(kv, tables, b, lens[b]), true[b]):
+                    x, y = want.double().transpose(0, 1), got.double().cpu()
+                    # half a step of a code, twice the least step of the block's scale (a row
+                    # can have been coded under a larger one before)
+                    top = x.abs().amax()
+                    assert ((x - y).abs() <= 2.0 ** -4 * x.abs() + 2.0 ** -9 * 2 * top / 224).all()
+
+    def admit(prompts):
+        """prompts[b] rows for the sequences that start anew, none for the others."""
+        q, k, v = rows(sum(prompts))
+        start, slots, pos = tables.plan(i32(lens), i32(prompts), sum(prompts), dev_status=st)
+        out = P.prompt_attention(q, k, v, start, dev_status=st, out_dtype=torch.float32)
+        kv.write(k, v, slots, dev_status=st)
+        s = start.tolist()
+        ref, mag, _ = ref64.causal(q, k, v, s, 128 ** -0.5)
+        assert ((out.double() - ref).abs() <= (2.0 ** -8 + 2.0 ** -11) * mag + 2.0 ** -8 * ref.abs()).all()
+        for b in range(B):
+            if prompts[b]:
+                assert pos[s[b]:s[b + 1]].tolist() == list(range(prompts[b]))
+                true[b] = [x[s[b]:s[b + 1]].cpu() for x in (k, v)]
+                lens[b] = prompts[b]
+
+    admit([100, 1, 257, 64])
+    check_rows()
+    for n in range(steps):
+        parent = np.stack([W.tree_uniform(rng, T)[0] for _ in range(B)])
+        tokens = np.stack([W.sibling_distinct_tokens(rng, parent[b], 500) for b in range(B)])
+        q, k, v = rows(B * T)
+        _, slots, _ = tables.plan(i32(lens), i32([T] * B), B * T, T, st)
+        kv.write(k, v, slots, dev_status=st)
+        out = kv.tree_attention(q.reshape(B, T, Hq, 128).contiguous(), tables.page_table, i32(lens), i32(parent),
+                                out_dtype=torch.float32, dev_status=st)
+        for b in range(B):
+            kc, vc = cached(kv, tables, b, lens[b] + T)
+            at = [(0, r.randrange(Hq), r.randrange(T)) for _ in range(6)]
+            ref = O.attention_rows(bits(q[b * T:(b + 1) * T][None]), bits(kc[None]), bits(vc[None]),
+                                   np.array([lens[b]], np.int32), parent[b:b + 1], 128 ** -0.5, at)
+            for x, (_, h, i) in zip(ref, at):
+                assert np.abs(out[b, i, h].cpu().numpy() - x).max() <= TOL
+        # a planted path is accepted
+        argmax = np.full((B, T + 1), 777, np.int32)
+        for b in range(B):
+            a, path = r.randrange(-1, T), []
+            while a >= 0:
+                path.append(a)
+                a = int(parent[b, a])
+            prev = 0
+            for a in path[::-1]:
+                argmax[b, prev] = tokens[b, a]
+                prev = a + 1
+        al, an, _ = P.verify(i32(argmax), i32(tokens), i32(parent), dev_status=st)
+        _, slots, pos = tables.plan(i32(lens), al, B * T, T, st)
+        kv.write(k, v, slots, src=an, rows_per_seq=T, dev_status=st)
+        for b, m in enumerate(al.tolist()):
+            src = [b * T + x for x in an[b, :m].tolist()]
+            true[b] = [torch.cat((x, y[src].cpu())) for x, y in zip(true[b], (k, v))]
+            assert pos[b * T:b * T + m].tolist() == list(range(lens[b], lens[b] + m))
+            lens[b] += m
+        check_rows()
+        assert tables.num_held.tolist() == [-(-x // page) for x in lens]
+        if n == 2:  # two sequences finish, new prompts take their pages
+            lens[0] = lens[2] = 0
+            tables.plan(i32(lens), i32([0] * B), 0, 1 * 0, st)
+            admit([33, 0, 130, 0])
+            check_rows()
+    tables.plan(i32([0] * B), i32([0] * B), 0, 0, st)
+    assert tables.num_free.item() == B * per and st.item() == 0
