@@ -11,6 +11,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ptd_async.hpp"
 #include "ptd_common.hpp"
@@ -18,7 +19,7 @@
 namespace {
 
 using ptd::dma16;
-using ptd::dma16_s;
+using ptd::dma16_s2;
 using ptd::lds_addr;
 using ptd::lds_barrier;
 using ptd::wait_vmcnt;
@@ -46,6 +47,7 @@ struct PromptParams {
   long long items;  // tiles (an upper bound) * Hkv
   float c;          // scale * log2(e)
   int out_bf16;
+  int wide;  // 64 rows span 2 GiB and more: no 32-bit offsets
 };
 
 // A tile: rows [r0, r0 + TM) of the M = n * G rows of a sequence that starts at
@@ -54,8 +56,16 @@ struct TileOf {
   int start, n, r0, g;
 };
 
-// Tile number w of all sequences' tiles, each sequence's last (longest) first; false
-// past the last one.  Every lane of a wave takes part.
+__device__ __forceinline__ int wave_sum_i32(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, PTD_WAVE);
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+// Tile number w of all sequences' tiles; false past the last one.  Up to 64 sequences:
+// longest tiles first (tile k of a sequence has k + 1 times the first one's keys), so that
+// the short ones fill in at the end; more: sequence by sequence, each one's
+// longest first.  Every lane of a wave takes part.
 template <int TM>
 __device__ __forceinline__ bool find_tile(const PromptParams& p, long long w, TileOf& t) {
   const int lane = threadIdx.x & 63;
@@ -73,22 +83,49 @@ __device__ __forceinline__ bool find_tile(const PromptParams& p, long long w, Ti
     }
     // (n * G <= N * Hq / Hkv, checked on the host to fit an int)
     const int nt = (n * p.G + TM - 1) / TM;
-    long long up = nt;
+    int x, k;  // sequence (lane), tile of it
+    if (p.B == 1) {
+      if (w >= __builtin_amdgcn_readfirstlane(nt)) return false;
+      x = 0;
+      k = __builtin_amdgcn_readfirstlane(nt) - 1 - static_cast<int>(w);
+    } else if (p.B <= PTD_WAVE) {
+      // level k: the tiles k of the sequences that have one; above it lie
+      // sum max(nt - k - 1, 0) tiles.  w belongs to the least k with no more than w above it.
+      if (w >= wave_sum_i32(nt)) return false;
+      int most = nt;
 #pragma unroll
-    for (int o = 1; o < PTD_WAVE; o <<= 1) {
-      const long long u = __shfl_up(up, o, PTD_WAVE);
-      up += lane >= o ? u : 0;
+      for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, PTD_WAVE));
+      int lo = 0, hi = __builtin_amdgcn_readfirstlane(most) - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (wave_sum_i32(max(nt - mid - 1, 0)) <= w) hi = mid;
+        else lo = mid + 1;
+      }
+      k = lo;
+      const int above = wave_sum_i32(max(nt - k - 1, 0));
+      // the (w - above)-th of the sequences with more than k tiles
+      uint64_t has = __ballot(nt > k);
+      for (int i = static_cast<int>(w) - above; i > 0; --i) has &= has - 1;
+      x = __builtin_ctzll(has);
+    } else {
+      long long up = nt;
+#pragma unroll
+      for (int o = 1; o < PTD_WAVE; o <<= 1) {
+        const long long u = __shfl_up(up, o, PTD_WAVE);
+        up += lane >= o ? u : 0;
+      }
+      const uint64_t past = __ballot(up > w);
+      if (!past) {
+        w -= __shfl(up, 63, PTD_WAVE);
+        continue;
+      }
+      x = __builtin_ctzll(past);
+      k = __builtin_amdgcn_readfirstlane(static_cast<int>(__shfl(up, x, PTD_WAVE) - w) - 1);
     }
-    const uint64_t past = __ballot(up > w);
-    if (past) {
-      const int x = __builtin_ctzll(past);
-      t.start = __builtin_amdgcn_readlane(s, x);
-      t.n = __builtin_amdgcn_readlane(n, x);
-      const int after = static_cast<int>(__shfl(up, x, PTD_WAVE) - w);  // 1 .. nt
-      t.r0 = __builtin_amdgcn_readfirstlane(after - 1) * TM;
-      return true;
-    }
-    w -= __shfl(up, 63, PTD_WAVE);
+    t.start = __builtin_amdgcn_readlane(s, x);
+    t.n = __builtin_amdgcn_readlane(n, x);
+    t.r0 = k * TM;
+    return true;
   }
   return false;
 }
@@ -102,9 +139,9 @@ __device__ __forceinline__ bool my_tile(const PromptParams& p, TileOf& t) {
   const int H = p.Hkv;
   long long w;
   if ((H & 7) == 0) {
-    const long long tiles = p.items / H, j = id >> 3;
-    t.g = static_cast<int>((id & 7) + 8 * (j / tiles));
-    w = j % tiles;
+    const long long j = id >> 3;
+    t.g = static_cast<int>((id & 7) + 8 * (j % (H >> 3)));
+    w = j / (H >> 3);
   } else if ((8 % H) == 0) {
     t.g = static_cast<int>((id & 7) % H);
     w = (id >> 3) * (8 / H) + (id & 7) / H;
@@ -169,6 +206,7 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
   constexpr int DB = D / 16;  // QK^T steps
   constexpr int DT = D / 32;  // 32-column parts of O
   __shared__ __attribute__((aligned(16))) unsigned char smem[L::NS * L::SLOT];
+  __shared__ int s_odd[2][NW];  // by parity of the tile, for each wave
 
   TileOf t;
   if (!my_tile<TM>(p, t)) return;
@@ -192,28 +230,34 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
   const uint16_t* kbase = static_cast<const uint16_t*>(p.k) + static_cast<size_t>(t.start) * p.ldk + static_cast<size_t>(t.g) * D;
   const uint16_t* vbase = static_cast<const uint16_t*>(p.v) + static_cast<size_t>(t.start) * p.ldv + static_cast<size_t>(t.g) * D;
   const uint32_t ring = lds_addr(smem);
-  int c_row[L::CPT], c_k[L::CPT], c_v[L::CPT];
+  uint32_t c_k[L::CPT], c_v[L::CPT];  // byte offsets of this thread's chunks in a tile
 #pragma unroll
   for (int u = 0; u < L::CPT; ++u) {
-    const int c = u * NT + tid;
-    c_row[u] = c / L::CH;
-    c_k[u] = ((c % L::CH) ^ L::swz_k(c_row[u])) * 8;
-    c_v[u] = ((c % L::CH) ^ L::swz_v(c_row[u])) * 8;
+    const int c = u * NT + tid, r = c / L::CH;
+    c_k[u] = static_cast<uint32_t>((r * p.ldk + ((c % L::CH) ^ L::swz_k(r)) * 8) * 2);
+    c_v[u] = static_cast<uint32_t>((r * p.ldv + ((c % L::CH) ^ L::swz_v(r)) * 8) * 2);
   }
   auto issue = [&](int tt) __attribute__((always_inline)) {
     const uint32_t dst = ring + (tt % L::NS) * L::SLOT + wave * PTD_WAVE * 16;
+    if ((tt + 1) * L::KEYS <= t.n && !p.wide) {  // uniform: a whole tile, from scalar bases
+      const uint16_t* kt = kbase + static_cast<size_t>(tt) * L::KEYS * p.ldk;
+      const uint16_t* vt = vbase + static_cast<size_t>(tt) * L::KEYS * p.ldv;
 #pragma unroll
-    for (int u = 0; u < L::CPT; ++u) {
-      const size_t key = min(tt * L::KEYS + c_row[u], t.n - 1);  // past the sequence: its last row again
-      dma16(kbase + key * p.ldk + c_k[u], dst + u * NT * 16);
-      dma16(vbase + key * p.ldv + c_v[u], dst + L::PART + u * NT * 16);
+      for (int u = 0; u < L::CPT; ++u) dma16_s2(kt, c_k[u], dst + u * NT * 16, vt, c_v[u], dst + L::PART + u * NT * 16);
+    } else {
+#pragma unroll
+      for (int u = 0; u < L::CPT; ++u) {
+        const int c = u * NT + tid, r = c / L::CH;
+        const size_t key = min(tt * L::KEYS + r, t.n - 1);  // past the sequence: its last row again
+        dma16(kbase + key * p.ldk + ((c % L::CH) ^ L::swz_k(r)) * 8, dst + u * NT * 16);
+        dma16(vbase + key * p.ldv + ((c % L::CH) ^ L::swz_v(r)) * 8, dst + L::PART + u * NT * 16);
+      }
     }
   };
   // keys up to the tile's last position
   const int last = (min(t.r0 + TM, M) - 1) / p.G;
   const int ntiles = last / L::KEYS + 1;
-  // positions of the wave's rows
-  const int wave_lo = min(t.r0 + wave * 32, M - 1) / p.G;
+  // last position of the wave's rows
   const int wave_hi = min(t.r0 + wave * 32 + 31, M - 1) / p.G;
 
   int koff[DB], voff[DT];
@@ -238,13 +282,9 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
 
   const int ninit = min(ntiles, L::NS - 1);
   for (int tt = 0; tt < ninit; ++tt) issue(tt);
-  for (int tt = 0; tt < ntiles; ++tt) {
-    // tile tt has landed; every wave is done with tile tt - 1, whose place is filled next
-    wait_vmcnt_le((min(ntiles, tt + L::NS - 1) - tt - 1) * 2 * L::CPT);
-    lds_barrier();
-    if (tt + L::NS - 1 < ntiles) issue(tt + L::NS - 1);
+  auto tile = [&](auto masked_tag, int tt) __attribute__((always_inline)) {
+    constexpr bool masked = decltype(masked_tag)::value;
     const int k0 = tt * L::KEYS;
-    if (k0 > wave_hi) continue;  // uniform over the wave
     const unsigned char* slot = smem + (tt % L::NS) * L::SLOT;
     f32x16 s[2];
 #pragma unroll
@@ -257,8 +297,7 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[kb], 0, 0, 0);
       }
     }
-    const bool masked = k0 + L::KEYS - 1 > wave_lo;
-    if (masked) {
+    if constexpr (masked) {
       const int lim = pos - k0 - 4 * h;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -302,7 +341,6 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
       exps();
     }
     l += ps;
-    bool odd = false;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -312,31 +350,78 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
         for (int dt = 0; dt < DT; ++dt) {
           const u32x2 a = lds_read_tr16(slot + v_at(dt, 32 * kb + 16 * st));
           const u32x2 b = lds_read_tr16(slot + v_at(dt, 32 * kb + 16 * st + 8));
-          u32x4 vw = {a[0], a[1], b[0], b[1]};
-          if (masked) {  // 0 * inf must not reach the rows that do not see the key
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const bool lo = (vw[w] & 0x7F80u) == 0x7F80u, hi = (vw[w] & 0x7F800000u) == 0x7F800000u;
-              odd |= lo || hi;
-              vw[w] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-            }
-          }
+          const u32x4 vw = {a[0], a[1], b[0], b[1]};
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vw), pf, o[dt], 0, 0, 0);
         }
       }
-    if (masked && __any(odd)) {  // rare: what is not finite, to the rows that see it
-      for (int key = 0; key < L::KEYS; ++key) {
-        const bool sees = k0 + key <= pos;
+  };
+  // A tile that not every row sees whole: 0 * inf must not reach a row that does not
+  // see the key.  Each thread clears what is not finite from the value chunks that it
+  // copied, before the barrier that shows them to the others; the rows that do see such
+  // a value get it after the tile, from memory (rare).
+  auto clear_odd = [&](int tt) __attribute__((always_inline)) {
+    unsigned char* mine = smem + (tt % L::NS) * L::SLOT + L::PART + tid * 16;
+    uint32_t top = 0;
+    u32x4 w[L::CPT];
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+    for (int u = 0; u < L::CPT; ++u) {
+      w[u] = *reinterpret_cast<const u32x4*>(mine + u * NT * 16);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int d = 32 * dt + 8 * (e / 4) + 4 * h + e % 4;
-            const uint32_t x = *reinterpret_cast<const uint16_t*>(slot + L::PART + key * L::RB + (((d >> 3) ^ L::swz_v(key)) * 16) + (d & 7) * 2);
-            const float f = __uint_as_float(x << 16);
-            if (sees && (x & 0x7F80u) == 0x7F80u) o[dt][e] += f;
-          }
+      for (int x = 0; x < 4; ++x) top |= (w[u][x] & 0x7F807F80u) + 0x00800080u;  // bits 15, 31: exponent all ones
+    }
+    const bool odd = __any((top & 0x80008000u) != 0);
+    if (odd) {
+#pragma unroll
+      for (int u = 0; u < L::CPT; ++u) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          w[u][x] &= ((w[u][x] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[u][x] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
+        *reinterpret_cast<u32x4*>(mine + u * NT * 16) = w[u];
       }
+    }
+    if (lane == 0) s_odd[tt & 1][wave] = odd;
+  };
+  auto add_odd = [&](int tt) __attribute__((always_inline)) {
+    int any = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) any |= s_odd[tt & 1][w];
+    if (!__builtin_amdgcn_readfirstlane(any)) return;
+    const int end = min((tt + 1) * L::KEYS, t.n);
+    for (int key = tt * L::KEYS; key < end; ++key) {
+      const uint16_t* vr = vbase + static_cast<size_t>(key) * p.ldv + 4 * h;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          const u32x2 x = *reinterpret_cast<const u32x2*>(vr + 32 * dt + 8 * e4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t f = (e & 1) ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16;
+            const bool add = key <= pos && (f & 0x7F800000u) == 0x7F800000u;
+            o[dt][4 * e4 + e] += add ? __uint_as_float(f) : 0.f;
+          }
+        }
+    }
+  };
+  // tile tt has landed; every wave is done with tile tt - 1, whose place is filled next
+  auto next = [&](int tt, bool masked) __attribute__((always_inline)) {
+    wait_vmcnt_le((min(ntiles, tt + L::NS - 1) - tt - 1) * 2 * L::CPT);
+    if (masked) clear_odd(tt);
+    lds_barrier();
+    if (tt + L::NS - 1 < ntiles) issue(tt + L::NS - 1);
+  };
+  // tiles that every row of the workgroup sees whole, then those that end at some row
+  const int nfull = (t.r0 / p.G + 1) / L::KEYS;
+  int tt = 0;
+  for (; tt < nfull; ++tt) {
+    next(tt, false);
+    tile(std::false_type{}, tt);
+  }
+  for (; tt < ntiles; ++tt) {
+    next(tt, true);
+    if (tt * L::KEYS <= wave_hi) {  // uniform over the wave
+      tile(std::true_type{}, tt);
+      add_odd(tt);
     }
   }
   if (row >= M) return;
@@ -526,6 +611,7 @@ extern "C" int ptd_prompt_attention(const void* q, const void* k, const void* v,
                     !ptd_aligned(k, 16) || !ptd_aligned(v, 16) || !ptd_aligned(out, 16),
                 PTD_ERR_ALIGN);
   if (s.N == 0) return PTD_OK;
+  prm.wide = std::max(prm.ldk, prm.ldv) >= (1 << 24);
   prm.q = q;
   prm.k = k;
   prm.v = v;
@@ -554,10 +640,10 @@ extern "C" int ptd_prompt_attention(const void* q, const void* k, const void* v,
     if (s.D == 128) hipLaunchKernelGGL(k_prompt_f32<128>, grid, dim3(kF32Threads), 0, st, prm);
     else hipLaunchKernelGGL(k_prompt_f32<64>, grid, dim3(kF32Threads), 0, st, prm);
   } else {
-    prm.items = items_of(256);
+    prm.items = items_of(128);
     const dim3 grid = grid_of(prm.items);
-    if (s.D == 128) hipLaunchKernelGGL((k_prompt_bf16<128, 512>), grid, dim3(512), 0, st, prm);
-    else hipLaunchKernelGGL((k_prompt_bf16<64, 512>), grid, dim3(512), 0, st, prm);
+    if (s.D == 128) hipLaunchKernelGGL((k_prompt_bf16<128, 256>), grid, dim3(256), 0, st, prm);
+    else hipLaunchKernelGGL((k_prompt_bf16<64, 256>), grid, dim3(256), 0, st, prm);
   }
   return ptd_launch_status();
 }
