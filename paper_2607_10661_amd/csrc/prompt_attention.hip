@@ -23,7 +23,6 @@ using ptd::dma16_s2;
 using ptd::lds_addr;
 using ptd::lds_barrier;
 using ptd::wait_vmcnt;
-using ptd::wait_vmcnt_le;
 
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
@@ -56,10 +55,23 @@ struct TileOf {
   int start, n, r0, g;
 };
 
+// Sum and largest of a wave's values >= 0 (DPP: shifts within rows of 16 lanes, then
+// broadcasts of rows' last lanes; lanes without a source add 0).
+template <typename F>
+__device__ __forceinline__ int wave_reduce(int v, F f) {
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true));   // row_shr:1
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true));   // row_shr:2
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true));   // row_shr:4
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true));   // row_shr:8
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));  // row_bcast:15
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));  // row_bcast:31
+  return __builtin_amdgcn_readlane(v, 63);
+}
 __device__ __forceinline__ int wave_sum_i32(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, PTD_WAVE);
-  return __builtin_amdgcn_readfirstlane(v);
+  return wave_reduce(v, [](int a, int b) { return a + b; });
+}
+__device__ __forceinline__ int wave_max_i32(int v) {
+  return wave_reduce(v, [](int a, int b) { return max(a, b); });
 }
 
 // Tile number w of all sequences' tiles; false past the last one.  Up to 64 sequences:
@@ -92,10 +104,7 @@ __device__ __forceinline__ bool find_tile(const PromptParams& p, long long w, Ti
       // level k: the tiles k of the sequences that have one; above it lie
       // sum max(nt - k - 1, 0) tiles.  w belongs to the least k with no more than w above it.
       if (w >= wave_sum_i32(nt)) return false;
-      int most = nt;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, PTD_WAVE));
-      int lo = 0, hi = __builtin_amdgcn_readfirstlane(most) - 1;
+      int lo = 0, hi = wave_max_i32(nt) - 1;
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (wave_sum_i32(max(nt - mid - 1, 0)) <= w) hi = mid;
@@ -149,7 +158,13 @@ __device__ __forceinline__ bool my_tile(const PromptParams& p, TileOf& t) {
     t.g = static_cast<int>(id % H);
     w = id / H;
   }
-  return find_tile<TM>(p, w, t);
+  if (!find_tile<TM>(p, w, t)) return false;
+  // (uniform: said so, or every loop and branch by them is made of lane masks)
+  t.start = __builtin_amdgcn_readfirstlane(t.start);
+  t.n = __builtin_amdgcn_readfirstlane(t.n);
+  t.r0 = __builtin_amdgcn_readfirstlane(t.r0);
+  t.g = __builtin_amdgcn_readfirstlane(t.g);
+  return true;
 }
 
 __device__ __forceinline__ float max_xor32(float v) {
@@ -182,30 +197,32 @@ __device__ __forceinline__ u32x2 lds_read_tr16(const unsigned char* p) {
 // lies at c ^ swz(r): for K, so that 16 rows x one chunk (a quarter of a ds_read_b128)
 // fall on 16 different places of 256 bytes; for V, so that 4 rows x 4 chunks (half of a
 // transposing read) do.
-template <int D, int NT>
+constexpr int kThreads = 256;  // four waves of 32 rows
+template <int D>
 struct Tiles {
   static constexpr int KEYS = 64;
   static constexpr int RB = D * 2;             // bytes per row
   static constexpr int CH = RB / 16;           // chunks per row
   static constexpr int PART = KEYS * RB;       // K (or V) bytes
   static constexpr int SLOT = 2 * PART;
-  static constexpr int CPT = KEYS * CH / NT;   // copies per thread of K (and of V)
-  static constexpr int NS = NT == 512 ? 4 : 2; // tiles in the ring
-  static_assert(CPT * NT == KEYS * CH, "copies divide");
+  static constexpr int CPT = KEYS * CH / kThreads;  // copies per thread of K (and of V)
+  static constexpr int NS = 2;                    // tiles in the ring: one is read while the next lands
+  static_assert(CPT * kThreads == KEYS * CH, "copies divide");
   __device__ static int swz_k(int r) { return CH == 16 ? r & 15 : (r >> 1) & 7; }
   __device__ static int swz_v(int r) {
     return CH == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
   }
 };
 
-template <int D, int NT>
-__global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
-  using L = Tiles<D, NT>;
-  constexpr int NW = NT / PTD_WAVE;
+template <int D>
+__global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
+  using L = Tiles<D>;
+  constexpr int NS = L::NS;
+  constexpr int NW = kThreads / PTD_WAVE;
   constexpr int TM = 32 * NW;
   constexpr int DB = D / 16;  // QK^T steps
   constexpr int DT = D / 32;  // 32-column parts of O
-  __shared__ __attribute__((aligned(16))) unsigned char smem[L::NS * L::SLOT];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[NS * L::SLOT];
   __shared__ int s_odd[2][NW];  // by parity of the tile, for each wave
 
   TileOf t;
@@ -220,12 +237,6 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
   const int row = t.r0 + wave * 32 + l32;
   const int rc = min(row, M - 1);
   const int pos = rc / p.G, hq = t.g * p.G + rc % p.G;
-  const uint16_t* qr = static_cast<const uint16_t*>(p.q) + static_cast<size_t>(t.start + pos) * p.ldq +
-                       static_cast<size_t>(hq) * D + 8 * h;
-  bf16x8 qf[DB];
-#pragma unroll
-  for (int i = 0; i < DB; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qr + 16 * i));
-
   // ---- tile copies
   const uint16_t* kbase = static_cast<const uint16_t*>(p.k) + static_cast<size_t>(t.start) * p.ldk + static_cast<size_t>(t.g) * D;
   const uint16_t* vbase = static_cast<const uint16_t*>(p.v) + static_cast<size_t>(t.start) * p.ldv + static_cast<size_t>(t.g) * D;
@@ -233,45 +244,54 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
   uint32_t c_k[L::CPT], c_v[L::CPT];  // byte offsets of this thread's chunks in a tile
 #pragma unroll
   for (int u = 0; u < L::CPT; ++u) {
-    const int c = u * NT + tid, r = c / L::CH;
+    const int c = u * kThreads + tid, r = c / L::CH;
     c_k[u] = static_cast<uint32_t>((r * p.ldk + ((c % L::CH) ^ L::swz_k(r)) * 8) * 2);
     c_v[u] = static_cast<uint32_t>((r * p.ldv + ((c % L::CH) ^ L::swz_v(r)) * 8) * 2);
   }
   auto issue = [&](int tt) __attribute__((always_inline)) {
-    const uint32_t dst = ring + (tt % L::NS) * L::SLOT + wave * PTD_WAVE * 16;
+    const uint32_t dst = ring + (tt % NS) * L::SLOT + wave * PTD_WAVE * 16;
     if ((tt + 1) * L::KEYS <= t.n && !p.wide) {  // uniform: a whole tile, from scalar bases
       const uint16_t* kt = kbase + static_cast<size_t>(tt) * L::KEYS * p.ldk;
       const uint16_t* vt = vbase + static_cast<size_t>(tt) * L::KEYS * p.ldv;
 #pragma unroll
-      for (int u = 0; u < L::CPT; ++u) dma16_s2(kt, c_k[u], dst + u * NT * 16, vt, c_v[u], dst + L::PART + u * NT * 16);
+      for (int u = 0; u < L::CPT; ++u) dma16_s2(kt, c_k[u], dst + u * kThreads * 16, vt, c_v[u], dst + L::PART + u * kThreads * 16);
     } else {
 #pragma unroll
       for (int u = 0; u < L::CPT; ++u) {
-        const int c = u * NT + tid, r = c / L::CH;
+        const int c = u * kThreads + tid, r = c / L::CH;
         const size_t key = min(tt * L::KEYS + r, t.n - 1);  // past the sequence: its last row again
-        dma16(kbase + key * p.ldk + ((c % L::CH) ^ L::swz_k(r)) * 8, dst + u * NT * 16);
-        dma16(vbase + key * p.ldv + ((c % L::CH) ^ L::swz_v(r)) * 8, dst + L::PART + u * NT * 16);
+        dma16(kbase + key * p.ldk + ((c % L::CH) ^ L::swz_k(r)) * 8, dst + u * kThreads * 16);
+        dma16(vbase + key * p.ldv + ((c % L::CH) ^ L::swz_v(r)) * 8, dst + L::PART + u * kThreads * 16);
       }
     }
   };
   // keys up to the tile's last position
   const int last = (min(t.r0 + TM, M) - 1) / p.G;
   const int ntiles = last / L::KEYS + 1;
+  issue(0);
+  const uint16_t* qr = static_cast<const uint16_t*>(p.q) + static_cast<size_t>(t.start + pos) * p.ldq +
+                       static_cast<size_t>(hq) * D + 8 * h;
+  bf16x8 qf[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qr + 16 * i));
+  // waited for here: a load pending at the loop would make the compiler wait for every copy
+#pragma unroll
+  for (int i = 0; i < DB; ++i) asm volatile("" : "+v"(qf[i]));
   // last position of the wave's rows
   const int wave_hi = min(t.r0 + wave * 32 + 31, M - 1) / p.G;
 
-  int koff[DB], voff[DT];
+  int koff[DB], voff[2][DT];
 #pragma unroll
   for (int i = 0; i < DB; ++i) koff[i] = l32 * L::RB + ((2 * i + h) ^ L::swz_k(l32)) * 16;
   // source lane 4 j + q of a group of 16 points at V[key j][.. + 4 q]; the group's
   // lane i receives its four keys' values of column i
   const int l16 = lane & 15, vrow = 4 * h + (l16 >> 2), q4 = l16 & 3, dsub = (lane >> 4) & 1;
+  // (rows 16 apart are permuted alike)
 #pragma unroll
-  for (int i = 0; i < DT; ++i) voff[i] = L::PART + vrow * L::RB + (q4 & 1) * 8;
-  auto v_at = [&](int dt, int r8) __attribute__((always_inline)) {  // r8: multiple of 8
-    const int r = vrow + r8;
-    return voff[dt] + r8 * L::RB + ((4 * dt + 2 * dsub + (q4 >> 1)) ^ L::swz_v(r)) * 16;
-  };
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      voff[i][dt] = L::PART + (vrow + 8 * i) * L::RB + (q4 & 1) * 8 + ((4 * dt + 2 * dsub + (q4 >> 1)) ^ L::swz_v(vrow + 8 * i)) * 16;
 
   f32x16 o[DT];
 #pragma unroll
@@ -280,56 +300,44 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
   float m = kNegBig, nmc = -kNegBig * p.c, l = 0.f;
 
-  const int ninit = min(ntiles, L::NS - 1);
-  for (int tt = 0; tt < ninit; ++tt) issue(tt);
-  auto tile = [&](auto masked_tag, int tt) __attribute__((always_inline)) {
-    constexpr bool masked = decltype(masked_tag)::value;
-    const int k0 = tt * L::KEYS;
-    const unsigned char* slot = smem + (tt % L::NS) * L::SLOT;
-    f32x16 s[2];
+  // scores of 32 keys
+  auto qk = [&](const unsigned char* slot, int kb) __attribute__((always_inline)) {
+    f32x16 s;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(slot + kb * 32 * L::RB + koff[i]));
-        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[kb], 0, 0, 0);
-      }
+    for (int i = 0; i < DB; ++i) {
+      const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(slot + kb * 32 * L::RB + koff[i]));
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s, 0, 0, 0);
     }
-    if constexpr (masked) {
-      const int lim = pos - k0 - 4 * h;
+    return s;
+  };
+  // weights 2^((s - m) c) as bf16 pairs, and the sum of what they were rounded to
+  struct Weights {
+    uint32_t w[8];
+    float sum;
+  };
+  auto exps = [&](const f32x16& s) __attribute__((always_inline)) {
+    Weights r;
+    float a = 0.f, b = 0.f;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          s[kb][e] = 32 * kb + 8 * (e / 4) + e % 4 <= lim ? s[kb][e] : -INFINITY;
+    for (int w = 0; w < 8; ++w) {
+      r.w[w] = ptd::cvt_pk_bf16(__builtin_amdgcn_exp2f(fmaf(s[2 * w], p.c, nmc)),
+                                __builtin_amdgcn_exp2f(fmaf(s[2 * w + 1], p.c, nmc)));
+      if (w & 1) b = sum_bf16x2(r.w[w], b);
+      else a = sum_bf16x2(r.w[w], a);
     }
-    // weights 2^((s - m) c) as bf16 pairs, and the sum of what they were rounded to
-    uint32_t pw[2][8];
-    float ps;
-    auto exps = [&]() __attribute__((always_inline)) {
-      ps = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-          pw[kb][w] = ptd::cvt_pk_bf16(__builtin_amdgcn_exp2f(fmaf(s[kb][2 * w], p.c, nmc)),
-                                       __builtin_amdgcn_exp2f(fmaf(s[kb][2 * w + 1], p.c, nmc)));
-          ps = sum_bf16x2(pw[kb][w], ps);
-        }
-    };
-    exps();
-    // A row's reference m stays while its weights are far inside the fp32 range; else it
-    // moves to the row's maximum (always at its first keys), whatever the other rows do.
-    const uint64_t over = __ballot(!(ps <= 65536.f));
+    r.sum = a + b;
+    return r;
+  };
+  // A row's reference m stays while its weights are far inside the fp32 range; else it
+  // moves to the row's maximum (always at its first keys), whatever the other rows do.
+  auto settle = [&](const f32x16& s, Weights& r, uint64_t over) __attribute__((always_inline)) {
     if (over) {
       const bool mine = ((static_cast<uint32_t>(over) | static_cast<uint32_t>(over >> 32)) >> l32) & 1u;
-      float mx = s[0][0];
+      float mx = s[0];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[kb][e]);
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
       mx = max_xor32(mx);
       const bool up = mine && mx > m;
       const float alpha = up ? __builtin_amdgcn_exp2f((m - mx) * p.c) : 1.f;
@@ -338,34 +346,64 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
       l *= alpha;
 #pragma unroll
       for (int i = 0; i < DT; ++i) o[i] *= alpha;
-      exps();
+      r = exps(s);
     }
-    l += ps;
+    l += r.sum;
+  };
+  auto over_of = [](const Weights& r) __attribute__((always_inline)) { return __ballot(!(r.sum <= 65536.f)); };
+  auto pv = [&](const unsigned char* slot, int kb, const Weights& r) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int st = 0; st < 2; ++st) {
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{r.w[4 * st], r.w[4 * st + 1], r.w[4 * st + 2], r.w[4 * st + 3]});
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pw[kb][4 * st], pw[kb][4 * st + 1], pw[kb][4 * st + 2], pw[kb][4 * st + 3]});
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const u32x2 a = lds_read_tr16(slot + v_at(dt, 32 * kb + 16 * st));
-          const u32x2 b = lds_read_tr16(slot + v_at(dt, 32 * kb + 16 * st + 8));
-          const u32x4 vw = {a[0], a[1], b[0], b[1]};
-          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vw), pf, o[dt], 0, 0, 0);
-        }
+      for (int dt = 0; dt < DT; ++dt) {
+        const u32x2 a = lds_read_tr16(slot + voff[0][dt] + (32 * kb + 16 * st) * L::RB);
+        const u32x2 b = lds_read_tr16(slot + voff[1][dt] + (32 * kb + 16 * st) * L::RB);
+        const u32x4 vw = {a[0], a[1], b[0], b[1]};
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vw), pf, o[dt], 0, 0, 0);
       }
+    }
+  };
+  // A tile that every row sees whole.  The second half's QK^T runs beside the first half's
+  // exponentials, the first half's PV beside the second's.
+  auto full_tile = [&](const unsigned char* slot, bool first) __attribute__((always_inline)) {
+    const f32x16 s0 = qk(slot, 0);
+    const f32x16 s1 = qk(slot, 1);
+    Weights w0;
+    uint64_t over = ~0ull;
+    if (!first) {
+      w0 = exps(s0);
+      over = over_of(w0);
+    }
+    settle(s0, w0, over);
+    Weights w1 = exps(s1);
+    pv(slot, 0, w0);
+    settle(s1, w1, over_of(w1));
+    pv(slot, 1, w1);
+  };
+  // a tile at some row's end: scores of keys behind a row's position become -inf
+  auto end_tile = [&](const unsigned char* slot, int k0, bool first) __attribute__((always_inline)) {
+    const int lim = pos - k0 - 4 * h;
+    for (int kb = 0; kb < 2 && k0 + 32 * kb <= wave_hi; ++kb) {  // uniform
+      f32x16 s = qk(slot + kb * 32 * L::RB, 0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 32 * kb + 8 * (e / 4) + e % 4 <= lim ? s[e] : -INFINITY;
+      Weights w = exps(s);
+      settle(s, w, first && kb == 0 ? ~0ull : over_of(w));
+      pv(slot + kb * 32 * L::RB, 0, w);
+    }
   };
   // A tile that not every row sees whole: 0 * inf must not reach a row that does not
   // see the key.  Each thread clears what is not finite from the value chunks that it
   // copied, before the barrier that shows them to the others; the rows that do see such
   // a value get it after the tile, from memory (rare).
   auto clear_odd = [&](int tt) __attribute__((always_inline)) {
-    unsigned char* mine = smem + (tt % L::NS) * L::SLOT + L::PART + tid * 16;
+    unsigned char* own = smem + (tt % NS) * L::SLOT + L::PART + tid * 16;
     uint32_t top = 0;
     u32x4 w[L::CPT];
 #pragma unroll
     for (int u = 0; u < L::CPT; ++u) {
-      w[u] = *reinterpret_cast<const u32x4*>(mine + u * NT * 16);
+      w[u] = *reinterpret_cast<const u32x4*>(own + u * kThreads * 16);
 #pragma unroll
       for (int x = 0; x < 4; ++x) top |= (w[u][x] & 0x7F807F80u) + 0x00800080u;  // bits 15, 31: exponent all ones
     }
@@ -376,7 +414,7 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           w[u][x] &= ((w[u][x] & 0x7F80u) == 0x7F80u ? 0u : 0xFFFFu) | ((w[u][x] & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u);
-        *reinterpret_cast<u32x4*>(mine + u * NT * 16) = w[u];
+        *reinterpret_cast<u32x4*>(own + u * kThreads * 16) = w[u];
       }
     }
     if (lane == 0) s_odd[tt & 1][wave] = odd;
@@ -404,23 +442,36 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
     }
   };
   // tile tt has landed; every wave is done with tile tt - 1, whose place is filled next
-  auto next = [&](int tt, bool masked) __attribute__((always_inline)) {
-    wait_vmcnt_le((min(ntiles, tt + L::NS - 1) - tt - 1) * 2 * L::CPT);
-    if (masked) clear_odd(tt);
+  auto next = [&](int tt, bool ends) __attribute__((always_inline)) {
+    wait_vmcnt<0>();
+    if (ends) clear_odd(tt);
     lds_barrier();
-    if (tt + L::NS - 1 < ntiles) issue(tt + L::NS - 1);
+    if (tt + 1 < ntiles) issue(tt + 1);
   };
   // tiles that every row of the workgroup sees whole, then those that end at some row
-  const int nfull = (t.r0 / p.G + 1) / L::KEYS;
+  const int full = (t.r0 / p.G + 1) / L::KEYS;
   int tt = 0;
-  for (; tt < nfull; ++tt) {
+  if (full > 0) {
+    next(0, false);
+    full_tile(smem, true);
+    tt = 1;
+  }
+  // two tiles a turn: their places in LDS are constants of the instructions
+  for (; tt + 1 < full; tt += 2) {
     next(tt, false);
-    tile(std::false_type{}, tt);
+    full_tile(smem + L::SLOT, false);
+    next(tt + 1, false);
+    full_tile(smem, false);
+  }
+  if (tt < full) {
+    next(tt, false);
+    full_tile(smem + L::SLOT, false);
+    ++tt;
   }
   for (; tt < ntiles; ++tt) {
     next(tt, true);
     if (tt * L::KEYS <= wave_hi) {  // uniform over the wave
-      tile(std::true_type{}, tt);
+      end_tile(smem + (tt % NS) * L::SLOT, tt * L::KEYS, tt == 0);
       add_odd(tt);
     }
   }
@@ -443,21 +494,33 @@ __global__ void __launch_bounds__(NT, 2) k_prompt_bf16(PromptParams p) {
 }
 
 // ===========================================================================
-// fp32: v_mfma_f32_32x32x2_f32, the same scheme with tiles of 32 keys
+// fp32: v_mfma_f32_32x32x2_f32
 // ===========================================================================
-// A step of QK^T contracts the columns 8 j + 4 h + e (h: half of the wave) of one
-// 16-byte load; a step of PV the keys 8 * (i / 4) + 4 h + i % 4 whose weights
-// the lane owns in element i.  Bound by the matrix cores: 64 cycles per MFMA.
-constexpr int kF32Threads = 256;
+// An MFMA takes 64 cycles for 4096 products, so operands need not be shared: the eight
+// waves of a workgroup hold the same 32 rows and take every eighth tile of 32 keys, each
+// straight from memory into registers, with a maximum and sum of its own; the
+// states merge through LDS at the end.  No barrier in between, and a row of n keys
+// waits for n / 256 tiles, not n / 32.  K is loaded when it is needed and V behind the
+// scores, into the same registers; the SIMD's other wave covers the waits (V and
+// the next K loaded ahead: 17.1 against 15.5 us on 512 rows of 4 heads x 64, and for D =
+// 128 the registers spill, 35.7 against 25.5).  Four waves over one ring in LDS, a
+// wave per 32 rows and all its keys, took 48.8 us there.
+//   S^T = K Q^T: step (j, e) contracts the columns 8 j + 4 h + e of 16-byte loads.
+//   O^T = V^T P^T: step e contracts the keys 8 * (e / 4) + 4 h + e % 4, whose weights the
+//   lane owns; row r of part dt stands for column DT * r + dt, so that a lane's loads are
+//   DT consecutive elements, and so are its outputs.
+constexpr int kF32Threads = 512;
+constexpr int kF32Waves = kF32Threads / PTD_WAVE;
 
 template <int D>
 __global__ void __launch_bounds__(kF32Threads, 2) k_prompt_f32(PromptParams p) {
-  constexpr int NT = kF32Threads, TM = 32 * (NT / PTD_WAVE);
-  constexpr int KEYS = 32, RB = D * 4, CH = RB / 16, PART = KEYS * RB, SLOT = 2 * PART, NS = 2;
-  constexpr int CPT = KEYS * CH / NT, KJ = D / 8, DT = D / 32;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[NS * SLOT];
-  auto swz_k = [](int r) __attribute__((always_inline)) { return r & 15; };
-  auto swz_v = [](int r) __attribute__((always_inline)) { return ((r >> 2) & 1) << 3; };
+  constexpr int TM = 32, KEYS = 32, CH = D / 4, KJ = D / 8, DT = D / 32;
+  using fvec = float __attribute__((ext_vector_type(DT)));
+  // rows in 16-byte chunks, chunk c of row r at c ^ (r mod 16)
+  __shared__ __attribute__((aligned(16))) float sq[TM * D];
+  __shared__ __attribute__((aligned(16))) float so[kF32Waves][TM * D];
+  __shared__ float2 sml[kF32Waves][TM];
+  auto chunk = [](int r, int c) __attribute__((always_inline)) { return (r * CH + (c ^ (r & 15))) * 4; };
 
   TileOf t;
   if (!my_tile<TM>(p, t)) return;
@@ -466,58 +529,86 @@ __global__ void __launch_bounds__(kF32Threads, 2) k_prompt_f32(PromptParams p) {
   const int lane = tid & 63;
   const int l32 = lane & 31, h = lane >> 5;
   const int M = t.n * p.G;
-  const int row = t.r0 + wave * 32 + l32;
-  const int rc = min(row, M - 1);
-  const int pos = rc / p.G, hq = t.g * p.G + rc % p.G;
-  const float* qr = static_cast<const float*>(p.q) + static_cast<size_t>(t.start + pos) * p.ldq +
-                    static_cast<size_t>(hq) * D + 4 * h;
-  f32x4 qf[KJ];
-#pragma unroll
-  for (int j = 0; j < KJ; ++j) qf[j] = *reinterpret_cast<const f32x4*>(qr + 8 * j);
+  const int pos = min(t.r0 + l32, M - 1) / p.G;  // this lane's query row
+  const int lo = t.r0 / p.G, hi = (min(t.r0 + TM, M) - 1) / p.G;
+  const int ntiles = hi / KEYS + 1;
   const float* kbase = static_cast<const float*>(p.k) + static_cast<size_t>(t.start) * p.ldk + static_cast<size_t>(t.g) * D;
   const float* vbase = static_cast<const float*>(p.v) + static_cast<size_t>(t.start) * p.ldv + static_cast<size_t>(t.g) * D;
-  const uint32_t ring = lds_addr(smem);
-  auto issue = [&](int tt) __attribute__((always_inline)) {
-    const uint32_t dst = ring + (tt % NS) * SLOT + wave * PTD_WAVE * 16;
+
+  f32x4 kf[KJ];
+  // whole tiles from scalar bases and 32-bit offsets: addresses in 64 bits would not
+  // leave the registers for the tiles in flight
+  const uint32_t koff = static_cast<uint32_t>(l32 * p.ldk + 4 * h) * 4u;
+  const uint32_t voff = static_cast<uint32_t>(4 * h * p.ldv + DT * l32) * 4u;
+  auto whole = [&](int tt) __attribute__((always_inline)) { return (tt + 1) * KEYS <= t.n && !p.wide; };
+  auto load_k = [&](int tt) __attribute__((always_inline)) {
+    if (whole(tt)) {
+      const char* src = reinterpret_cast<const char*>(kbase + static_cast<size_t>(tt) * KEYS * p.ldk);
 #pragma unroll
-    for (int u = 0; u < CPT; ++u) {
-      const int c = u * NT + tid, r = c / CH;
-      const size_t key = min(tt * KEYS + r, t.n - 1);
-      dma16(kbase + key * p.ldk + ((c % CH) ^ swz_k(r)) * 4, dst + u * NT * 16);
-      dma16(vbase + key * p.ldv + ((c % CH) ^ swz_v(r)) * 4, dst + PART + u * NT * 16);
+      for (int j = 0; j < KJ; ++j) kf[j] = *reinterpret_cast<const f32x4*>(src + koff + 32 * j);
+    } else {
+      const float* src = kbase + static_cast<size_t>(min(tt * KEYS + l32, t.n - 1)) * p.ldk + 4 * h;
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) kf[j] = *reinterpret_cast<const f32x4*>(src + 8 * j);
     }
   };
-  const int ntiles = (min(t.r0 + TM, M) - 1) / p.G / KEYS + 1;
-  const int wave_lo = min(t.r0 + wave * 32, M - 1) / p.G;
-  const int wave_hi = min(t.r0 + wave * 32 + 31, M - 1) / p.G;
+  for (int x = tid; x < TM * CH; x += kF32Threads) {
+    const int r = x / CH, c = x % CH, rr = min(t.r0 + r, M - 1);
+    const float* src = static_cast<const float*>(p.q) + static_cast<size_t>(t.start + rr / p.G) * p.ldq +
+                       static_cast<size_t>(t.g * p.G + rr % p.G) * D;
+    *reinterpret_cast<f32x4*>(sq + chunk(r, c)) = *reinterpret_cast<const f32x4*>(src + 4 * c);
+  }
+  __syncthreads();
+
   f32x16 o[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-  float m = kNegBig, l = 0.f;
-  issue(0);
-  for (int tt = 0; tt < ntiles; ++tt) {
-    wait_vmcnt<0>();
-    lds_barrier();
-    if (tt + 1 < ntiles) issue(tt + 1);
+  float m = kNegBig, l = 0.f;  // l: this lane's keys only
+  for (int tt = wave; tt < ntiles; tt += kF32Waves) {
     const int k0 = tt * KEYS;
-    if (k0 > wave_hi) continue;
-    const unsigned char* slot = smem + (tt % NS) * SLOT;
+    fvec vf[16];
+    auto load_v = [&]() __attribute__((always_inline)) {
+      if (whole(tt)) {
+        const char* src = reinterpret_cast<const char*>(vbase + static_cast<size_t>(k0) * p.ldv);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          vf[e] = *reinterpret_cast<const fvec*>(src + static_cast<size_t>(8 * (e / 4) + e % 4) * p.ldv * 4 + voff);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = min(k0 + 8 * (e / 4) + 4 * h + e % 4, t.n - 1);
+          vf[e] = *reinterpret_cast<const fvec*>(vbase + static_cast<size_t>(key) * p.ldv + DT * l32);
+        }
+      }
+    };
+    load_k(tt);
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
     for (int j = 0; j < KJ; ++j) {
-      const f32x4 kf = *reinterpret_cast<const f32x4*>(slot + l32 * RB + ((2 * j + h) ^ swz_k(l32)) * 16);
+      const f32x4 qv = *reinterpret_cast<const f32x4*>(sq + chunk(l32, 2 * j + h));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[j][e], s, 0, 0, 0);
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[j][e], qv[e], s, 0, 0, 0);
     }
-    const bool masked = k0 + KEYS - 1 > wave_lo;
-    if (masked) {
+    load_v();
+    const bool ends = k0 + KEYS - 1 > lo;  // uniform: some row does not see all of the tile
+    bool odd = false;
+    if (ends) {
       const int lim = pos - k0 - 4 * h;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = 8 * (e / 4) + e % 4 <= lim ? s[e] : -INFINITY;
+      // 0 * inf must not reach a row that does not see the key
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const bool bad = (__float_as_uint(vf[e][dt]) & 0x7F800000u) == 0x7F800000u;
+          odd |= bad;
+          vf[e][dt] = bad ? 0.f : vf[e][dt];
+        }
     }
     float mx = s[0];
 #pragma unroll
@@ -533,55 +624,68 @@ __global__ void __launch_bounds__(kF32Threads, 2) k_prompt_f32(PromptParams p) {
       ps += s[e];
     }
     l = fmaf(l, alpha, ps);
-    if (__any(alpha != 1.f)) {
 #pragma unroll
-      for (int i = 0; i < DT; ++i) o[i] *= alpha;
-    }
-    bool odd = false;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int r = 8 * (e / 4) + 4 * h + e % 4;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        float v = *reinterpret_cast<const float*>(slot + PART + r * RB + ((8 * dt + (l32 >> 2)) ^ swz_v(r)) * 16 + (l32 & 3) * 4);
-        if (masked) {
-          const bool bad = (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u;
-          odd |= bad;
-          v = bad ? 0.f : v;
-        }
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[e], o[dt], 0, 0, 0);
-      }
-    }
-    if (masked && __any(odd)) {
-      for (int key = 0; key < KEYS; ++key) {
-        const bool sees = k0 + key <= pos;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int d = 32 * dt + 8 * (e / 4) + 4 * h + e % 4;
-            const float f = *reinterpret_cast<const float*>(slot + PART + key * RB + ((d >> 2) ^ swz_v(key)) * 16 + (d & 3) * 4);
-            if (sees && (__float_as_uint(f) & 0x7F800000u) == 0x7F800000u) o[dt][e] += f;
-          }
-      }
-    }
-  }
-  if (row >= M) return;
-  const float inv = 1.f / sum_xor32(l);
-  const size_t off = (static_cast<size_t>(t.start + pos) * p.Hq + hq) * D + 4 * h;
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
+    for (int i = 0; i < DT; ++i) o[i] *= alpha;
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
-      const f32x4 v = {o[dt][4 * e4] * inv, o[dt][4 * e4 + 1] * inv, o[dt][4 * e4 + 2] * inv, o[dt][4 * e4 + 3] * inv};
-      const size_t at = off + 32 * dt + 8 * e4;
-      if (p.out_bf16) {
-        const u32x2 w = {ptd::cvt_pk_bf16(v[0], v[1]), ptd::cvt_pk_bf16(v[2], v[3])};
-        *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = w;
-      } else {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = v;
-      }
+      if (k0 + 8 * e4 > hi) break;  // uniform: keys that no row sees
+#pragma unroll
+      for (int e = 4 * e4; e < 4 * e4 + 4; ++e)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[e][dt], s[e], o[dt], 0, 0, 0);
     }
+    if (ends && __any(odd)) {  // rare: what is not finite, to the rows that see it
+      const int end = min(k0 + KEYS, t.n);
+      for (int key = k0; key < end; ++key)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const fvec f = *reinterpret_cast<const fvec*>(vbase + static_cast<size_t>(key) * p.ldv + DT * (8 * (e / 4) + 4 * h + e % 4));
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const bool add = key <= pos && (__float_as_uint(f[dt]) & 0x7F800000u) == 0x7F800000u;
+            o[dt][e] += add ? f[dt] : 0.f;
+          }
+        }
+    }
+  }
+
+  // ---- merge of the waves
+  l = sum_xor32(l);
+  if (h == 0) sml[wave][l32] = make_float2(m, l);
+  if (wave < ntiles) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4 / DT) {  // four consecutive columns from 4 / DT elements
+      const int r = 8 * (e / 4) + 4 * h + e % 4;
+      f32x4 x;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) x[y] = o[y % DT][e + y / DT];
+      *reinterpret_cast<f32x4*>(&so[wave][chunk(l32, r * DT / 4)]) = x;
+    }
+  }
+  __syncthreads();
+  const int nw = min(ntiles, kF32Waves);
+  for (int x = tid; x < TM * CH; x += kF32Threads) {
+    const int r = x / CH, c = x % CH, rr = t.r0 + r;
+    if (rr >= M) break;
+    float mm = kNegBig;
+    for (int w = 0; w < nw; ++w) mm = fmaxf(mm, sml[w][r].x);
+    float den = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < nw; ++w) {
+      const float2 ml = sml[w][r];
+      const float f = __builtin_amdgcn_exp2f((ml.x - mm) * p.c);
+      den = fmaf(f, ml.y, den);
+      acc += *reinterpret_cast<const f32x4*>(&so[w][chunk(r, c)]) * f;
+    }
+    const f32x4 v = acc * (1.f / den);
+    const size_t at = (static_cast<size_t>(t.start + rr / p.G) * p.Hq + t.g * p.G + rr % p.G) * D + 4 * c;
+    if (p.out_bf16) {
+      const u32x2 w = {ptd::cvt_pk_bf16(v[0], v[1]), ptd::cvt_pk_bf16(v[2], v[3])};
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = w;
+    } else {
+      *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = v;
+    }
+  }
 }
 
 }  // namespace
@@ -635,15 +739,15 @@ extern "C" int ptd_prompt_attention(const void* q, const void* k, const void* v,
   };
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (s.in_dtype == PTD_F32) {
-    prm.items = items_of(128);
+    prm.items = items_of(32);
     const dim3 grid = grid_of(prm.items);
     if (s.D == 128) hipLaunchKernelGGL(k_prompt_f32<128>, grid, dim3(kF32Threads), 0, st, prm);
     else hipLaunchKernelGGL(k_prompt_f32<64>, grid, dim3(kF32Threads), 0, st, prm);
   } else {
     prm.items = items_of(128);
     const dim3 grid = grid_of(prm.items);
-    if (s.D == 128) hipLaunchKernelGGL((k_prompt_bf16<128, 256>), grid, dim3(256), 0, st, prm);
-    else hipLaunchKernelGGL((k_prompt_bf16<64, 256>), grid, dim3(256), 0, st, prm);
+    if (s.D == 128) hipLaunchKernelGGL(k_prompt_bf16<128>, grid, dim3(kThreads), 0, st, prm);
+    else hipLaunchKernelGGL(k_prompt_bf16<64>, grid, dim3(kThreads), 0, st, prm);
   }
   return ptd_launch_status();
 }

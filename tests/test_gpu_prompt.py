@@ -221,3 +221,25 @@ def test_graph_and_streams(P):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, P.prompt_attention(q, k, v, s))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (2, 1), (6, 2), (16, 16), (7, 7), (24, 1)])
+def test_many_sequences_of_all_lengths(P, dtype, Hq, Hkv):
+    # tiles of several sequences, longest first, whatever the heads' share of the XCDs
+    r = np.random.default_rng(Hq)
+    check(P, [int(x) for x in r.integers(0, 400, 9)], Hq, Hkv, 64, dtype, seed=Hq)
+    check(P, [int(x) for x in r.integers(0, 90, 65)], Hq, Hkv, 64, dtype, seed=Hq + 1)
+
+
+def test_rows_far_apart(P):
+    # 64 rows span more than 2 GiB: offsets beyond 32 bits
+    D, n, ld = 64, 70, 1 << 24
+    buf = torch.zeros(n * ld, dtype=torch.bfloat16, device="cuda")
+    wide = buf.view(n, ld)[:, :D].unflatten(1, (1, D))
+    q, k, v = inputs([n], 1, 1, D, torch.bfloat16)
+    want = P.prompt_attention(q, k, v, i32([0, n]))
+    wide.copy_(v)
+    assert torch.equal(P.prompt_attention(q, k, wide, i32([0, n])), want)
+    wide.copy_(k)
+    assert torch.equal(P.prompt_attention(q, wide, v, i32([0, n])), want)
