@@ -52,30 +52,25 @@ __device__ inline Want want_of(const PlanParams& p, int b, int32_t* report_to) {
   return w;
 }
 
-__device__ __forceinline__ long long wave_scan(long long v) {  // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < PTD_WAVE; o <<= 1) {
-    const long long u = __shfl_up(v, o, PTD_WAVE);
-    v += lane >= o ? u : 0;
-  }
-  return v;
-}
-
-// Exclusive sum over the workgroup; total to every thread.
-__device__ __forceinline__ long long block_scan(long long v, long long* lds, long long* total) {
+// Exclusive sums of three values over the workgroup; totals to every thread.
+struct Sums {
+  long long back, grow, rows;
+};
+__device__ __forceinline__ Sums block_scan(const Sums& v, Sums* lds, Sums* total) {
   const int wave = threadIdx.x >> 6;
-  const long long in = wave_scan(v);
+  const Sums in = {ptd::wave_scan_i64(v.back), ptd::wave_scan_i64(v.grow), ptd::wave_scan_i64(v.rows)};
   __syncthreads();  // lds of the call before is read
   if ((threadIdx.x & 63) == 63) lds[wave] = in;
   __syncthreads();
-  long long base = 0, all = 0;
+  Sums base = {0, 0, 0}, all = {0, 0, 0};
+#pragma unroll
   for (int w = 0; w < kPlanWaves; ++w) {
-    base += w < wave ? lds[w] : 0;
-    all += lds[w];
+    const Sums x = lds[w];
+    if (w < wave) base.back += x.back, base.grow += x.grow, base.rows += x.rows;
+    all.back += x.back, all.grow += x.grow, all.rows += x.rows;
   }
   *total = all;
-  return base + in - v;
+  return {base.back + in.back - v.back, base.grow + in.grow - v.grow, base.rows + in.rows - v.rows};
 }
 
 // Last index x of [0, n) with a[x] <= v (a ascending, a[0] <= v).
@@ -90,26 +85,23 @@ __device__ __forceinline__ int upper(const A& a, int n, long long v) {
   return lo;
 }
 
-// Slot and position of row i: row r of sequence b (r < rows: a live one).
-__device__ __forceinline__ void put_row(const PlanParams& p, int i, int b, int r, int rows, int kv, int held) {
-  int slot = -1, pos = -1;
-  if (r < rows) {
-    pos = kv + r;
-    const int pg = pos >> p.page_shift;
-    if (pg < held) {
-      const int id = p.s.page_table[static_cast<size_t>(b) * p.s.max_pages + pg];
-      if (static_cast<uint32_t>(id) < static_cast<uint32_t>(p.s.num_pages))
-        slot = (id << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
-      else
-        ptd::report(p.dev_status, PTD_ERR_PAGE);
-    }
-  }
+// Slot and position of row i, row r of sequence b.
+__device__ __forceinline__ void put_row(const PlanParams& p, int i, int slot, int pos) {
   p.slots[i] = slot;
   if (p.positions) p.positions[i] = pos;
 }
+__device__ __forceinline__ int slot_at(const PlanParams& p, int id, int pos) {
+  if (static_cast<uint32_t>(id) < static_cast<uint32_t>(p.s.num_pages))
+    return (id << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+  ptd::report(p.dev_status, PTD_ERR_PAGE);
+  return -1;
+}
+__device__ __forceinline__ const int32_t* table_of(const PlanParams& p, int b) {
+  return p.s.page_table + static_cast<size_t>(b) * p.s.max_pages;
+}
 
-// Both kernels' row loop: rows [i0, i1) by `step`.  Sequences of packed rows come
-// from row_start (in LDS where they fit, else in memory).
+// Rows [i0, i1) by `step` when the tables are written.  starts: of packed rows, in LDS
+// where they fit, else in memory.
 template <typename Starts>
 __device__ __forceinline__ void put_rows(const PlanParams& p, const Starts& starts, int i0, int i1, int step) {
   for (int i = i0; i < i1; i += step) {
@@ -122,34 +114,49 @@ __device__ __forceinline__ void put_rows(const PlanParams& p, const Starts& star
       r = i - starts[b];
     }
     const Want w = want_of(p, b, nullptr);
-    put_row(p, i, b, r, w.rows, w.kv, w.held);
+    const bool row = r < w.rows;
+    const int pos = w.kv + r;
+    const bool page = row && (pos >> p.page_shift) < w.held;
+    put_row(p, i, page ? slot_at(p, table_of(p, b)[pos >> p.page_shift], pos) : -1, row ? pos : -1);
   }
 }
 
 // One workgroup: a thread per sequence (in rounds of 512) counts pages, sums over
 // the workgroup give every sequence its places on the free list and in the rows,
-// then a thread per page moves ids.  Bound by latency: about seven dependent
-// accesses to memory, whatever the lengths (16 sequences that take and trim 17
-// pages each).  Outputs depend on nothing but the inputs: no atomics.
+// then a thread per page moves ids.  Outputs depend on nothing but the inputs: no
+// atomics.  Bound by latency: with ONE round of sequences, the lengths are loaded
+// once, new rows take their page ids from where the tables get them, and a step of 16
+// sequences waits three times for memory: lengths, ids, stores.
+template <bool ONE>
 __global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanParams p) {
-  __shared__ long long s_scan[kPlanWaves];
-  __shared__ int s_off[kPlanThreads], s_need[kPlanThreads], s_held[kPlanThreads], s_start[kPlanThreads + 1];
+  __shared__ Sums s_scan[kPlanWaves];
+  __shared__ int s_back[kPlanThreads], s_need[kPlanThreads], s_off[kPlanThreads], s_grow[kPlanThreads];
+  __shared__ int s_held[kPlanThreads], s_start[kPlanThreads], s_kv[kPlanThreads], s_rows[kPlanThreads];
   const int tid = threadIdx.x;
   const int B = p.s.B;
+  const Want none = {0, 0, 0, 0};
+  Want w = none;
+  if (ONE && tid < B) w = want_of(p, tid, p.dev_status);
   int count = p.s.num_free[0];
   if (count < 0 || count > p.s.num_pages) {  // uniform
     if (tid == 0) ptd::report(p.dev_status, PTD_ERR_PAGE);
     count = min(max(count, 0), p.s.num_pages);
   }
+  auto sums_of = [](const Want& x) __attribute__((always_inline)) {
+    return Sums{max(x.held - x.need, 0), max(x.need - x.held, 0), x.rows};
+  };
   // ---- pages that go back: their number first, as the first sequence's lie deepest
-  long long total = 0;
-  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
-    Want w = {0, 0, 0, 0};
-    if (b0 + tid < B) w = want_of(p, b0 + tid, nullptr);
-    long long t;
-    block_scan(max(w.held - w.need, 0), s_scan, &t);
-    total += t;
+  Sums at = {0, 0, 0}, all = {0, 0, 0};
+  if (ONE) {
+    at = block_scan(sums_of(w), s_scan, &all);
+  } else {
+    for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+      Sums t;
+      block_scan(sums_of(b0 + tid < B ? want_of(p, b0 + tid, nullptr) : none), s_scan, &t);
+      all.back += t.back;
+    }
   }
+  long long total = all.back;
   if (total > p.s.num_pages - count) {  // pages held twice: the list cannot take them
     if (tid == 0) ptd::report(p.dev_status, PTD_ERR_PAGE);
     total = p.s.num_pages - count;
@@ -157,77 +164,80 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanParams p) {
   const int count1 = count + static_cast<int>(total);
   long long done = 0;
   for (int b0 = 0; b0 < B && total > 0; b0 += kPlanThreads) {  // uniform
-    Want w = {0, 0, 0, 0};
-    if (b0 + tid < B) w = want_of(p, b0 + tid, nullptr);
-    long long t;
-    const long long off = block_scan(max(w.held - w.need, 0), s_scan, &t);
-    s_off[tid] = static_cast<int>(off);
+    Sums t = all;
+    if (!ONE) {
+      w = b0 + tid < B ? want_of(p, b0 + tid, nullptr) : none;
+      at = block_scan(sums_of(w), s_scan, &t);
+    }
+    s_back[tid] = static_cast<int>(at.back);
     s_need[tid] = w.need;
     __syncthreads();
     const int n = min(B - b0, kPlanThreads);
-    for (int j = tid; j < t; j += kPlanThreads) {
-      const int x = upper(s_off, n, j);
-      const long long at = count1 - 1 - (done + j);
-      if (at >= count)
-        p.s.free_pages[at] = p.s.page_table[static_cast<size_t>(b0 + x) * p.s.max_pages + s_need[x] + (j - s_off[x])];
+#pragma unroll 4
+    for (int j = tid; j < t.back; j += kPlanThreads) {
+      const int x = upper(s_back, n, j);
+      const long long to = count1 - 1 - (done + j);
+      if (to >= count) p.s.free_pages[to] = table_of(p, b0 + x)[s_need[x] + (j - s_back[x])];
     }
-    done += t;
+    done += t.back;
     __syncthreads();
   }
   // ---- pages that are taken, in order while the list lasts; starts of the rows
   long long taken = 0, rows = 0;
   bool short_of = false;
   for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
-    Want w = {0, 0, 0, 0};
     const bool live = b0 + tid < B;
-    if (live) w = want_of(p, b0 + tid, p.dev_status);
+    Sums t = all;
+    if (!ONE) {
+      w = live ? want_of(p, b0 + tid, p.dev_status) : none;
+      at = block_scan(sums_of(w), s_scan, &t);
+    }
     if (p.rows_per_seq > 0 && w.rows > p.rows_per_seq) ptd::report(p.dev_status, PTD_ERR_ROWS);
     const int grow = max(w.need - w.held, 0);
-    long long t, tr;
-    const long long off = block_scan(grow, s_scan, &t);
-    const long long at = rows + block_scan(w.rows, s_scan, &tr);
-    const bool ok = grow == 0 || taken + off + grow <= count1;
+    const bool ok = grow == 0 || taken + at.grow + grow <= count1;
     if (!ok) ptd::report(p.dev_status, PTD_ERR_NO_PAGES);
     const int now = ok ? w.need : w.held;
-    s_off[tid] = static_cast<int>(min(off, static_cast<long long>(p.s.num_pages)));
-    s_need[tid] = ok ? grow : 0;
+    s_off[tid] = static_cast<int>(min(at.grow, static_cast<long long>(p.s.num_pages)));
+    s_grow[tid] = ok ? grow : 0;
     s_held[tid] = w.held;
     if (p.rows_per_seq == 0) {
-      const int start = static_cast<int>(min(at, static_cast<long long>(0x7FFFFFFF)));
+      const int start = static_cast<int>(min(rows + at.rows, static_cast<long long>(0x7FFFFFFF)));
       if (live) p.row_start[b0 + tid] = start;
       s_start[tid] = start;
     }
-    __syncthreads();
+    if (ONE) {
+      s_kv[tid] = w.kv;
+      s_rows[tid] = w.rows;
+      s_need[tid] = now;
+    }
+    // sequences after the first that was refused take none
+    const bool any_bad = __syncthreads_or(!ok);
     const int n = min(B - b0, kPlanThreads);
-    const long long room = min(t, static_cast<long long>(count1) - taken);
+    const long long room = min(t.grow, static_cast<long long>(count1) - taken);
+#pragma unroll 4
     for (int j = tid; j < room; j += kPlanThreads) {
       const int x = upper(s_off, n, j);
       const int k = j - s_off[x];
-      if (k < s_need[x])
+      if (k < s_grow[x])
         p.s.page_table[static_cast<size_t>(b0 + x) * p.s.max_pages + s_held[x] + k] =
             p.s.free_pages[count1 - 1 - (taken + j)];
     }
     // (a sequence refused above keeps num_held as it is, whatever it says)
     if (live && now != w.held) p.s.num_held[b0 + tid] = now;
-    // sequences after the first that was refused took none
-    const bool any_bad = __syncthreads_or(!ok);
     if (any_bad && !short_of) {
-      long long mx = ok && grow > 0 ? off + grow : 0;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        const long long u = __shfl_xor(mx, o, PTD_WAVE);
-        mx = u > mx ? u : mx;
-      }
-      if ((tid & 63) == 0) s_scan[tid >> 6] = mx;
+      // (at most num_pages, as they were taken)
+      const int used = ptd::wave_max_i32(ok && grow > 0 ? static_cast<int>(at.grow) + grow : 0);
       __syncthreads();
-      mx = 0;
-      for (int w2 = 0; w2 < kPlanWaves; ++w2) mx = max(mx, s_scan[w2]);
+      if ((tid & 63) == 0) s_scan[tid >> 6].grow = used;
       __syncthreads();
+      long long mx = 0;
+      for (int x = 0; x < kPlanWaves; ++x) mx = max(mx, s_scan[x].grow);
       if (tid == 0) p.s.num_free[0] = count1 - static_cast<int>(taken + mx);
       short_of = true;
     }
-    taken += t;
-    rows += tr;
+    taken += t.grow;
+    rows += t.rows;
+    if (!ONE) __syncthreads();
   }
   if (tid == 0) {
     if (!short_of) p.s.num_free[0] = count1 - static_cast<int>(taken);
@@ -237,9 +247,29 @@ __global__ void __launch_bounds__(kPlanThreads) k_page_plan(PlanParams p) {
     }
   }
   if (p.N > kPlanRows) return;
-  __syncthreads();
-  if (p.rows_per_seq > 0 || B <= kPlanThreads) put_rows(p, s_start, tid, p.N, kPlanThreads);
-  else put_rows(p, p.row_start, tid, p.N, kPlanThreads);
+  if (ONE) {
+    // ids of pages that were held come from the table, of new ones from the free list
+#pragma unroll 4
+    for (int i = tid; i < p.N; i += kPlanThreads) {
+      int b, r;
+      if (p.rows_per_seq > 0) {
+        b = i / p.rows_per_seq;
+        r = i - b * p.rows_per_seq;
+      } else {
+        b = upper(s_start, B, i);
+        r = i - s_start[b];
+      }
+      const bool row = r < s_rows[b];
+      const int pos = s_kv[b] + r;
+      const int pg = pos >> p.page_shift;
+      const bool page = row && pg < s_need[b];
+      const int32_t* from = pg < s_held[b] ? table_of(p, b) + pg : p.s.free_pages + (count1 - 1 - (s_off[b] + pg - s_held[b]));
+      put_row(p, i, page ? slot_at(p, *from, pos) : -1, row ? pos : -1);
+    }
+  } else {
+    __syncthreads();
+    put_rows(p, p.row_start, tid, p.N, kPlanThreads);
+  }
 }
 
 constexpr int kSlotThreads = 256;
@@ -312,7 +342,6 @@ struct Row8<uint16_t> {
     const uint4 v = *reinterpret_cast<const uint4*>(s);
     w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
   }
-  __device__ void clear() { w[0] = w[1] = w[2] = w[3] = 0u; }
   // (the compiler would keep the floats of one use for the next: twice the registers)
   __device__ void forget() { asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3])); }
   __device__ float at(int j) const { return (j & 1) ? ptd::bf16_hi(w[j >> 1]) : ptd::bf16_lo(w[j >> 1]); }
@@ -332,9 +361,6 @@ struct Row8<float> {
     const uint4 a = *reinterpret_cast<const uint4*>(s), b = *reinterpret_cast<const uint4*>(s + 4);
     w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
     w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
-  }
-  __device__ void clear() {
-    for (int j = 0; j < 8; ++j) w[j] = 0u;
   }
   __device__ void forget() {
     asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]), "+v"(w[4]), "+v"(w[5]), "+v"(w[6]), "+v"(w[7]));
@@ -370,7 +396,7 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float(static_cas
 // m < 2, that is x - 8, or x - 7 where m > 1.75.  A power of two leaves the
 // codes' three mantissa bits untouched, so a live row is coded anew without
 // loss while it stays a normal number of the format.
-template <typename T, int S>
+template <typename T, int S, bool FROM>
 __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
   constexpr int R = S / 4;  // rows per lane
   // registers hold the block's rows (up to 64 registers of them), or 32 rows at a
@@ -380,12 +406,17 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kind = wave & 1;
-  const int g = blockIdx.y * 2 + (wave >> 1);
+  // (head pairs run fastest: workgroups in flight together read whole rows of all heads, and
+  // not the same few memory channels)
+  const int pairs = (p.Hkv + 1) / 2;
+  const uint32_t id = blockIdx.x + gridDim.x * blockIdx.y;
+  const int part = static_cast<int>(id / pairs);
+  const int g = static_cast<int>(id % pairs) * 2 + (wave >> 1);
   if (g >= p.Hkv) return;
   const int sub = lane >> 4, d8 = (lane & 15) * 8;
   const T* src = static_cast<const T*>(p.src[kind]) + static_cast<size_t>(g) * kHeadDim + d8;
   const int64_t ld = p.ld[kind];
-  const int end = static_cast<int>(min(static_cast<long long>(p.N), (blockIdx.x + 1LL) * p.chunk));
+  const int end = static_cast<int>(min(static_cast<long long>(p.N), (part + 1LL) * p.chunk));
   // slot of row i, or -1 (off the rows, not to be written, outside the pages)
   auto slot_of = [&](int i) __attribute__((always_inline)) {
     int s = i >= 0 && i < p.N ? p.slots[i] : -1;
@@ -395,7 +426,7 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
     }
     return s;
   };
-  for (int i = blockIdx.x * p.chunk; i < end;) {
+  for (int i = static_cast<int>(min(static_cast<long long>(p.N), static_cast<long long>(part) * p.chunk)); i < end;) {
     // next row of the chunk that opens a block: one whose row before it is not in
     // the same block
     const int cur = slot_of(i + lane), prev = slot_of(i + lane - 1);
@@ -406,38 +437,54 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
       i += PTD_WAVE;
       continue;
     }
-    i += __builtin_ctzll(heads);
-    // the run: rows whose slots go on by one inside the block
-    const int slot0 = __builtin_amdgcn_readfirstlane(slot_of(i));
+    const int first = __builtin_ctzll(heads);
+    i += first;
+    const int slot0 = __builtin_amdgcn_readlane(cur, first);
     const int off0 = slot0 & (S - 1);
-    int n = 0;
-#pragma unroll
-    for (int h = 0; h < (S + 63) / 64; ++h) {
-      const int j = h * 64 + lane;
-      const bool in = j < S - off0 && slot_of(i + j) == slot0 + j;
-      const uint64_t m = ~__ballot(in);
-      if (n == h * 64) n += m ? __builtin_ctzll(m) : 64;
+    // the run: rows whose slots go on by one inside the block, in this window or the next ones
+    const uint64_t goes_on = __ballot(same && cur == prev + 1) >> first >> 1;
+    int n = 1 + __builtin_ctzll(~goes_on);
+    if (first + n == PTD_WAVE) {
+      for (int j = n; j < S - off0; j += PTD_WAVE) {  // uniform
+        const uint64_t m = ~__ballot(j + lane < S - off0 && slot_of(i + j + lane) == slot0 + j + lane);
+        n += m ? __builtin_ctzll(m) : PTD_WAVE;
+        if (m) break;
+      }
     }
     const size_t block = (((static_cast<size_t>(slot0) >> p.page_shift) * p.Hkv + g) << (p.page_shift - p.scale_shift)) +
                          ((slot0 & ((1 << p.page_shift) - 1)) >> p.scale_shift);
     uint8_t* page = p.pages[kind] + block * (S * kHeadDim) + d8;
     uint8_t* scale = p.scales + block * 2 + kind;
     Row8<T> x[RH];
+    uint2 old[R];  // codes of the live rows
+    int e_old = 0;
     auto is_new = [&](int r) __attribute__((always_inline)) { return r >= off0 && r < off0 + n; };
+    // source row of the run's row j, in lane j % 64 of word j / 64
+    int source[(S + 63) / 64];
+    if constexpr (FROM) {
+#pragma unroll
+      for (int h = 0; h < (S + 63) / 64; ++h) {
+        const int row = i + min(h * 64 + lane, n - 1);
+        const int f = p.from[row];
+        if (f < 0 || f >= p.rows_per_seq) ptd::report(p.dev_status, PTD_ERR_ROWS);
+        source[h] = row / p.rows_per_seq * p.rows_per_seq + min(max(f, 0), p.rows_per_seq - 1);
+      }
+    }
+    // (rows outside the run stand for its first or last one: another look at the same
+    // elements changes no maximum, and a load without a condition no register)
     auto load = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
       for (int t = 0; t < RH; ++t) {
-        const int r = 4 * (t0 + t) + sub;
-        x[t].clear();
-        if (is_new(r)) {
-          int row = i + r - off0;
-          if (p.from) {
-            const int f = p.from[row];
-            if (f < 0 || f >= p.rows_per_seq) ptd::report(p.dev_status, PTD_ERR_ROWS);
-            row = row / p.rows_per_seq * p.rows_per_seq + min(max(f, 0), p.rows_per_seq - 1);
+        const int j = min(max(4 * (t0 + t) + sub - off0, 0), n - 1);
+        int row = i + j;
+        if constexpr (FROM) {
+          row = __shfl(source[0], j & 63, PTD_WAVE);
+          if constexpr (S > 64) {
+            const int far = __shfl(source[1], j & 63, PTD_WAVE);
+            row = j < 64 ? row : far;
           }
-          x[t].load(src + row * ld);
         }
+        x[t].load(src + row * ld);
       }
     };
     // ---- largest magnitude
@@ -445,6 +492,13 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
     bool odd = false;  // something not finite
     for (int t0 = 0; t0 < R; t0 += RH) {
       load(t0);
+      if (t0 == 0 && off0 > 0) {  // uniform: all of the block's loads in flight together
+        e_old = *scale;
+#pragma unroll
+        for (int t = 0; t < R; ++t) {
+          old[t] = *reinterpret_cast<const uint2*>(page + min(4 * t + sub, off0 - 1) * kHeadDim);
+        }
+      }
       uint32_t m = 0;
 #pragma unroll
       for (int t = 0; t < RH; ++t) m = max(m, x[t].top());
@@ -462,21 +516,18 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
       top = max(top, m);
     }
     if (odd) ptd::report(p.dev_status, PTD_ERR_VALUE);
-    int e_old = 0;
-    if (off0 > 0) {  // uniform: live rows
-      e_old = __builtin_amdgcn_readfirstlane(*scale) - 127;
+    if (off0 > 0) {
+      e_old = __builtin_amdgcn_readfirstlane(e_old) - 127;
       uint32_t code = 0;
-      for (int r = sub; r < off0; r += 4) {
-        const uint2 c = *reinterpret_cast<const uint2*>(page + r * kHeadDim);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) code = max(code, max((c.x >> (8 * j)) & 0x7Fu, (c.y >> (8 * j)) & 0x7Fu));
-      }
+      for (int t = 0; t < R; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) code = max(code, max((old[t].x >> (8 * j)) & 0x7Fu, (old[t].y >> (8 * j)) & 0x7Fu));
       // its value, times the scale it was coded with (both in normal range)
       const float v = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(min(code, 0x7Eu)), 0) * pow2(min(max(e_old, -126), kExpMax));
       top = max(top, __float_as_uint(v));
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), o, PTD_WAVE)));
+    top = static_cast<uint32_t>(ptd::wave_max_i32(static_cast<int>(top)));
     int e = static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
     e = top == 0 ? 0 : min(max(e, kExpMin), kExpMax);
     // ---- codes
@@ -497,21 +548,24 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
     }
     if (off0 > 0 && e != e_old) {  // uniform
       const float fo = pow2(min(max(e_old - e, -126), 127));
-      for (int r = sub; r < off0; r += 4) {
-        const uint2 c = *reinterpret_cast<const uint2*>(page + r * kHeadDim);
-        float y[8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int w = static_cast<int>(h ? c.y : c.x);
-          y[4 * h + 0] = __builtin_amdgcn_cvt_f32_fp8(w, 0);
-          y[4 * h + 1] = __builtin_amdgcn_cvt_f32_fp8(w, 1);
-          y[4 * h + 2] = __builtin_amdgcn_cvt_f32_fp8(w, 2);
-          y[4 * h + 3] = __builtin_amdgcn_cvt_f32_fp8(w, 3);
+      for (int t = 0; t < R; ++t) {
+        asm volatile("" : "+v"(old[t].x), "+v"(old[t].y));  // (as forget())
+        if (4 * t + sub < off0) {
+          float y[8];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int w = static_cast<int>(h ? old[t].y : old[t].x);
+            y[4 * h + 0] = __builtin_amdgcn_cvt_f32_fp8(w, 0);
+            y[4 * h + 1] = __builtin_amdgcn_cvt_f32_fp8(w, 1);
+            y[4 * h + 2] = __builtin_amdgcn_cvt_f32_fp8(w, 2);
+            y[4 * h + 3] = __builtin_amdgcn_cvt_f32_fp8(w, 3);
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = to_range(y[j], fo);
+          *reinterpret_cast<uint2*>(page + (4 * t + sub) * kHeadDim) =
+              make_uint2(codes4(y[0], y[1], y[2], y[3]), codes4(y[4], y[5], y[6], y[7]));
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = to_range(y[j], fo);
-        *reinterpret_cast<uint2*>(page + r * kHeadDim) =
-            make_uint2(codes4(y[0], y[1], y[2], y[3]), codes4(y[4], y[5], y[6], y[7]));
       }
     }
     if (lane == 0) *scale = static_cast<uint8_t>(e + 127);
@@ -519,11 +573,11 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
   }
 }
 
-template <typename T>
+template <typename T, bool FROM>
 void launch_write(const WriteParams& prm, int scale_rows, dim3 grid, hipStream_t st) {
-  if (scale_rows == 32) hipLaunchKernelGGL((k_kv_write<T, 32>), grid, dim3(kWriteThreads), 0, st, prm);
-  else if (scale_rows == 64) hipLaunchKernelGGL((k_kv_write<T, 64>), grid, dim3(kWriteThreads), 0, st, prm);
-  else hipLaunchKernelGGL((k_kv_write<T, 128>), grid, dim3(kWriteThreads), 0, st, prm);
+  if (scale_rows == 32) hipLaunchKernelGGL((k_kv_write<T, 32, FROM>), grid, dim3(kWriteThreads), 0, st, prm);
+  else if (scale_rows == 64) hipLaunchKernelGGL((k_kv_write<T, 64, FROM>), grid, dim3(kWriteThreads), 0, st, prm);
+  else hipLaunchKernelGGL((k_kv_write<T, 128, FROM>), grid, dim3(kWriteThreads), 0, st, prm);
 }
 
 }  // namespace
@@ -559,7 +613,8 @@ extern "C" int ptd_page_plan(const ptd_page_state* state, const int32_t* kv_len,
   prm.N = N;
   prm.rows_per_seq = rows_per_seq;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(k_page_plan, dim3(1), dim3(kPlanThreads), 0, st, prm);
+  if (state->B <= kPlanThreads) hipLaunchKernelGGL(k_page_plan<true>, dim3(1), dim3(kPlanThreads), 0, st, prm);
+  else hipLaunchKernelGGL(k_page_plan<false>, dim3(1), dim3(kPlanThreads), 0, st, prm);
   if (N > kPlanRows) {
     const unsigned grid = static_cast<unsigned>((static_cast<long long>(N) + kSlotRows - 1) / kSlotRows);
     hipLaunchKernelGGL(k_page_slots, dim3(grid), dim3(kSlotThreads), 0, st, prm);
@@ -613,9 +668,13 @@ extern "C" int ptd_kv_write_fp8blk(const void* k, const void* v, ptd_dtype dtype
   const int pairs = (Hkv + 1) / 2;
   prm.chunk = sr;
   while (prm.chunk > 1 && (static_cast<long long>(N) + prm.chunk - 1) / prm.chunk * pairs < 1024) prm.chunk /= 2;
-  const dim3 grid(static_cast<unsigned>((static_cast<long long>(N) + prm.chunk - 1) / prm.chunk), pairs);
+  // (two dimensions: one holds fewer than 2^32 threads; workgroups past the rows find none)
+  const long long all = (static_cast<long long>(N) + prm.chunk - 1) / prm.chunk * pairs;
+  PTD_RETURN_IF(all > 0x7FFFFFFFLL, PTD_ERR_SHAPE);
+  const long long gx = std::min(all, 1LL << 20);
+  const dim3 grid(static_cast<unsigned>(gx), static_cast<unsigned>((all + gx - 1) / gx));
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (dtype == PTD_F32) launch_write<float>(prm, sr, grid, st);
-  else launch_write<uint16_t>(prm, sr, grid, st);
+  if (dtype == PTD_F32) src ? launch_write<float, true>(prm, sr, grid, st) : launch_write<float, false>(prm, sr, grid, st);
+  else src ? launch_write<uint16_t, true>(prm, sr, grid, st) : launch_write<uint16_t, false>(prm, sr, grid, st);
   return ptd_launch_status();
 }

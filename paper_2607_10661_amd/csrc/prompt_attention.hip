@@ -55,25 +55,6 @@ struct TileOf {
   int start, n, r0, g;
 };
 
-// Sum and largest of a wave's values >= 0 (DPP: shifts within rows of 16 lanes, then
-// broadcasts of rows' last lanes; lanes without a source add 0).
-template <typename F>
-__device__ __forceinline__ int wave_reduce(int v, F f) {
-  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true));   // row_shr:1
-  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true));   // row_shr:2
-  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true));   // row_shr:4
-  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true));   // row_shr:8
-  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));  // row_bcast:15
-  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));  // row_bcast:31
-  return __builtin_amdgcn_readlane(v, 63);
-}
-__device__ __forceinline__ int wave_sum_i32(int v) {
-  return wave_reduce(v, [](int a, int b) { return a + b; });
-}
-__device__ __forceinline__ int wave_max_i32(int v) {
-  return wave_reduce(v, [](int a, int b) { return max(a, b); });
-}
-
 // Tile number w of all sequences' tiles; false past the last one.  Up to 64 sequences:
 // longest tiles first (tile k of a sequence has k + 1 times the first one's keys), so that
 // the short ones fill in at the end; more: sequence by sequence, each one's
@@ -103,15 +84,15 @@ __device__ __forceinline__ bool find_tile(const PromptParams& p, long long w, Ti
     } else if (p.B <= PTD_WAVE) {
       // level k: the tiles k of the sequences that have one; above it lie
       // sum max(nt - k - 1, 0) tiles.  w belongs to the least k with no more than w above it.
-      if (w >= wave_sum_i32(nt)) return false;
-      int lo = 0, hi = wave_max_i32(nt) - 1;
+      if (w >= ptd::wave_sum_i32(nt)) return false;
+      int lo = 0, hi = ptd::wave_max_i32(nt) - 1;
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (wave_sum_i32(max(nt - mid - 1, 0)) <= w) hi = mid;
+        if (ptd::wave_sum_i32(max(nt - mid - 1, 0)) <= w) hi = mid;
         else lo = mid + 1;
       }
       k = lo;
-      const int above = wave_sum_i32(max(nt - k - 1, 0));
+      const int above = ptd::wave_sum_i32(max(nt - k - 1, 0));
       // the (w - above)-th of the sequences with more than k tiles
       uint64_t has = __ballot(nt > k);
       for (int i = static_cast<int>(w) - above; i > 0; --i) has &= has - 1;

@@ -68,6 +68,43 @@ __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
   return v;
 }
 
+
+// Over a wave by DPP: shifts within rows of 16 lanes, then broadcasts of the rows' last
+// lanes; a lane without a source gets 0.  scan: inclusive; reduce: to every lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp0(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, ROWS == 0xF);
+}
+template <typename F>
+__device__ __forceinline__ int wave_scan_i32(int v, F f) {
+  v = f(v, dpp0<0x111, 0xF>(v));  // row_shr:1, 2, 4, 8
+  v = f(v, dpp0<0x112, 0xF>(v));
+  v = f(v, dpp0<0x114, 0xF>(v));
+  v = f(v, dpp0<0x118, 0xF>(v));
+  v = f(v, dpp0<0x142, 0xA>(v));  // row_bcast:15, row_bcast:31
+  return f(v, dpp0<0x143, 0xC>(v));
+}
+__device__ __forceinline__ int wave_sum_i32(int v) {
+  return __builtin_amdgcn_readlane(wave_scan_i32(v, [](int a, int b) { return a + b; }), 63);
+}
+__device__ __forceinline__ int wave_max_i32(int v) {  // of values >= 0
+  return __builtin_amdgcn_readlane(wave_scan_i32(v, [](int a, int b) { return a > b ? a : b; }), 63);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ long long dpp0_i64(long long v) {
+  const uint32_t lo = static_cast<uint32_t>(dpp0<CTRL, ROWS>(static_cast<int>(v)));
+  const int hi = dpp0<CTRL, ROWS>(static_cast<int>(v >> 32));
+  return (static_cast<long long>(hi) << 32) | lo;
+}
+__device__ __forceinline__ long long wave_scan_i64(long long v) {
+  v += dpp0_i64<0x111, 0xF>(v);
+  v += dpp0_i64<0x112, 0xF>(v);
+  v += dpp0_i64<0x114, 0xF>(v);
+  v += dpp0_i64<0x118, 0xF>(v);
+  v += dpp0_i64<0x142, 0xA>(v);
+  return v + dpp0_i64<0x143, 0xC>(v);
+}
+
 }  // namespace ptd
 
 // ---------------------------------------------------------------------------
