@@ -316,10 +316,13 @@ typedef struct {
  * ptd_tree_attention_paged_fp8blk -- ptd_tree_attention_paged_fp8kv on pages
  * with block scales: key row j = e4m3(code) * 2^(e - 127) with e of its block,
  * values likewise.  Codes and scale widen to bf16 exactly wherever the product
- * is a normal bf16 number, so the arithmetic is that of the bf16 path on the
- * decoded pages (bit for bit).  A tree of one node is the decoding step of a
+ * is a normal bf16 number.  The softmax weights are rounded to bf16 above and
+ * below the line (out within 2^-7 of the largest value it averages, before its
+ * own rounding; the bf16 path carries large weights with twice the bits, which a
+ * value known to 2^-4 does not need).  A tree of one node is the decoding step of a
  * single token; a chain of up to PTD_MAX_T nodes continues a prompt whose
- * beginning is cached.  Blocks without a live row (committed, or of a live
+ * beginning is cached.  The exponents are read as 4-byte words: the last one of
+ * the array has to be readable as a whole.  Blocks without a live row (committed, or of a live
  * node) are not read beyond the sub-tile of 32 rows that holds the last one.
  * Other arguments, workspace, dev_status and errors as
  * ptd_tree_attention_paged_fp8kv; PTD_ERR_SHAPE for scale_rows.

@@ -211,6 +211,10 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
   constexpr bool F8 = KIND != kBf16;
   constexpr bool BLK = KIND == kE4m3Block;
   static_assert(!BLK || PAGED, "block scales live in pages");
+  // Weights above kPreciseFrac as bf16 hi + lo.  Not for block scales, whose codes are off by
+  // up to 2^-4 of a value where a bf16 weight is off by 2^-8 of itself (16 sequences of
+  // 512-8192 keys with outliers: 106 against 124 us).
+  constexpr bool RESIDUE = !BLK;
   using KV = std::conditional_t<F8, uint8_t, uint16_t>;
   constexpr int ES = F8 ? 1 : 2;
   using R = Ring<D, ES, NT>;
@@ -496,25 +500,30 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
   // together with the ring copies behind it.  A block is at least a sub-tile, so
   // one pair serves the wave's 32 keys.  e0 belongs to the wave's sub-tile of the
   // round, e1 to the next round's; the one after that is requested at the head
-  // of a round, ahead of its wait and barrier.
+  // of a round, ahead of its wait and barrier.  The staged pages' first blocks
+  // are worked out once, a page per lane: the scalar unit serves all waves.
   using cu32 = const __attribute__((address_space(4))) uint32_t;
+  const int blocks_shift = BLK ? p.page_shift - p.scale_shift : 0;  // blocks per page and head
+  uint32_t pgb[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) pgb[r] = BLK ? (pg[r] * p.Hkv + g) << blocks_shift : 0u;
   auto tile_scales = [&](int t) __attribute__((always_inline)) -> uint32_t {
     if constexpr (!BLK) return 0u;
     const int row0 = start + min(t, (end - start - 1) / R::SUB) * R::SUB;
     const int ti = (row0 >> p.page_shift) - first_page;
-    uint32_t phys;
-    if (ti < 4 * PTD_WAVE) {
-      const uint32_t v0 = __builtin_amdgcn_readlane(pg[0], ti & 63);
-      const uint32_t v1 = __builtin_amdgcn_readlane(pg[1], ti & 63);
-      const uint32_t v2 = __builtin_amdgcn_readlane(pg[2], ti & 63);
-      const uint32_t v3 = __builtin_amdgcn_readlane(pg[3], ti & 63);
-      phys = ti < 64 ? v0 : ti < 128 ? v1 : ti < 192 ? v2 : v3;
+    uint32_t blk;
+    if (ti < PTD_WAVE) {
+      blk = __builtin_amdgcn_readlane(pgb[0], ti);
+    } else if (ti < 4 * PTD_WAVE) {
+      const uint32_t v1 = __builtin_amdgcn_readlane(pgb[1], ti & 63);
+      const uint32_t v2 = __builtin_amdgcn_readlane(pgb[2], ti & 63);
+      const uint32_t v3 = __builtin_amdgcn_readlane(pgb[3], ti & 63);
+      blk = ti < 128 ? v1 : ti < 192 ? v2 : v3;
     } else {  // beyond the staged ids (reported by the sub-tile's copy)
-      phys = ((cu32*)p.page_table)[static_cast<size_t>(b) * p.max_pages + (row0 >> p.page_shift)];
-      phys = phys < static_cast<uint32_t>(p.num_pages) ? phys : 0u;
+      const uint32_t phys = ((cu32*)p.page_table)[static_cast<size_t>(b) * p.max_pages + (row0 >> p.page_shift)];
+      blk = ((phys < static_cast<uint32_t>(p.num_pages) ? phys : 0u) * p.Hkv + g) << blocks_shift;
     }
-    const size_t blk = ((static_cast<size_t>(phys) * p.Hkv + g) << (p.page_shift - p.scale_shift)) +
-                       ((row0 & ((1 << p.page_shift) - 1)) >> p.scale_shift);
+    blk += (row0 & ((1 << p.page_shift) - 1)) >> p.scale_shift;
     return ((cu32*)p.scales)[blk >> 1] >> (16 * (blk & 1));
   };
   uint32_t e0 = 0, e1 = 0;
@@ -811,7 +820,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
     unsigned pmask = 0;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
-      pmask |= __any(!(pm[qb] <= p.precise * ls[qb][0])) ? (1u << qb) : 0u;
+      pmask |= RESIDUE && __any(!(pm[qb] <= p.precise * ls[qb][0])) ? (1u << qb) : 0u;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const bool precise = pmask & (1u << qb);
@@ -989,7 +998,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
         unsigned pmask = 0;
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
-          pmask |= __any(!(pm[qb] <= p.precise * ls[qb][0])) ? (1u << qb) : 0u;
+          pmask |= RESIDUE && __any(!(pm[qb] <= p.precise * ls[qb][0])) ? (1u << qb) : 0u;
         PFrag pf;
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {

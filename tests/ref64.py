@@ -87,3 +87,29 @@ def write_block(live, live_e, new):
     e = scale_exponent(np.abs(x[np.isfinite(x)]).max(initial=0.0))
     y = x * 2.0 ** -e
     return e4m3_round(np.nan_to_num(y, nan=0.0, posinf=1e9, neginf=-1e9)), e
+
+
+def tree(q, k, v, kv_len, parent, scale, live):
+    """Tree attention of one sequence: q [T][Hq][D], k, v [Hkv][rows][D] with node i's row at
+    kv_len + i.  Returns the outputs of the `live` first nodes (the others zero) and the
+    averages of |v| under the same weights."""
+    q, k, v = (x.double() for x in (q, k, v))
+    T, Hq, D = q.shape
+    G = Hq // k.shape[0]
+    out, mag = torch.zeros_like(q), torch.zeros_like(q)
+    if not live:
+        return out, mag
+    anc = torch.zeros((live, live), dtype=torch.bool)
+    for i in range(live):
+        if parent[i] >= 0:
+            anc[i] = anc[int(parent[i])]
+        anc[i, i] = True
+    seen = torch.cat((torch.ones((live, kv_len), dtype=torch.bool), anc), 1).to(q.device)
+    for h in range(Hq):
+        kh, vh = k[h // G, :kv_len + live], v[h // G, :kv_len + live]
+        x = (q[:live, h] @ kh.t().contiguous() * scale).masked_fill(~seen, -np.inf)
+        w = torch.exp(x - x.amax(1, keepdim=True))
+        w = w / w.sum(1, keepdim=True)
+        out[:live, h] = w @ vh
+        mag[:live, h] = w @ vh.abs()
+    return out, mag
