@@ -43,7 +43,7 @@ struct PromptParams {
   int32_t* dev_status;
   int64_t ldq, ldk, ldv;  // elements
   int B, N, Hq, Hkv, G;
-  long long items;  // tiles (an upper bound) * Hkv
+  uint32_t items;  // tiles (an upper bound) * Hkv
   float c;          // scale * log2(e)
   int out_bf16;
   int wide;  // 64 rows span 2 GiB and more: no 32-bit offsets
@@ -60,7 +60,8 @@ struct TileOf {
 // the short ones fill in at the end; more: sequence by sequence, each one's
 // longest first.  Every lane of a wave takes part.
 template <int TM>
-__device__ __forceinline__ bool find_tile(const PromptParams& p, long long w, TileOf& t) {
+__device__ __forceinline__ bool find_tile(const PromptParams& p, uint32_t tile, TileOf& t) {
+  long long w = tile;
   const int lane = threadIdx.x & 63;
   for (int b0 = 0; b0 < p.B; b0 += PTD_WAVE) {
     const int b = b0 + lane;
@@ -124,20 +125,20 @@ __device__ __forceinline__ bool find_tile(const PromptParams& p, long long w, Ti
 // them (one L2 each) as its share of the work allows.
 template <int TM>
 __device__ __forceinline__ bool my_tile(const PromptParams& p, TileOf& t) {
-  const long long id = blockIdx.x + static_cast<long long>(gridDim.x) * blockIdx.y;
+  const uint32_t id = blockIdx.x + gridDim.x * blockIdx.y;
   if (id >= p.items) return false;
-  const int H = p.Hkv;
-  long long w;
+  const uint32_t H = p.Hkv;
+  uint32_t w;
   if ((H & 7) == 0) {
-    const long long j = id >> 3;
-    t.g = static_cast<int>((id & 7) + 8 * (j % (H >> 3)));
+    const uint32_t j = id >> 3;
     w = j / (H >> 3);
-  } else if ((8 % H) == 0) {
-    t.g = static_cast<int>((id & 7) % H);
-    w = (id >> 3) * (8 / H) + (id & 7) / H;
-  } else {
-    t.g = static_cast<int>(id % H);
+    t.g = static_cast<int>((id & 7) + 8 * (j - w * (H >> 3)));
+  } else if (H <= 4 && H != 3) {
+    t.g = static_cast<int>(id & (H - 1));  // (H divides 8)
     w = id / H;
+  } else {
+    w = id / H;
+    t.g = static_cast<int>(id - w * H);
   }
   if (!find_tile<TM>(p, w, t)) return false;
   // (uniform: said so, or every loop and branch by them is made of lane masks)
@@ -332,24 +333,37 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
     l += r.sum;
   };
   auto over_of = [](const Weights& r) __attribute__((always_inline)) { return __ballot(!(r.sum <= 65536.f)); };
-  auto pv = [&](const unsigned char* slot, int kb, const Weights& r) __attribute__((always_inline)) {
+  struct Values {
+    u32x4 v[2][DT];
+  };
+  auto read_v = [&](const unsigned char* slot, int kb) __attribute__((always_inline)) {
+    Values r;
 #pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{r.w[4 * st], r.w[4 * st + 1], r.w[4 * st + 2], r.w[4 * st + 3]});
+    for (int st = 0; st < 2; ++st)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const u32x2 a = lds_read_tr16(slot + voff[0][dt] + (32 * kb + 16 * st) * L::RB);
         const u32x2 b = lds_read_tr16(slot + voff[1][dt] + (32 * kb + 16 * st) * L::RB);
-        const u32x4 vw = {a[0], a[1], b[0], b[1]};
-        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vw), pf, o[dt], 0, 0, 0);
+        r.v[st][dt] = u32x4{a[0], a[1], b[0], b[1]};
       }
+    return r;
+  };
+  auto pv = [&](const Values& v, const Weights& r) __attribute__((always_inline)) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{r.w[4 * st], r.w[4 * st + 1], r.w[4 * st + 2], r.w[4 * st + 3]});
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v.v[st][dt]), pf, o[dt], 0, 0, 0);
     }
   };
   // A tile that every row sees whole.  The second half's QK^T runs beside the first half's
   // exponentials, the first half's PV beside the second's.
-  auto full_tile = [&](const unsigned char* slot, bool first) __attribute__((always_inline)) {
+  auto full_tile = [&](const unsigned char* slot, bool first, auto&& among) __attribute__((always_inline)) {
     const f32x16 s0 = qk(slot, 0);
+    among(0);
     const f32x16 s1 = qk(slot, 1);
+    among(1);
     Weights w0;
     uint64_t over = ~0ull;
     if (!first) {
@@ -357,10 +371,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
       over = over_of(w0);
     }
     settle(s0, w0, over);
+    among(2);
     Weights w1 = exps(s1);
-    pv(slot, 0, w0);
+    pv(read_v(slot, 0), w0);
     settle(s1, w1, over_of(w1));
-    pv(slot, 1, w1);
+    among(3);
+    pv(read_v(slot, 1), w1);
   };
   // a tile at some row's end: scores of keys behind a row's position become -inf
   auto end_tile = [&](const unsigned char* slot, int k0, bool first) __attribute__((always_inline)) {
@@ -371,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
       for (int e = 0; e < 16; ++e) s[e] = 32 * kb + 8 * (e / 4) + e % 4 <= lim ? s[e] : -INFINITY;
       Weights w = exps(s);
       settle(s, w, first && kb == 0 ? ~0ull : over_of(w));
-      pv(slot + kb * 32 * L::RB, 0, w);
+      pv(read_v(slot + kb * 32 * L::RB, 0), w);
     }
   };
   // A tile that not every row sees whole: 0 * inf must not reach a row that does not
@@ -430,24 +446,41 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
     if (tt + 1 < ntiles) issue(tt + 1);
   };
   // tiles that every row of the workgroup sees whole, then those that end at some row
-  const int full = (t.r0 / p.G + 1) / L::KEYS;
+  // (the last tile is among these: a full one has a next one)
+  const int full = min((t.r0 / p.G + 1) / L::KEYS, ntiles - 1);
   int tt = 0;
+  auto nothing = [](int) __attribute__((always_inline)) {};
   if (full > 0) {
     next(0, false);
-    full_tile(smem, true);
+    full_tile(smem, true, nothing);
     tt = 1;
   }
-  // two tiles a turn: their places in LDS are constants of the instructions
-  for (; tt + 1 < full; tt += 2) {
-    next(tt, false);
-    full_tile(smem + L::SLOT, false);
-    next(tt + 1, false);
-    full_tile(smem, false);
+  // Two tiles a turn: their places in LDS are constants of the instructions.  The next
+  // tile's copies are issued among a tile's products, a quarter at a time: together they
+  // keep a wave at the vector memory unit for 600 of a tile's 2900 cycles.
+  const int whole = p.wide ? 0 : min(full, t.n / L::KEYS - 1);  // tiles before a whole one
+  auto spread = [&](int tt, int place) __attribute__((always_inline)) {
+    const uint16_t* kt = kbase + static_cast<size_t>(tt) * L::KEYS * p.ldk;
+    const uint16_t* vt = vbase + static_cast<size_t>(tt) * L::KEYS * p.ldv;
+    const uint32_t dst = ring + place * L::SLOT + wave * PTD_WAVE * 16;
+    return [=](int q) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < L::CPT; ++u)
+        if (u * 4 / L::CPT == q)
+          ptd::dma16_s2_among(kt, c_k[u], dst + u * kThreads * 16, vt, c_v[u], dst + L::PART + u * kThreads * 16);
+    };
+  };
+  for (; tt + 1 < whole; tt += 2) {
+    wait_vmcnt<0>();
+    lds_barrier();
+    full_tile(smem + L::SLOT, false, spread(tt + 1, 0));
+    wait_vmcnt<0>();
+    lds_barrier();
+    full_tile(smem, false, spread(tt + 2, 1));
   }
-  if (tt < full) {
+  for (; tt < full; ++tt) {
     next(tt, false);
-    full_tile(smem + L::SLOT, false);
-    ++tt;
+    full_tile(smem + (tt % NS) * L::SLOT, false, nothing);
   }
   for (; tt < ntiles; ++tt) {
     next(tt, true);
@@ -714,18 +747,20 @@ extern "C" int ptd_prompt_attention(const void* q, const void* k, const void* v,
   const auto items_of = [&](int tm) {
     return (static_cast<long long>(s.N) * prm.G / tm + std::min(s.B, s.N)) * s.Hkv;
   };
+  // (the grid is rounded up to a multiple of 8 and of its first dimension: all ids fit 32 bits)
+  PTD_RETURN_IF(items_of(32) > 0x7FFFFFFFLL, PTD_ERR_SHAPE);
   const auto grid_of = [&](long long items) {  // two dimensions: one holds fewer than 2^32 threads
     const long long x = std::min<long long>((items + 7) / 8 * 8, 1 << 20);
     return dim3(static_cast<unsigned>(x), static_cast<unsigned>((items + x - 1) / x));
   };
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (s.in_dtype == PTD_F32) {
-    prm.items = items_of(32);
+    prm.items = static_cast<uint32_t>(items_of(32));
     const dim3 grid = grid_of(prm.items);
     if (s.D == 128) hipLaunchKernelGGL(k_prompt_f32<128>, grid, dim3(kF32Threads), 0, st, prm);
     else hipLaunchKernelGGL(k_prompt_f32<64>, grid, dim3(kF32Threads), 0, st, prm);
   } else {
-    prm.items = items_of(128);
+    prm.items = static_cast<uint32_t>(items_of(128));
     const dim3 grid = grid_of(prm.items);
     if (s.D == 128) hipLaunchKernelGGL(k_prompt_bf16<128>, grid, dim3(kThreads), 0, st, prm);
     else hipLaunchKernelGGL(k_prompt_bf16<64>, grid, dim3(kThreads), 0, st, prm);

@@ -80,6 +80,34 @@ __device__ __forceinline__ void dma16_s2(const void* base0, uint32_t voff0, uint
       : "memory");
 }
 
+// The same two copies without the compiler's memory barrier: for copies into LDS that
+// nothing reads or writes before the next barrier, issued among LDS reads of other
+// places that may move across them.
+__device__ __forceinline__ void dma16_s2_among(const void* base0, uint32_t voff0, uint32_t lds0,
+                                         const void* base1, uint32_t voff1, uint32_t lds1) {
+  const uint64_t b0 = reinterpret_cast<uint64_t>(base0);
+  const uint64_t b1 = reinterpret_cast<uint64_t>(base1);
+  const uint64_t s0 = (static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b0 >> 32)))) << 32) |
+                      static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b0)));
+  const uint64_t s1 = (static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b1 >> 32)))) << 32) |
+                      static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b1)));
+  lds0 = uniform_u32(lds0);
+  lds1 = uniform_u32(lds1);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %2, %3\n\t"
+      "s_mov_b32 m0, %4\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %5, %6\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(lds0), "v"(voff0), "s"(s0), "s"(lds1), "v"(voff1), "s"(s1)
+      :);
+}
+
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");

@@ -243,3 +243,10 @@ def test_rows_far_apart(P):
     assert torch.equal(P.prompt_attention(q, k, wide, i32([0, n])), want)
     wide.copy_(k)
     assert torch.equal(P.prompt_attention(q, wide, v, i32([0, n])), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_heads_share_a_position(P, dtype):
+    # a tile of rows is one position, so the last tile of keys can be seen whole
+    check(P, [130, 64, 193], 128, 1, 64, dtype)
+    check(P, [129], 96, 1, 128, dtype)
