@@ -404,6 +404,7 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
   // time that the second pass reads again
   constexpr bool HOLD = R * sizeof(T) * 2 <= 64;
   constexpr int RH = HOLD ? R : 8;
+  constexpr int RO = R <= 16 ? R : 8;  // the same for the codes of live rows
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kind = wave & 1;
@@ -457,7 +458,7 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
     uint8_t* page = p.pages[kind] + block * (S * kHeadDim) + d8;
     uint8_t* scale = p.scales + block * 2 + kind;
     Row8<T> x[RH];
-    uint2 old[R];  // codes of the live rows
+    uint2 old[RO];  // codes of the live rows
     int e_old = 0;
     auto is_new = [&](int r) __attribute__((always_inline)) { return r >= off0 && r < off0 + n; };
     // source row of the run's row j, in lane j % 64 of word j / 64
@@ -488,6 +489,11 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
         x[t].load(src + row * ld);
       }
     };
+    auto load_old = [&](int t0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int t = 0; t < RO; ++t)
+        old[t] = *reinterpret_cast<const uint2*>(page + min(4 * (t0 + t) + sub, off0 - 1) * kHeadDim);
+    };
     // ---- largest magnitude
     uint32_t top = 0;
     bool odd = false;  // something not finite
@@ -495,10 +501,7 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
       load(t0);
       if (t0 == 0 && off0 > 0) {  // uniform: all of the block's loads in flight together
         e_old = *scale;
-#pragma unroll
-        for (int t = 0; t < R; ++t) {
-          old[t] = *reinterpret_cast<const uint2*>(page + min(4 * t + sub, off0 - 1) * kHeadDim);
-        }
+        load_old(0);
       }
       uint32_t m = 0;
 #pragma unroll
@@ -520,10 +523,13 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
     if (off0 > 0) {
       e_old = __builtin_amdgcn_readfirstlane(e_old) - 127;
       uint32_t code = 0;
+      for (int t0 = 0; t0 < R && 4 * t0 < off0; t0 += RO) {  // uniform
+        if (t0 > 0) load_old(t0);
 #pragma unroll
-      for (int t = 0; t < R; ++t)
+        for (int t = 0; t < RO; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) code = max(code, max((old[t].x >> (8 * j)) & 0x7Fu, (old[t].y >> (8 * j)) & 0x7Fu));
+          for (int j = 0; j < 4; ++j) code = max(code, max((old[t].x >> (8 * j)) & 0x7Fu, (old[t].y >> (8 * j)) & 0x7Fu));
+      }
       // its value, times the scale it was coded with (both in normal range)
       const float v = __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(min(code, 0x7Eu)), 0) * pow2(min(max(e_old, -126), kExpMax));
       top = max(top, __float_as_uint(v));
@@ -549,23 +555,27 @@ __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
     }
     if (off0 > 0 && e != e_old) {  // uniform
       const float fo = pow2(min(max(e_old - e, -126), 127));
+      for (int t0 = 0; t0 < R && 4 * t0 < off0; t0 += RO) {  // uniform
+        if (RO < R) load_old(t0);
 #pragma unroll
-      for (int t = 0; t < R; ++t) {
-        asm volatile("" : "+v"(old[t].x), "+v"(old[t].y));  // (as forget())
-        if (4 * t + sub < off0) {
-          float y[8];
+        for (int t = 0; t < RO; ++t) {
+          const int r = 4 * (t0 + t) + sub;
+          asm volatile("" : "+v"(old[t].x), "+v"(old[t].y));  // (as forget())
+          if (r < off0) {
+            float y[8];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int w = static_cast<int>(h ? old[t].y : old[t].x);
-            y[4 * h + 0] = __builtin_amdgcn_cvt_f32_fp8(w, 0);
-            y[4 * h + 1] = __builtin_amdgcn_cvt_f32_fp8(w, 1);
-            y[4 * h + 2] = __builtin_amdgcn_cvt_f32_fp8(w, 2);
-            y[4 * h + 3] = __builtin_amdgcn_cvt_f32_fp8(w, 3);
+            for (int h = 0; h < 2; ++h) {
+              const int w = static_cast<int>(h ? old[t].y : old[t].x);
+              y[4 * h + 0] = __builtin_amdgcn_cvt_f32_fp8(w, 0);
+              y[4 * h + 1] = __builtin_amdgcn_cvt_f32_fp8(w, 1);
+              y[4 * h + 2] = __builtin_amdgcn_cvt_f32_fp8(w, 2);
+              y[4 * h + 3] = __builtin_amdgcn_cvt_f32_fp8(w, 3);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = to_range(y[j], fo);
+            *reinterpret_cast<uint2*>(page + r * kHeadDim) =
+                make_uint2(codes4(y[0], y[1], y[2], y[3]), codes4(y[4], y[5], y[6], y[7]));
           }
-#pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = to_range(y[j], fo);
-          *reinterpret_cast<uint2*>(page + (4 * t + sub) * kHeadDim) =
-              make_uint2(codes4(y[0], y[1], y[2], y[3]), codes4(y[4], y[5], y[6], y[7]));
         }
       }
     }
@@ -666,11 +676,12 @@ extern "C" int ptd_kv_write_fp8blk(const void* k, const void* v, ptd_dtype dtype
   while ((1 << prm.page_shift) < ps) ++prm.page_shift;
   prm.scale_shift = sr == 32 ? 5 : sr == 64 ? 6 : 7;
   // Rows per workgroup: a block's rows (one run each for prompts), halved while
-  // workgroups are too few to fill the chip -- a step's rows open several blocks
-  // within that many rows, which a wave would code one after the other.
+  // workgroups are fewer than CUs -- a step's rows open several blocks within that many
+  // rows, which a wave codes one after the other.  (16 x 64 rows: 7.3 us, and 10.1 with four
+  // times the workgroups, most of which find no block; 64 x 64 rows 11.6 and 23.)
   const int pairs = (Hkv + 1) / 2;
   prm.chunk = sr;
-  while (prm.chunk > 1 && (static_cast<long long>(N) + prm.chunk - 1) / prm.chunk * pairs < 1024) prm.chunk /= 2;
+  while (prm.chunk > 1 && (static_cast<long long>(N) + prm.chunk - 1) / prm.chunk * pairs < 256) prm.chunk /= 2;
   // (two dimensions: one holds fewer than 2^32 threads; workgroups past the rows find none)
   const long long all = (static_cast<long long>(N) + prm.chunk - 1) / prm.chunk * pairs;
   PTD_RETURN_IF(all > 0x7FFFFFFFLL, PTD_ERR_SHAPE);
