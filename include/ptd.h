@@ -450,7 +450,8 @@ typedef struct {
  * What a row may not see does not reach it, infinities and NaN included.  bf16
  * inputs run on v_mfma_f32_32x32x16_bf16 with the softmax weights rounded to bf16
  * above and below the line (out within 2^-7 of the largest value it averages,
- * before its own rounding); fp32 inputs on v_mfma_f32_32x32x2_f32, fp32 throughout.  q, k, v and out must be
+ * before its own rounding; scores |scale * q . k| below 2^30); fp32 inputs on
+ * v_mfma_f32_32x32x2_f32, fp32 throughout.  q, k, v and out must be
  * 16-byte aligned.  Outputs do not depend on the other sequences of the call.
  * dev_status: PTD_ERR_ROWS (a sequence whose start and end are not in order within
  * [0, N] is not computed).

@@ -322,9 +322,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
       mx = max_xor32(mx);
       const bool up = mine && mx > m;
-      const float alpha = up ? __builtin_amdgcn_exp2f((m - mx) * p.c) : 1.f;
+      // (from the products as they were rounded, which for large scores is off by more
+      // than the weights' own steps)
+      const float to = up ? -mx * p.c : nmc;
+      const float alpha = __builtin_amdgcn_exp2f(to - nmc);
       m = up ? mx : m;
-      nmc = -m * p.c;
+      nmc = to;
       l *= alpha;
 #pragma unroll
       for (int i = 0; i < DT; ++i) o[i] *= alpha;
@@ -630,11 +633,10 @@ __global__ void __launch_bounds__(kF32Threads, 2) k_prompt_f32(PromptParams p) {
     mx = fmaxf(m, max_xor32(mx));
     const float alpha = __builtin_amdgcn_exp2f((m - mx) * p.c);
     m = mx;
-    const float nmc = -m * p.c;
     float ps = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], p.c, nmc));
+      s[e] = __builtin_amdgcn_exp2f((s[e] - mx) * p.c);
       ps += s[e];
     }
     l = fmaf(l, alpha, ps);
@@ -743,9 +745,10 @@ extern "C" int ptd_prompt_attention(const void* q, const void* k, const void* v,
   prm.G = s.Hq / s.Hkv;
   prm.c = (s.scale > 0.f ? s.scale : 1.0f / sqrtf(static_cast<float>(s.D))) * kLog2e;
   prm.out_bf16 = s.out_dtype == PTD_BF16;
-  // every sequence has at most one tile that is not full
+  // every sequence has at most one tile that is not full; one more of none where the
+  // starts take several looks, so that somebody sees the last of them
   const auto items_of = [&](int tm) {
-    return (static_cast<long long>(s.N) * prm.G / tm + std::min(s.B, s.N)) * s.Hkv;
+    return (static_cast<long long>(s.N) * prm.G / tm + std::min(s.B, s.N) + (s.B > PTD_WAVE ? 1 : 0)) * s.Hkv;
   };
   // (the grid is rounded up to a multiple of 8 and of its first dimension: all ids fit 32 bits)
   PTD_RETURN_IF(items_of(32) > 0x7FFFFFFFLL, PTD_ERR_SHAPE);

@@ -121,6 +121,28 @@ def test_low_scores(P, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n", [64, 200, 450])
+def test_huge_scores(P, dtype, n):
+    # scores of up to 2^23, exact in fp32: a few keys 10 above the first one, 0 elsewhere, then one 12
+    # above it, so that the weights of the keys before count beside its own
+    D = 64
+    q, k, v = (torch.zeros((n, 1, D), device="cuda") for _ in range(3))
+    q[:, 0, 0] = (8 * torch.arange(n, device="cuda") % 1024 + 1024).float()
+    q[:, 0, 1] = 1
+    k[:, 0, 0] = 4096
+    k[32:n - 1:32, 0, 1] = 10
+    k[n - 1, 0, 1] = 12
+    v[n - 1] = 1
+    q, k, v = (torch.cat([x] * 20).to(dtype) for x in (q, k, v))
+    for s in range(20):  # another product for each of the last rows
+        q[(s + 1) * n - 1, 0, 0] = 1024 + 8 * s
+    starts = starts_of([n] * 20)
+    out = P.prompt_attention(q, k, v, i32(starts), out_dtype=torch.float32, scale=1.0)
+    ref, mag, _ = ref64.causal(q, k, v, starts, 1.0)
+    assert ((out.double() - ref).abs() <= (2.0 ** -8 + 2.0 ** -11) * mag + 2.0 ** -8 * ref.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("at", [0, 70, 129])
 @pytest.mark.parametrize("what", [float("inf"), -float("inf"), float("nan")])
 def test_what_is_not_seen_does_not_matter(P, dtype, at, what):
@@ -180,6 +202,12 @@ def test_bad_starts_are_reported(P):
         out = P.prompt_attention(q, k, v, i32(starts), dev_status=st)
         assert st.item() == 13, starts
         assert torch.equal(out[:50], good)
+    # fewer rows than sequences, the wrong one behind all of them
+    for dtype in (torch.bfloat16, torch.float32):
+        q, k, v = inputs([1], 2, 2, 64, dtype)
+        st = i32([0])
+        out = P.prompt_attention(q, k, v, i32([0] + [1] * 130 + [2]), dev_status=st)
+        assert st.item() == 13 and torch.equal(out, v)
 
 
 def test_same_results_again_and_alone(P):
