@@ -720,6 +720,8 @@ def _rows(t, heads=None):
     if t.dim() != 3 or (t.shape[0] and (t.stride(2) != 1 or
                                         (t.shape[1] > 1 and t.stride(1) != t.shape[2]))):
         raise ValueError("expected [N][heads][D] rows with dense heads")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1] * t.shape[2]:
+        raise ValueError("expected rows that do not overlap")
     return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 
@@ -827,9 +829,11 @@ class BlockKV:
         B, T, Hq, D = q.shape
         if page_table.shape[0] != B or kv_len.numel() != B or parent.shape != (B, T):
             raise ValueError("expected page_table [B][max_pages], kv_len [B], parent [B][T]")
-        od = out_dtype or (q.dtype if out is None else out.dtype)
         if out is None:
-            out = torch.empty((B, T, Hq, D), dtype=od, device=q.device)
+            out = torch.empty((B, T, Hq, D), dtype=out_dtype or q.dtype, device=q.device)
+        elif out.shape != q.shape or not out.is_contiguous():
+            raise ValueError("expected contiguous out of q's shape")
+        _need_here(out, workspace)
         shape = AttnShape(B, Hq, self.Hkv, D, page_table.shape[1] * self.page_size, _dtype_code(q),
                           _dtype_code(out), float(scale))
         nbytes = ptd_tree_attention_workspace_bytes(shape, T)

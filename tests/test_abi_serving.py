@@ -118,6 +118,11 @@ def test_helpers_refuse_what_the_calls_cannot_see():
         P.prompt_attention(x, x, x, torch.zeros(2, dtype=torch.int32))
     with pytest.raises(ValueError):
         P.BlockKV(4, 2, 64, 48, device="cpu")
+    wide = torch.zeros((4, 6, 64), dtype=torch.bfloat16)
+    assert P._rows(x) == 128 and P._rows(wide[:, 1:3]) == 384 and P._rows(x[:1]) == 128
+    for bad in (x[:1].expand(4, 2, 64), x.transpose(0, 1), wide[:, ::2], wide[..., ::2], x[0]):
+        with pytest.raises(ValueError):  # a stride of 0 would stand for dense rows
+            P._rows(bad)
     with pytest.raises(ValueError):
         P.BlockKV(4, 2, 32, 64, device="cpu")
     kv = P.BlockKV(4, 2, 64, 32, device="cpu")
