@@ -170,12 +170,13 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
       w = b0 + tid < B ? want_of(p, b0 + tid, nullptr) : none;
       at = block_scan<NT>(sums_of(w), s_scan, &t);
     }
-    s_back[tid] = static_cast<int>(at.back);
+    s_back[tid] = static_cast<int>(min(at.back, static_cast<long long>(0x7FFFFFFF)));
     s_need[tid] = w.need;
     __syncthreads();
     const int n = min(B - b0, NT);
+    const long long back = min(t.back, total);  // (held pages that make up more are not all moved)
 #pragma unroll 4
-    for (int j = tid; j < t.back; j += NT) {
+    for (int j = tid; j < back; j += NT) {
       const int x = upper(s_back, n, j);
       const long long to = count1 - 1 - (done + j);
       if (to >= count) p.s.free_pages[to] = table_of(p, b0 + x)[s_need[x] + (j - s_back[x])];

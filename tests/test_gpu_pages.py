@@ -373,3 +373,19 @@ def test_strided_rows_and_graph(P):
         torch.cuda.synchronize()
         for a, b in ((kv.k_pages, other.k_pages), (kv.v_pages, other.v_pages), (kv.scales, other.scales)):
             assert torch.equal(a, b)
+
+
+def test_pages_held_twice_are_reported(P):
+    # the free list takes no more than there are pages, and nothing behind it is written
+    t = P.PageTables(3, 64, 4, 8)
+    wide = torch.full((32,), -7, dtype=torch.int32, device="cuda")
+    wide[:8] = t.free_pages
+    t.free_pages = wide[:8]
+    t.page_table.fill_(5)
+    t.num_held.fill_(4)
+    t.num_free.fill_(1)
+    st = i32([0])
+    t.plan(i32([0, 0, 0]), i32([0, 0, 0]), 0, 0, st)
+    assert st.item() == 10 and t.num_free.item() == 8
+    assert wide[:8].tolist() == [7] + [5] * 7 and (wide[8:] == -7).all()
+    assert t.num_held.tolist() == [0, 0, 0]
