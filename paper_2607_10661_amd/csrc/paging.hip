@@ -22,9 +22,15 @@ struct PlanParams {
 };
 
 // Rows whose slots the planning workgroup writes itself; more take a launch of
-// their own, over the whole chip.
-constexpr int kPlanRows = 8192;
+// their own, over the whole chip.  (A plan and its release, 16 sequences: of 1024 rows 10.1 us
+// and with a launch 13.1, of 2048 12.2 and 13.3, of 4096 16.7 and 13.1.)
+constexpr int kPlanRows = 2048;
 constexpr int kPlanSmall = 256, kPlanLarge = 1024;  // threads
+// Pages of the new rows from which on the planning workgroup is a large one.  (Both calls
+// with 256 threads and with 1024: of 32 pages 13.2 and 15.2 us, of 1024 13.4 and 15.5, of
+// 2048 16.5 and 16.1, of 8192 45.8 and 23.3.  A call without rows, which
+// follows every step, stays small, whatever it releases.)
+constexpr int kPlanPages = 1536;
 
 // A sequence's lengths and pages, checked.  rows: new rows (0 where refused).
 struct Want {
@@ -123,9 +129,9 @@ __device__ __forceinline__ void put_rows(const PlanParams& p, const Starts& star
 
 // One workgroup: a thread per sequence (in rounds of the workgroup's size) counts pages, sums over
 // the workgroup give every sequence its places on the free list and in the rows,
-// then a thread per page moves ids.  256 threads, or 1024 where the call's rows are many
-// (64 prompts of 16-8192 rows, 4200 pages: 5 against 8.5 us).  Outputs depend on nothing but the inputs: no
-// atomics.  Bound by latency: with ONE round of sequences, the lengths are loaded
+// then a thread per page moves ids.  Outputs depend on nothing but the inputs: no
+// atomics.  Bound by latency (5 us for 16 sequences and 1024 rows, 8 for 64 prompts
+// and 4200 pages): with ONE round of sequences, the lengths are loaded
 // once, new rows take their page ids from where the tables get them, and a step of 16
 // sequences waits three times for memory: lengths, ids, stores.
 template <bool ONE, int NT>
@@ -625,7 +631,7 @@ extern "C" int ptd_page_plan(const ptd_page_state* state, const int32_t* kv_len,
   prm.N = N;
   prm.rows_per_seq = rows_per_seq;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool large = N > kPlanRows || state->B > kPlanSmall;
+  const bool large = (N >> prm.page_shift) > kPlanPages || state->B > kPlanSmall;
   if (!large) hipLaunchKernelGGL((k_page_plan<true, kPlanSmall>), dim3(1), dim3(kPlanSmall), 0, st, prm);
   else if (state->B <= kPlanLarge) hipLaunchKernelGGL((k_page_plan<true, kPlanLarge>), dim3(1), dim3(kPlanLarge), 0, st, prm);
   else hipLaunchKernelGGL((k_page_plan<false, kPlanLarge>), dim3(1), dim3(kPlanLarge), 0, st, prm);
