@@ -404,11 +404,16 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float(static_cas
 // m < 2, that is x - 8, or x - 7 where m > 1.75.  A power of two leaves the
 // codes' three mantissa bits untouched, so a live row is coded anew without
 // loss while it stays a normal number of the format.
+// Bound by HBM where the rows are many: prompts of 28000 rows in all, 8 heads, S = 64, 177 MB, take
+// 40 us, 4.4 TB/s (a large copy reaches 5.2); by latency at a step: slots, rows, scale,
+// codes one after the other, 7 us for 16 trees of 64 rows.
 template <typename T, int S, bool FROM>
 __global__ void __launch_bounds__(kWriteThreads, 2) k_kv_write(WriteParams p) {
   constexpr int R = S / 4;  // rows per lane
   // registers hold the block's rows (up to 64 registers of them), or 32 rows at a
-  // time that the second pass reads again
+  // time that the second pass reads again: beyond, waves per SIMD are worth more than one
+  // reading.  (8192 rows: 64 rows of bf16 held 12.3 us and not 13.9, 32 rows of fp32 17.1 and
+  // 20.4; 64 rows of fp32 43 and 28, 128 rows of bf16 29 and 16.)
   constexpr bool HOLD = R * sizeof(T) * 2 <= 64;
   constexpr int RH = HOLD ? R : 8;
   constexpr int RO = R <= 16 ? R : 8;  // the same for the codes of live rows

@@ -57,8 +57,9 @@ struct TileOf {
 
 // Tile number w of all sequences' tiles; false past the last one.  Up to 64 sequences:
 // longest tiles first (tile k of a sequence has k + 1 times the first one's keys), so that
-// the short ones fill in at the end; more: sequence by sequence, each one's
-// longest first.  Every lane of a wave takes part.
+// the short ones fill in at the end (3 prompts, 40 heads: 62 against 87 us in order); more:
+// sequence by sequence, each one's longest first, as levels would take a search over
+// several looks at the starts.  Every lane of a wave takes part.
 template <int TM>
 __device__ __forceinline__ bool find_tile(const PromptParams& p, uint32_t tile, TileOf& t) {
   long long w = tile;
@@ -179,6 +180,15 @@ __device__ __forceinline__ u32x2 lds_read_tr16(const unsigned char* p) {
 // lies at c ^ swz(r): for K, so that 16 rows x one chunk (a quarter of a ds_read_b128)
 // fall on 16 different places of 256 bytes; for V, so that 4 rows x 4 chunks (half of a
 // transposing read) do.
+//
+// Bound by the matrix units at the clock that they leave the card: 8192 rows of 32 / 8 heads
+// x 128 take 483-500 us, 1100-1140 TFLOP/s (a large matrix product reaches 1214; all-zero
+// inputs run at 1370).  Two workgroups of four waves per CU, so that one's softmax and
+// barriers run beside the other's products: 128 rows a workgroup.  256 rows and eight waves
+// took 623 against 585 us there, 32-key tiles and three waves per SIMD (registers
+// spill) 355 against 241 on 16 prompts of 17-2048 rows, four tiles in flight and one
+// workgroup per CU 30.9 against 27.3 on 1024 rows.  Short prompts wait for memory and
+// for find_tile: 1-64 rows take 6 us, launch included.
 constexpr int kThreads = 256;  // four waves of 32 rows
 template <int D>
 struct Tiles {
@@ -526,6 +536,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
 //   O^T = V^T P^T: step e contracts the keys 8 * (e / 4) + 4 h + e % 4, whose weights the
 //   lane owns; row r of part dt stands for column DT * r + dt, so that a lane's loads are
 //   DT consecutive elements, and so are its outputs.
+// Bound by the latency of a wave's tiles: four prompts of up to 513 rows, 4 / 2 heads x 64, take
+// 13 us, 6 TFLOP/s.
 constexpr int kF32Threads = 512;
 constexpr int kF32Waves = kF32Threads / PTD_WAVE;
 
