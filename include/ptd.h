@@ -446,7 +446,8 @@ typedef struct {
  *   q          [N][Hq][D], rows ldq apart;  k, v  [N][Hkv][D], rows ldk, ldv apart
  *   row_start  int32 [B + 1]: sequence b's rows are row_start[b] ..
  *              row_start[b + 1] - 1 (none: an empty prompt); ascending, in [0, N]
- *   out        [N][Hq][D]; rows outside the sequences are left as they were
+ *   out        [N][Hq][D]; rows outside the sequences are left as they were; overlaps
+ *              none of the inputs
  * What a row may not see does not reach it, infinities and NaN included.  bf16
  * inputs run on v_mfma_f32_32x32x16_bf16 with the softmax weights rounded to bf16
  * above and below the line (out within 2^-7 of the largest value it averages,
