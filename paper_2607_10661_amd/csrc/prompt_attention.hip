@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
 //   lane owns; row r of part dt stands for column DT * r + dt, so that a lane's loads are
 //   DT consecutive elements, and so are its outputs.
 // Bound by the latency of a wave's tiles: four prompts of up to 513 rows, 4 / 2 heads x 64, take
-// 13 us, 6 TFLOP/s.
+// 13 us; 2048 rows of 32 / 8 heads x 128 take 353 us, 97 TFLOP/s (a large fp32 product: 153).
 constexpr int kF32Threads = 512;
 constexpr int kF32Waves = kF32Threads / PTD_WAVE;
 
