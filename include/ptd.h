@@ -455,7 +455,7 @@ typedef struct {
  * v_mfma_f32_32x32x2_f32, fp32 throughout.  q, k, v and out must be
  * 16-byte aligned.  Outputs do not depend on the other sequences of the call.
  * dev_status: PTD_ERR_ROWS (a sequence whose start and end are not in order within
- * [0, N] is not computed).
+ * [0, N] is not computed; sequences that overlap others then may not be either).
  * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_DTYPE, PTD_ERR_ALIGN, PTD_ERR_HIP.
  * N = 0 does nothing.
  */
