@@ -318,7 +318,8 @@ typedef struct {
  * values likewise.  Codes and scale widen to bf16 exactly wherever the product
  * is a normal bf16 number.  The softmax weights are rounded to bf16 above and
  * below the line (out within 2^-7 of the largest value it averages, before its
- * own rounding; the bf16 path carries large weights with twice the bits, which a
+ * own rounding, given the scores, which are fp32 sums; |q . k| below 2^99; the bf16
+ * path carries large weights with twice the bits, which a
  * value known to 2^-4 does not need).  A tree of one node is the decoding step of a
  * single token; a chain of up to PTD_MAX_T nodes continues a prompt whose
  * beginning is cached.  The exponents are read as 4-byte words: the last one of

@@ -754,9 +754,12 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
                        fmaxf(fmaxf(x.s[1][qb][0], x.s[1][qb][1]), fmaxf(x.s[1][qb][2], x.s[1][qb][3])));
       mx = max_xor32(max_xor16(mx));
       const bool up = mx > m[qb];
-      const float alpha = up ? __builtin_amdgcn_exp2f((m[qb] - mx) * c) : 1.0f;  // 0 for the first keys
+      // (from the products as they were rounded, which the weights were formed with:
+      // the maxima's own difference is another factor, off by up to two at scores of 2^23)
+      const float to = up ? -mx * c : nmc[qb];
+      const float alpha = up ? __builtin_amdgcn_exp2f(to - nmc[qb]) : 1.0f;  // 0 for the first keys
       m[qb] = up ? mx : m[qb];
-      nmc[qb] = up ? -mx * c : nmc[qb];
+      nmc[qb] = to;
       ls[qb] *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[qb][dt] *= alpha;
@@ -1076,7 +1079,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
 
   // ---- epilogue.  The key groups of a row group hold their fragments in the
   //      same lane layout (lane: query column l16, d = 16*dt + 4*l4 + 0..3), so
-  //      the merge is lane-local: every wave parks its fragments and (m, l)
+  //      the merge is lane-local: every wave parks its fragments and (m c, l)
   //      per column in LDS, then wave (wr, kg) merges the key groups (fixed
   //      order) for d-tiles [kg*DPW, (kg+1)*DPW) of its row group and stores
   //      them.  With one key group the fragments are stored directly.
@@ -1111,7 +1114,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) store_tile(qb, dt, o[qb][dt], m[qb] * c, lsum[qb]);
+      for (int dt = 0; dt < DT; ++dt) store_tile(qb, dt, o[qb][dt], -nmc[qb], lsum[qb]);
   } else {
     f32x4* so = reinterpret_cast<f32x4*>(smem);  // [WR][WK][QB][DT][64]
     float2* sml = reinterpret_cast<float2*>(smem + PARK_O);  // [WR][WK][QB][64]
@@ -1119,14 +1122,14 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
     for (int qb = 0; qb < QB; ++qb) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) so[(((wr * WK + kg) * QB + qb) * DT + dt) * 64 + lane] = o[qb][dt];
-      sml[((wr * WK + kg) * QB + qb) * 64 + lane] = make_float2(m[qb], lsum[qb]);
+      sml[((wr * WK + kg) * QB + qb) * 64 + lane] = make_float2(-nmc[qb], lsum[qb]);
     }
     lds_barrier();
     if (!wave_stores) return;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      float mk[WK], w[WK];
-      float mm = kNegBig, den = 0.f;
+      float mk[WK], w[WK];  // references as rounded products, as in move_ref
+      float mm = -INFINITY, den = 0.f;
 #pragma unroll
       for (int k2 = 0; k2 < WK; ++k2) {
         mk[k2] = sml[((wr * WK + k2) * QB + qb) * 64 + lane].x;
@@ -1134,7 +1137,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
       }
 #pragma unroll
       for (int k2 = 0; k2 < WK; ++k2) {
-        w[k2] = __builtin_amdgcn_exp2f((mk[k2] - mm) * c);
+        w[k2] = __builtin_amdgcn_exp2f(mk[k2] - mm);
         den += w[k2] * sml[((wr * WK + k2) * QB + qb) * 64 + lane].y;
       }
 #pragma unroll
@@ -1143,7 +1146,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k2 = 0; k2 < WK; ++k2) acc += so[(((wr * WK + k2) * QB + qb) * DT + dt) * 64 + lane] * w[k2];
-        store_tile(qb, dt, acc, mm * c, den);
+        store_tile(qb, dt, acc, mm, den);
       }
     }
   }
