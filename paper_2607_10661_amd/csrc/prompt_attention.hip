@@ -290,7 +290,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[i][e] = 0.f;
-  float m = kNegBig, nmc = -kNegBig * p.c, l = 0.f;
+  // (finite at every scale: it stays where a row's first keys score -inf, and inf - inf is NaN)
+  float m = kNegBig, nmc = fminf(-kNegBig * p.c, -kNegBig), l = 0.f;
 
   // scores of 32 keys
   auto qk = [&](const unsigned char* slot, int kb) __attribute__((always_inline)) {

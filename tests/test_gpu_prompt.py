@@ -278,3 +278,18 @@ def test_many_heads_share_a_position(P, dtype):
     # a tile of rows is one position, so the last tile of keys can be seen whole
     check(P, [130, 64, 193], 128, 1, 64, dtype)
     check(P, [129], 96, 1, 128, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("scale", [0.0, 1.0, 40.0])
+@pytest.mark.parametrize("n0", [1, 40, 64, 130])
+def test_keys_that_weigh_nothing_come_first(P, dtype, scale, n0):
+    # scores of -inf before the first finite one: rows from there on are as if those keys were
+    # not there, at any scale
+    n, D = 300, 64
+    q, k, v = inputs([n], 4, 2, D, dtype, seed=n0)
+    q[..., 0] = 1
+    k[:n0, :, 0] = -float("inf")
+    out = P.prompt_attention(q, k, v, i32([0, n]), out_dtype=torch.float32, scale=scale)[n0:]
+    ref, mag, top = ref64.causal(q[n0:], k[n0:], v[n0:], [0, n - n0], scale or D ** -0.5)
+    assert ((out.double() - ref).abs() <= bound(ref, mag, top, n, D, dtype, torch.float32)).all()
