@@ -722,7 +722,7 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
     m[qb] = kNegBig;
-    nmc[qb] = -kNegBig * c;
+    nmc[qb] = fminf(-kNegBig * c, 3.0e38f);  // (finite at every scale: inf - inf is NaN)
     ls[qb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[qb][dt] = f32x4{0.f, 0.f, 0.f, 0.f};

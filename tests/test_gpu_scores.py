@@ -93,3 +93,20 @@ def test_large_scores(P, kind, B, T, Hq, Hkv, n):
     for b in range(B):
         ref, mag = ref64.tree(q[b], k[b], v[b], lens[b], parent[b], 1.0, T)
         assert ((out[b] - ref).abs() <= (2.0 ** -8 + 2.0 ** -11) * mag + 2.0 ** -8 * ref.abs()).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("B,T", [(1, 100), (2, 200)])
+def test_large_scale(P, kind, B, T):
+    # a scale of 2^29 on products of about 2^-29, and rows whose first keys are other branches'
+    Hq, Hkv, scale = 4, 2, 2.0 ** 29
+    L = (T + 63) // 64 * 64
+    g = torch.Generator("cuda").manual_seed(T)
+    q = (torch.randn((B, T, Hq, 128), generator=g, device="cuda") * 2.0 ** -34).bfloat16()
+    k = (torch.randint(-8, 9, (B, Hkv, L, 128), generator=g, device="cuda") * 2.0).bfloat16()
+    v = torch.randint(-8, 9, (B, Hkv, L, 128), generator=g, device="cuda").bfloat16()
+    parent = np.stack([W.tree_star(T)[0]] * B)
+    out = attend(P, kind, q, k, v, [0] * B, parent, scale).double()
+    for b in range(B):
+        ref, mag = ref64.tree(q[b], k[b], v[b], 0, parent[b], scale, T)
+        assert ((out[b] - ref).abs() <= (2.0 ** -8 + 2.0 ** -11) * mag + 2.0 ** -8 * ref.abs()).all()
