@@ -827,8 +827,12 @@ class BlockKV:
         _need_here(q, self.k_pages)
         _need_i32(page_table, kv_len, parent, tree_len, dev_status)
         B, T, Hq, D = q.shape
-        if page_table.shape[0] != B or kv_len.numel() != B or parent.shape != (B, T):
-            raise ValueError("expected page_table [B][max_pages], kv_len [B], parent [B][T]")
+        if page_table.dim() != 2 or page_table.shape[0] != B or kv_len.numel() != B \
+                or parent.shape != (B, T) or (tree_len is not None and tree_len.numel() != B):
+            raise ValueError("expected page_table [B][max_pages], kv_len and tree_len [B], "
+                             "parent [B][T]")
+        if workspace is not None and not workspace.is_contiguous():
+            raise ValueError("expected a contiguous workspace")
         if out is None:
             out = torch.empty((B, T, Hq, D), dtype=out_dtype or q.dtype, device=q.device)
         elif out.shape != q.shape or not out.is_contiguous():

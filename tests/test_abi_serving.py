@@ -131,3 +131,22 @@ def test_helpers_refuse_what_the_calls_cannot_see():
                  torch.zeros(4, dtype=torch.int32))
     with pytest.raises(ValueError):
         P.PageTables(2, 64, 4, 8, device="cpu")
+
+
+def test_block_attention_helper_counts_what_the_kernel_reads(monkeypatch):
+    # tensors on the host, as if they were on the GPU: a helper that lets one through reaches the call
+    monkeypatch.setattr(P, "_need_gpu", lambda *ts: None)
+    monkeypatch.setattr(P, "_need_here", lambda *ts: None)
+    monkeypatch.setattr(P, "ptd_tree_attention_paged_fp8blk", lambda *a: reached.append(a))
+    reached = []
+    kv = P.BlockKV(4, 2, 64, 32, device="cpu")
+    i32 = lambda *n: torch.zeros(n, dtype=torch.int32)
+    good = dict(q=torch.zeros((2, 8, 4, 128), dtype=torch.bfloat16), page_table=i32(2, 2), kv_len=i32(2), parent=i32(2, 8))
+    kv.tree_attention(**good, tree_len=i32(2))
+    assert len(reached) == 1
+    for bad in (dict(tree_len=i32(1)), dict(tree_len=i32(3)), dict(kv_len=i32(1)), dict(page_table=i32(4)),
+                dict(page_table=i32(1, 4)), dict(parent=i32(2, 7)), dict(parent=i32(16)),
+                dict(workspace=torch.zeros(1, dtype=torch.uint8).expand(1 << 24))):
+        with pytest.raises(ValueError):
+            kv.tree_attention(**dict(good, **bad))
+    assert len(reached) == 1
