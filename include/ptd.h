@@ -359,6 +359,16 @@ int ptd_tree_attention_paged_fp8blk(const void* q, const ptd_kv_pages_fp8blk* kv
  * row that is coded anew under a larger scale adds at most 2^-10 s.  Codes of dead
  * rows stay as they are.  Values beyond 448 * 2^119 and infinities saturate, a
  * NaN becomes 0; whatever is not finite is reported and does not enter s.
+ * What is written and not kept: tree rows take part in the scale of the block that
+ * holds the last committed rows.  A rejected row 2^n times as large as the others
+ * has these coded under a scale up to 2^n larger (2^-10 of it lost per element); the commit
+ * makes the scale small again, but what was lost stays lost, so committed rows then depend on
+ * what was rejected.  Rows of padding nodes are kept out by their slots (new_len =
+ * the tree's size in ptd_page_plan).  A program that wants committed rows free of all rejected ones
+ * keeps the rows of each sequence's last block as they were (fewer than scale_rows)
+ * and commits them anew with the accepted ones, from the block's first row on (src
+ * gathers both from one array, kv_len of the plan is the block's start): no
+ * row is live in that call, and the cache is that of a single write of the kept rows.
  * k_pages and v_pages 16-byte, scales 4-byte aligned; D must be 128.
  * dev_status: PTD_ERR_PAGE (a slot outside the pages: not written), PTD_ERR_ROWS
  * (slot order; src outside [0, rows_per_seq)), PTD_ERR_VALUE.

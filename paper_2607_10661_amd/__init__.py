@@ -809,7 +809,10 @@ class BlockKV:
 
     def write(self, k, v, slots, src=None, rows_per_seq: int = 0, dev_status=None):
         """Rows of k, v [N][Hkv][128] (bf16 or fp32) to the slots int32 [N] (any shape
-        of N elements); src: rows within each sequence's rows_per_seq."""
+        of N elements); src: rows within each sequence's rows_per_seq.  The rows of a
+        block in front of the first new one keep their values, coded under the block's new
+        scale: rejected tree rows can cost them places for good, unless a commit writes the
+        sequence's last block anew from its first row (ptd_kv_write_fp8blk)."""
         _need_here(k, v, self.k_pages)
         _need_i32(slots, src, dev_status)
         N = slots.numel()
