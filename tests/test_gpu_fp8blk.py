@@ -158,3 +158,34 @@ def test_graph(P):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, kv.tree_attention(q, table, n, par)) and st.item() == 0
+
+
+@pytest.mark.parametrize("B,T,Hq,Hkv,page,S,rows", [(1, 1, 8, 2, 64, 32, 3000), (16, 1, 8, 8, 128, 64, 700), (1, 64, 4, 2, 64, 64, 1500),
+                                                    (1, 64, 8, 2, 32, 32, 9000), (3, 64, 8, 2, 128, 128, 900), (2, 200, 8, 2, 64, 32, 1100)])
+def test_weights_that_need_no_rounding_give_the_bf16_outputs(P, B, T, Hq, Hkv, page, S, rows):
+    # scores that are whole numbers in the exponential's domain: the weights are powers of two, and
+    # nothing is left of what the two kernels do differently, bit for bit
+    g = torch.Generator("cuda").manual_seed(rows)
+    r = np.random.default_rng(rows)
+    per = -(-rows // page)
+    n = B * per + 2
+    kv = P.BlockKV(n, Hkv, page, S)
+    q = (torch.randint(-1, 2, (B, T, Hq, 128), generator=g, device="cuda") *
+         (torch.rand((B, T, Hq, 128), generator=g, device="cuda") < 0.1)).bfloat16()
+    for kind, x in enumerate((kv.k_pages, kv.v_pages)):
+        e = torch.randint(-2, 3, (n, Hkv, page // S), generator=g, device="cuda")
+        y = torch.randint(-7, 8, x.shape, generator=g, device="cuda") if kind == 0 else \
+            torch.randn(x.shape, generator=g, device="cuda")
+        y = y.unflatten(2, (-1, S)) * torch.exp2(-e.float())[..., None, None]
+        x.copy_(y.to(torch.float8_e4m3fn).view(torch.uint8).flatten(2, 3))
+        kv.scales[..., kind] = (127 + e).to(torch.uint8)
+    kp, vp = (decode(x, kv.scales[..., i], S).to(torch.bfloat16) for i, x in enumerate((kv.k_pages, kv.v_pages)))
+    table = i32(r.permutation(n)[:B * per].reshape(B, per))
+    lens = i32([rows - T - 5 * b for b in range(B)])
+    parent = i32(np.stack([W.tree_uniform(r, T)[0] for _ in range(B)]))
+    scale = float(np.float32(1) / np.float32(1.4426950408889634))  # times log2(e), in fp32: 1
+    assert np.float32(scale) * np.float32(1.4426950408889634) == 1
+    for od in (torch.float32, torch.bfloat16):
+        out = kv.tree_attention(q, table, lens, parent, out_dtype=od, scale=scale)
+        assert torch.equal(out, P.tree_attention_paged(q, kp, vp, table, lens, parent, out_dtype=od, scale=scale))
+        assert out.float().abs().amax() > 0.1
