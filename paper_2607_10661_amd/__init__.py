@@ -730,7 +730,8 @@ def prompt_attention(q, k, v, row_start, out=None, out_dtype=None, scale: float 
     """Causal attention over packed prompts: q [N][Hq][D], k, v [N][Hkv][D] (views of
     a wider projection are taken as they are), row_start int32 [B + 1].  Returns
     out [N][Hq][D]; rows outside the sequences are left as they are (a new out:
-    zero)."""
+    zero, which is a pass over it: 10 of 509 us for 8192 rows of 32 heads; an out that
+    is passed in spares it)."""
     _need_here(q, k, v)
     _need_i32(row_start, dev_status)
     N, Hq, D = q.shape

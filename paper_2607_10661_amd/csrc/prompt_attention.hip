@@ -57,9 +57,14 @@ struct TileOf {
 
 // Tile number w of all sequences' tiles; false past the last one.  Up to 64 sequences:
 // longest tiles first (tile k of a sequence has k + 1 times the first one's keys), so that
-// the short ones fill in at the end (3 prompts, 40 heads: 62 against 87 us in order); more:
-// sequence by sequence, each one's longest first, as levels would take a search over
-// several looks at the starts.  Every lane of a wave takes part.
+// the short ones fill in at the end; more: sequence by sequence, each one's longest first,
+// as levels would take a search over several looks at the starts.  (Time in order over time
+// longest first, five head layouts x four mixtures of lengths: 1.01-1.05 on average for 2
+// to 32 prompts, at worst 0.88 and 1.23; 0.97 for 48 and 0.93 for 64, whose keys stay in
+// the L2 in order, but up to 1.31 where the longest comes last.  3 prompts of 462-1498
+// rows, 40 heads: 47 against 52 us in order.)  A tile of sequence b is found after b / 64
+// dependent looks at the starts, which is most of the time of thousands of short prompts
+// (1024 of one row 157 us, 8192 of them 5.9 ms).  Every lane of a wave takes part.
 template <int TM>
 __device__ __forceinline__ bool find_tile(const PromptParams& p, uint32_t tile, TileOf& t) {
   long long w = tile;
@@ -181,9 +186,16 @@ __device__ __forceinline__ u32x2 lds_read_tr16(const unsigned char* p) {
 // fall on 16 different places of 256 bytes; for V, so that 4 rows x 4 chunks (half of a
 // transposing read) do.
 //
+// The weights are rounded to bf16 as the operand of O^T (two operands, the number and what
+// its rounding leaves, would be half as many products again), and their sum is that of the
+// rounded ones, in fp32, so that the output is an exact average under weights off by at most
+// 2^-8 of themselves: bf16 outputs over up to 8192 keys are off by 0.0020 of their size
+// (their own rounding makes 0.0015 of it).
+//
 // Bound by the matrix units at the clock that they leave the card: 8192 rows of 32 / 8 heads
-// x 128 take 483-500 us, 1100-1140 TFLOP/s (a large matrix product reaches 1214; all-zero
-// inputs run at 1370).  Two workgroups of four waves per CU, so that one's softmax and
+// x 128 take 483-504 us, 1090-1140 TFLOP/s (a large matrix product reaches 1214; all-zero
+// inputs run at 1370); the clock settles after some 100 such calls, the first ones of an idle
+// card take 515 to 666.  Two workgroups of four waves per CU, so that one's softmax and
 // barriers run beside the other's products: 128 rows a workgroup.  256 rows and eight waves
 // took 623 against 585 us there, 32-key tiles and three waves per SIMD (registers
 // spill) 355 against 241 on 16 prompts of 17-2048 rows, four tiles in flight and one

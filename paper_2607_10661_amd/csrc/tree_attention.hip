@@ -1544,6 +1544,12 @@ bool make_plan(const ptd_attn_shape* s, int T, Plan* pl) {
       //    there on up to 1.12).
       // Longer splits carry fewer of a row's keys as hi + lo; half the threshold keeps
       // the error no larger (over drawn batches 0.975 of it on average, 1.009 at most).
+      // Block-scaled pages go by the same counts, measured on bf16 pages, with half the
+      // bytes per key (and no hi + lo).  Over 60 drawn calls, inputs in the caches, a call
+      // takes 1.00 (one sequence), 1.08 (single tokens) and 1.12 (trees) of the time of
+      // the count that is best for it, at worst 1.1, 1.5 and 1.45: fewer would do for 2
+      // long single tokens (2 x 18020 keys, 64 / 32 splits: 29 / 19 us) and for short
+      // trees (14 x 64 nodes x 241 keys, two / one: 34 / 25 us).
       const int even = splits_for(2 * kTargetBlocks);
       const long long keys = (s->L_cap + even - 1LL) / even;
       const bool one_split = even == 1 && keys <= 544 && items >= 384;
