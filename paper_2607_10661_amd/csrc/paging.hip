@@ -26,12 +26,13 @@ struct PlanParams {
 // and with a launch 13.1, of 2048 12.2 and 13.3, of 4096 16.7 and 13.1.)
 constexpr int kPlanRows = 2048;
 constexpr int kPlanSmall = 256, kPlanLarge = 1024;  // threads
-// Pages of the new rows from which on the planning workgroup is a large one.  (Both calls
-// with 256 threads and with 1024: of 32 pages 13.2 and 15.2 us, of 1024 13.4 and 15.5, of
-// 2048 16.5 and 16.1, of 8192 45.8 and 23.3.)  A call without rows (N = 0) is a small one
-// whatever it gives back, which the host does not know: it follows every step, where it
-// moves a page or two per sequence and takes 1.1 to 1.7 us less than with 1024 threads.  Finished
-// sequences give back 2500 pages in equal time, 4063 in 4 us more, 6897 in 12, 16384 in 24.
+// Pages of the new rows from which on the planning workgroup is a large one.  (A plan and
+// the release of its pages by a call without rows, both with 256 threads and with 1024: of 32
+// pages 12.2 and 12.5 us, of 1024 13.5 and 15.0, of 2048 16.9 and 16.0, of 8192 39.2 and
+// 22.0.)  A call without rows (N = 0) is a small one whatever it gives back, which the host
+// does not know: it follows every step, where it moves a page or two per sequence, up to 1.2 us
+// shorter than with 1024 threads.  Finished sequences give back about 1500 pages in equal
+// time, 4063 in 4 us more, 6897 in 12, 16384 in 25.
 constexpr int kPlanPages = 1536;
 
 // A sequence's lengths and pages, checked.  rows: new rows (0 where refused).
@@ -109,10 +110,12 @@ __device__ __forceinline__ const int32_t* table_of(const PlanParams& p, int b) {
 }
 
 // Rows [i0, i1) by `step` when the tables are written.  starts: of packed rows, in LDS
-// where they fit, else in memory.
+// where they fit, else in memory.  (Rows and pages are counted without a sign: up to 2^31
+// of either, a step past the last one does not wrap.)
 template <typename Starts>
 __device__ __forceinline__ void put_rows(const PlanParams& p, const Starts& starts, int i0, int i1, int step) {
-  for (int i = i0; i < i1; i += step) {
+  for (uint32_t u = i0; u < static_cast<uint32_t>(i1); u += step) {
+    const int i = static_cast<int>(u);
     int b, r;
     if (p.rows_per_seq > 0) {
       b = i / p.rows_per_seq;
@@ -184,7 +187,8 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
     const int n = min(B - b0, NT);
     const long long back = min(t.back, total);  // (held pages that make up more are not all moved)
 #pragma unroll 4
-    for (int j = tid; j < back; j += NT) {
+    for (uint32_t u = tid; u < back; u += NT) {
+      const int j = static_cast<int>(u);
       const int x = upper(s_back, n, j);
       const long long to = count1 - 1 - (done + j);
       if (to >= count) p.s.free_pages[to] = table_of(p, b0 + x)[s_need[x] + (j - s_back[x])];
@@ -225,7 +229,8 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
     const int n = min(B - b0, NT);
     const long long room = min(t.grow, static_cast<long long>(count1) - taken);
 #pragma unroll 4
-    for (int j = tid; j < room; j += NT) {
+    for (uint32_t u = tid; u < room; u += NT) {
+      const int j = static_cast<int>(u);
       const int x = upper(s_off, n, j);
       const int k = j - s_off[x];
       if (k < s_grow[x])

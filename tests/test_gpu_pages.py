@@ -389,3 +389,14 @@ def test_pages_held_twice_are_reported(P):
     assert st.item() == 10 and t.num_free.item() == 8
     assert wide[:8].tolist() == [7] + [5] * 7 and (wide[8:] == -7).all()
     assert t.num_held.tolist() == [0, 0, 0]
+
+
+def test_as_many_rows_as_there_can_be(P):
+    # 2^31 - 1 rows of slots: the last workgroup's next row would be past 32 bits
+    t = P.PageTables(2, 64, 4, 8)
+    N = 2 ** 31 - 1
+    slots, start, st = torch.full((N,), 7, dtype=torch.int32, device="cuda"), i32([0, 0, 0]), i32([0])
+    P.ptd_page_plan(t.state(), i32([0, 0]), i32([70, 3]), N, 0, start, slots, None, st)
+    assert st.item() == 0 and start.tolist() == [0, 70, 73]
+    assert slots[:74].tolist() == list(range(70)) + [128, 129, 130, -1]
+    assert slots[74:].amax().item() == -1 and slots[74:].amin().item() == -1
