@@ -35,3 +35,16 @@ def test_no_register_load_without_its_wait():
                 found.append((os.path.basename(path), body.strip()[:60]))
     assert len(SOURCES) >= 8 and seen >= 8
     assert not found
+
+
+def test_committed_counters_are_of_the_present_kernel():
+    # bench.py leaves out counters that were taken on another tree_attention.hip
+    import hashlib
+    import json
+
+    path = os.path.join(ROOT, "paper_2607_10661_amd", "csrc", "tree_attention.hip")
+    now = hashlib.sha256(open(path, "rb").read()).hexdigest()[:16]
+    files = glob.glob(os.path.join(ROOT, "profiles", "*_tree_attention_*.json"))
+    assert len(files) == 8
+    for f in files:
+        assert json.load(open(f))["kernel_source_sha"] == now, f"{os.path.basename(f)}: collect it again"
