@@ -339,14 +339,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
   // moves to the row's maximum (always at its first keys), whatever the other rows do.
   auto settle = [&](const f32x16& s, Weights& r, uint64_t over) __attribute__((always_inline)) {
     if (over) {
+#pragma clang fp contract(off)
       const bool mine = ((static_cast<uint32_t>(over) | static_cast<uint32_t>(over >> 32)) >> l32) & 1u;
       float mx = s[0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
       mx = max_xor32(mx);
       const bool up = mine && mx > m;
-      // (from the products as they were rounded, which for large scores is off by more
-      // than the weights' own steps)
+      // (from the products as they were rounded, hence no contraction here: for large
+      // scores the rounding is more than the weights' own steps)
       const float to = up ? -mx * p.c : nmc;
       const float alpha = __builtin_amdgcn_exp2f(to - nmc);
       m = up ? mx : m;

@@ -748,18 +748,19 @@ __global__ void __launch_bounds__(NT, kThreads / NT) k_attn_mfma(AttnParams p) {
   // of 1 where the reference stays): rescaling accumulators under a per-lane
   // branch returned wrong row sums in some builds.
   auto move_ref = [&](const Tile& x) __attribute__((always_inline)) {
+#pragma clang fp contract(off)
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       float mx = fmaxf(fmaxf(fmaxf(x.s[0][qb][0], x.s[0][qb][1]), fmaxf(x.s[0][qb][2], x.s[0][qb][3])),
                        fmaxf(fmaxf(x.s[1][qb][0], x.s[1][qb][1]), fmaxf(x.s[1][qb][2], x.s[1][qb][3])));
       mx = max_xor32(max_xor16(mx));
       const bool up = mx > m[qb];
-      // (from the products as they were rounded, which the weights were formed with:
-      // the maxima's own difference is another factor, off by up to two at scores of 2^23)
-      const float to = up ? -mx * c : nmc[qb];
-      const float alpha = up ? __builtin_amdgcn_exp2f(to - nmc[qb]) : 1.0f;  // 0 for the first keys
+      // (from the products as they were rounded, which the weights were formed with --
+      // hence no contraction here: the maxima's own difference is another factor, off by
+      // up to two at scores of 2^23)
+      const float alpha = up ? __builtin_amdgcn_exp2f(-mx * c - nmc[qb]) : 1.0f;  // 0 for the first keys
       m[qb] = up ? mx : m[qb];
-      nmc[qb] = to;
+      nmc[qb] = up ? -mx * c : nmc[qb];
       ls[qb] *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[qb][dt] *= alpha;
