@@ -192,10 +192,12 @@ __device__ __forceinline__ u32x2 lds_read_tr16(const unsigned char* p) {
 // 2^-8 of themselves: bf16 outputs over up to 8192 keys are off by 0.0020 of their size
 // (their own rounding makes 0.0015 of it).
 //
-// Bound by the matrix units at the clock that they leave the card: 8192 rows of 32 / 8 heads
-// x 128 take 483-504 us, 1090-1140 TFLOP/s (a large matrix product reaches 1214; all-zero
-// inputs run at 1370); the clock settles after some 100 such calls, the first ones of an idle
-// card take 515 to 666.  Two workgroups of four waves per CU, so that one's softmax and
+// Bound, where prompts are long, by what two waves per SIMD issue at the clock that the
+// products leave the card (about 1.9 GHz): 8192 rows of 32 / 8 heads x 128 take 484-504 us,
+// 1090-1140 TFLOP/s, with the matrix units busy for 57 % of the cycles (a large matrix product
+// reaches 1214 TFLOP/s, all-zero inputs run at 1370); a batch of 17-2048 rows, 36 %, waits
+// more.  The clock settles after some 100 such calls; the first ones of an idle card take
+// 515 to 666 us.  Two workgroups of four waves per CU, so that one's softmax and
 // barriers run beside the other's products: 128 rows a workgroup.  256 rows and eight waves
 // took 623 against 585 us there, 32-key tiles and three waves per SIMD (registers
 // spill) 355 against 241 on 16 prompts of 17-2048 rows, four tiles in flight and one
