@@ -318,7 +318,8 @@ typedef struct {
  * values likewise.  Codes and scale widen to bf16 exactly wherever the product
  * is a normal bf16 number.  The softmax weights are rounded to bf16 above and
  * below the line (out within 2^-7 of the largest value it averages, before its
- * own rounding, given the scores, which are fp32 sums; |q . k| below 2^99; the bf16
+ * own rounding, given the scores, which are fp32 sums; |q . k| below 2^99, values
+ * below 2^90, as the sums of weights before they are divided reach 2^35; the bf16
  * path carries large weights with twice the bits, which a
  * value known to 2^-4 does not need).  A tree of one node is the decoding step of a
  * single token; a chain of up to PTD_MAX_T nodes continues a prompt whose
@@ -462,7 +463,8 @@ typedef struct {
  * What a row may not see does not reach it, infinities and NaN included.  bf16
  * inputs run on v_mfma_f32_32x32x16_bf16 with the softmax weights rounded to bf16
  * above and below the line (out within 2^-7 of the largest value it averages,
- * before its own rounding; scores |scale * q . k| below 2^30); fp32 inputs on
+ * before its own rounding; scores |scale * q . k| below 2^30, values below 2^90 as the
+ * sums of weights before they are divided reach 2^35); fp32 inputs on
  * v_mfma_f32_32x32x2_f32, fp32 throughout.  q, k, v and out must be
  * 16-byte aligned.  Outputs do not depend on the other sequences of the call.
  * dev_status: PTD_ERR_ROWS (a sequence whose start and end are not in order within
