@@ -552,8 +552,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_prompt_bf16(PromptParams p) {
 //   O^T = V^T P^T: step e contracts the keys 8 * (e / 4) + 4 h + e % 4, whose weights the
 //   lane owns; row r of part dt stands for column DT * r + dt, so that a lane's loads are
 //   DT consecutive elements, and so are its outputs.
-// Bound by the latency of a wave's tiles: four prompts of up to 513 rows, 4 / 2 heads x 64, take
-// 13 us; 2048 rows of 32 / 8 heads x 128 take 353 us, 97 TFLOP/s (a large fp32 product: 153).
+// Short prompts make too few workgroups: four prompts of 58-370 rows, 4 / 2 heads x 64, take
+// 13 us with 80 of them on 256 CUs, of which the longest's 12 tiles are 5 us of products on
+// its four SIMDs, the rest waits for memory.  2048 rows of 32 / 8 heads x 128 take 353 us, 97
+// TFLOP/s (a large fp32 product: 153).
 constexpr int kF32Threads = 512;
 constexpr int kF32Waves = kF32Threads / PTD_WAVE;
 
