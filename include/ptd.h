@@ -17,6 +17,12 @@
  *                        fills the caches before the first step)
  *   ptd_page_plan        page tables and slot maps from the sequences' lengths
  *   ptd_kv_write_fp8blk  key/value rows into 8-bit pages (block scales)
+ *   ptd_qk_norm_rope     norms of query and key heads, rotation by position, rows
+ *                        into the caches
+ *   ptd_page_plan_shared, ptd_page_fork, ptd_page_compact, ptd_page_copy
+ *                        pages that several sequences hold: samples of one prompt,
+ *                        beams, and moving pages
+ *   ptd_token_logprobs   log probabilities of tokens, entropy, likeliest tokens
  *   ptd_topk_argmax      per-row argmax / top-k of the verification logits
  *   ptd_verify           greedy longest accepted path (+ bonus token)
  *   ptd_expand           progressive expansion with top-k children
@@ -84,7 +90,8 @@ typedef enum {
   PTD_ERR_ROWS = 13,     /* device-detected: row starts not ascending within [0, N], more
                             rows than there is room for, a source row or slot order that
                             the call does not allow */
-  PTD_ERR_VALUE = 14     /* device-detected: a key or value that is not finite */
+  PTD_ERR_VALUE = 14     /* device-detected: a key or value that is not finite; a token
+                            outside the vocabulary */
 } ptd_status;
 
 /* Dimension pairs turned together by the rotary embedding. */
@@ -437,6 +444,158 @@ int ptd_page_plan(const ptd_page_state* state, const int32_t* kv_len, const int3
                   int32_t N, int32_t rows_per_seq, int32_t* row_start, int32_t* slots,
                   int32_t* positions, int32_t* dev_status, void* stream);
 
+/* Rows of queries, keys and values (host struct, read during the call only). */
+typedef struct {
+  int32_t N;              /* rows */
+  int32_t Hq, Hkv;        /* heads; one of them may be 0 */
+  int32_t D;              /* head dim: 64 or 128 */
+  int32_t rot_dim;        /* leading dimensions that are turned: a multiple of 16, 0 .. D */
+  int32_t pairing;        /* a ptd_rope_pairing, of the rot_dim dimensions */
+  int32_t norm;           /* 1: heads are normed; 0: turned only */
+  ptd_dtype dtype;        /* of the rows, outputs and pages */
+  ptd_dtype w_dtype;      /* of the weights */
+  int64_t ldq, ldk, ldv;  /* elements from one row to the next: at least heads * D and a
+                             multiple of 16 bytes; 0 selects heads * D */
+  int64_t ldqo, ldko;     /* likewise of q_out and k_out */
+  double eps;             /* >= 0; not used without the norm */
+  double theta;           /* base of the default frequencies theta^(-2p/rot_dim) */
+} ptd_qk_shape;
+
+/*
+ * Places of key and value rows (host struct, read during the call only): pages as in
+ * ptd_kv_pages, or contiguous caches [B][Hkv][L_cap][D], which are B pages of L_cap rows.
+ */
+typedef struct {
+  void* k_pages;       /* [num_pages][Hkv][page_size][D] of dtype */
+  void* v_pages;       /* likewise */
+  int32_t page_size;   /* >= 1; num_pages * page_size < 2^31 */
+  int32_t num_pages;
+} ptd_kv_store;
+
+/*
+ * ptd_qk_norm_rope -- what stands between the projections and the attention: the root
+ * mean square norm of every query and key head, the rotary embedding (ptd_tree_rope) at the
+ * rows' positions, and the rows into the caches.  For head x of row i:
+ *   y = x * weight / sqrt(mean(x^2) + eps)          (norm 0: y = x)
+ *   pairs p < rot_dim / 2 of y turned by positions[i] * inv_freq[p]; dimensions from
+ *   rot_dim on stay
+ *   q, k, v    [N][heads][D], rows ldq, ldk, ldv apart; v is not changed, and NULL
+ *              without store
+ *   q_weight, k_weight  [D] of w_dtype, or NULL for ones; both NULL with norm 0
+ *   positions  int32 [N] (as ptd_page_plan or ptd_tree_rope writes them); a row at -1 (any
+ *              negative one) is not read, and none of its outputs is written.  NULL with
+ *              rot_dim 0: every row is there
+ *   slots      int32 [N]: row i of k_out and v also goes to page slots[i] / page_size,
+ *              row slots[i] % page_size of it, -1: nowhere.  NULL without store.  Two rows
+ *              with one slot leave either
+ *   q_out, k_out  [N][heads][D]; may be q and k themselves with the same row stride, else they
+ *              overlap no input.  k_out may be NULL with store
+ *   store      host struct, or NULL: no caches
+ *   inv_freq   HOST double [rot_dim/2], at most 2^20 each, or NULL for those of theta
+ * Sums, norm and rotation are fp32, angles and their sine and cosine fp64 (rounded to
+ * fp32); each output is rounded once, to nearest even.  Heads whose sum of squares leaves fp32's range
+ * (elements beyond 2^60), infinities and NaN give no numbers in their own head only.
+ * Data and weights 16-byte aligned.
+ * dev_status: PTD_ERR_PAGE (a slot that is neither -1 nor in the pages: not stored).
+ * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_DTYPE, PTD_ERR_ALIGN, PTD_ERR_HIP.
+ * N = 0 does nothing.
+ */
+int ptd_qk_norm_rope(const void* q, const void* k, const void* v, const void* q_weight,
+                     const void* k_weight, const int32_t* positions, const int32_t* slots,
+                     void* q_out, void* k_out, const ptd_kv_store* store,
+                     const ptd_qk_shape* shape, const double* inv_freq, int32_t* dev_status,
+                     void* stream);
+
+/*
+ * Pages that several sequences hold.  refs int32 [num_pages], zero at ptd_page_init, counts the
+ * sequences that hold each page (0: it is free).  A state with refs is changed by the three
+ * calls below only; ptd_page_plan does not know of them.
+ *
+ * ptd_page_plan_shared -- ptd_page_plan on such a state.  A page that a sequence gives up
+ * goes back to the free list only when no sequence is left that holds it, in the place of the
+ * lowest sequence of the call that gave it up; the list's order is otherwise that of ptd_page_plan.  A
+ * new row never goes to a page that another sequence holds too: its slot is -1 and
+ * PTD_ERR_PAGE is reported (a sequence that was cut back into shared rows: ptd_page_fork with
+ * from[b] = b gives it a page of its own).  Other arguments, dev_status and errors as
+ * ptd_page_plan; PTD_ERR_PAGE too where a held page's count is not positive.
+ */
+int ptd_page_plan_shared(const ptd_page_state* state, int32_t* refs, const int32_t* kv_len,
+                         const int32_t* new_len, int32_t N, int32_t rows_per_seq,
+                         int32_t* row_start, int32_t* slots, int32_t* positions,
+                         int32_t* dev_status, void* stream);
+
+/*
+ * ptd_page_fork -- every sequence goes on from a sequence's rows: samples begin from a prompt,
+ * beams continue beams, sequences stay (from[b] = b), are cut back, or end (from[b] = -1).
+ *   from, len   int32 [B]: in the next tables sequence b holds the first len[b] rows of what
+ *               sequence from[b] holds now; len[b] <= page_size * num_held[from[b]]; from
+ *               -1: nothing (len not read)
+ *   table_next, held_next  int32 [B][max_pages], [B]: the next page_table and num_held (not
+ *               the state's own; a sequence's pages first, the entries behind them left as they were)
+ *   copy_src, copy_dst, copy_rows  int32 [B]: see below; -1, -1, 0 where sequence b needs no copy
+ * Whole pages are shared.  A page that sequence b fills in part stays its own if no sequence
+ * holds it as a whole one and b is the lowest that goes on in it; otherwise b gets a page from
+ * the free list's end, in the order of b, and rows 0 .. copy_rows[b] - 1 of page
+ * copy_src[b] have to be copied to page copy_dst[b] (ptd_page_copy; a program's next kernel on
+ * the stream may be the copy, as no page is both).  So the next row of every sequence goes to a page
+ * of its own.  Pages that nobody holds any more go to the list's end, the highest id first.
+ * The next tables then stand for the state with free_pages, num_free and refs, which are
+ * changed in place; the old tables are spent.  All or nothing: after a device-reported
+ * error the next tables are the old ones and nothing else has changed.
+ * dev_status: PTD_ERR_ROWS (from outside [-1, B)), PTD_ERR_KV_LEN (len), PTD_ERR_NO_PAGES,
+ * PTD_ERR_PAGE (num_held, num_free or a page id out of range).
+ * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_HIP.
+ */
+int ptd_page_fork(const ptd_page_state* state, int32_t* refs, const int32_t* from,
+                  const int32_t* len, int32_t* table_next, int32_t* held_next,
+                  int32_t* copy_src, int32_t* copy_dst, int32_t* copy_rows,
+                  int32_t* dev_status, void* stream);
+
+/*
+ * ptd_page_compact -- the pages that are held get the lowest ids: with L of them, the k-th free
+ * id below L takes the k-th held page from L on.  Tables, refs and the free list (L is taken next, then
+ * L + 1, ...) are changed in place.
+ *   move_src, move_dst  int32 [num_pages / 2]: the moves, ascending, then -1 (the data follows
+ *               by ptd_page_copy: no page is source and destination)
+ * Pages that no sequence holds are free afterwards, whether they were on the list or not.
+ * dev_status: PTD_ERR_PAGE (num_held or a page id out of range: left as they are; a negative count: 0).
+ * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_HIP.
+ */
+int ptd_page_compact(const ptd_page_state* state, int32_t* refs, int32_t* move_src,
+                     int32_t* move_dst, int32_t* dev_status, void* stream);
+
+/*
+ * One array of a cache's pages (host struct, read during the call only): page p is heads x
+ * units x unit_bytes bytes from base + p * that size on.  Keys or values: units = page_size,
+ * unit_rows = 1, unit_bytes = D * size of an element; scales of ptd_kv_pages_fp8blk:
+ * units = page_size / scale_rows, unit_rows = scale_rows, unit_bytes = 2.
+ */
+typedef struct {
+  void* base;
+  int32_t heads;
+  int32_t units;       /* per head of a page */
+  int32_t unit_rows;   /* rows that a unit stands for */
+  int32_t unit_bytes;
+} ptd_page_array;
+
+/*
+ * ptd_page_copy -- pages' data to other pages, in any number of arrays (all layers' keys,
+ * values and scales in one call).
+ *   arrays     HOST [num_arrays]; a page of each is below 2^31 bytes
+ *   src, dst   int32 [n]: page src[i] is copied to page dst[i]; nothing where either is -1 or
+ *              both are equal
+ *   rows       int32 [n] or NULL: only the first rows[i] rows (whole units of them), the
+ *              destination's others stay.  NULL: whole pages
+ * A page that is a destination is neither a source nor another's destination in the same call.
+ * Bytes are moved as they are.  Any alignment (16-byte units are the fast ones).
+ * dev_status: PTD_ERR_PAGE (an id outside [0, num_pages)), PTD_ERR_ROWS (rows outside the page):
+ * that pair is not copied.
+ * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_HIP.  n = 0 or num_arrays = 0 does nothing.
+ */
+int ptd_page_copy(const ptd_page_array* arrays, int32_t num_arrays, int32_t num_pages,
+                  int32_t n, const int32_t* src, const int32_t* dst, const int32_t* rows,
+                  int32_t* dev_status, void* stream);
+
 /* Packed prompts (host struct, read during the call only). */
 typedef struct {
   int32_t B;           /* sequences, 1 .. 65536 */
@@ -507,6 +666,48 @@ int ptd_topk_argmax(const void* logits, ptd_dtype dtype, int32_t R, int32_t V,
                     int64_t ld, int32_t k, int32_t* argmax, int32_t* topk_idx,
                     float* topk_val, void* workspace, size_t workspace_bytes,
                     void* stream);
+
+/*
+ * Workspace bytes ptd_token_logprobs needs (0: none, or invalid arguments).  It needs no
+ * initialisation; calls sharing one must not overlap.
+ */
+size_t ptd_token_logprobs_workspace_bytes(int32_t R, int32_t V, int32_t k);
+
+/*
+ * ptd_token_logprobs -- log probabilities of given tokens under softmax(row / temperature),
+ * entropy and the likeliest tokens with their log probabilities.
+ *   logits      rows of V entries of dtype, ld elements apart, finite or -inf (masked entries:
+ *               probability 0)
+ *   R           entries of tokens and the outputs, >= 1
+ *   V           1 .. 262144;  ld >= V
+ *   tokens      int32 [R] or NULL: entry r's token.  -1: the entry stands for nothing, its
+ *               row is not read, and its outputs are 0, 0, -1 (indices) and 0.  NULL: no
+ *               logprob, every entry stands for its row
+ *   nodes, T    NULL: entry r reads row r.  int32 [R / (T + 1)][T] (accept_nodes of
+ *               ptd_verify, tokens being its out_tokens): entry b * (T + 1) + j reads the row that
+ *               emitted token j, b * (T + 1) for j = 0, else b * (T + 1) + nodes[b][j - 1] + 1
+ *   temperature 1e-30 .. 1e30
+ *   k           0 .. PTD_MAX_K, k <= V; 0 with topk_idx and topk_logprob NULL
+ *   logprob     float [R] or NULL (-inf for a masked token)
+ *   entropy     float [R] or NULL, in nats: -sum p log p
+ *   topk_idx    int32 [R][k] or NULL, in the order of ptd_topk_argmax
+ *   topk_logprob  float [R][k] or NULL
+ *   workspace   >= ptd_token_logprobs_workspace_bytes(R, V, k), 8-byte aligned
+ * At least one output.  A row whose entries are all -inf has no distribution: log
+ * probabilities -inf, entropy 0, indices in order.  With a NaN or +inf in a row its own values are
+ * NaN or unspecified.  Terms are fp32, sums fp64; what is left beside the row's largest
+ * entries is summed apart, so log probabilities and entropies next to 0 keep their relative
+ * precision.
+ * dev_status: PTD_ERR_VALUE (a token outside [-1, V)), PTD_ERR_ROWS (a node outside [0, T) on a
+ * path): that entry stands for nothing.
+ * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_DTYPE, PTD_ERR_ALIGN, PTD_ERR_WORKSPACE,
+ * PTD_ERR_HIP.
+ */
+int ptd_token_logprobs(const void* logits, ptd_dtype dtype, int32_t R, int32_t V, int64_t ld,
+                       const int32_t* tokens, const int32_t* nodes, int32_t T,
+                       double temperature, int32_t k, float* logprob, float* entropy,
+                       int32_t* topk_idx, float* topk_logprob, void* workspace,
+                       size_t workspace_bytes, int32_t* dev_status, void* stream);
 
 /*
  * ptd_verify -- greedy verification (Sec. 3.2; Alg. 1 steps 5-6).  The edge

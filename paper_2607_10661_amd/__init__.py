@@ -10,9 +10,9 @@ device memory and the stream.  There is no CPU fallback: without a built
 
 The lower-case helpers (``tree_mask``, ``tree_attention``, ``topk_argmax``,
 ``verify``, ``expand``, ``verify_expand``, ``tree_rope``, ``kv_commit``,
-``verify_sample``, ``step_prune``, ``prompt_attention``, the ``Pool``,
-``PageTables`` and ``BlockKV`` classes) allocate outputs with torch and call the
-entry points.
+``verify_sample``, ``step_prune``, ``prompt_attention``, ``qk_norm_rope``,
+``token_logprobs``, ``page_copy``, the ``Pool``, ``PageTables`` and ``BlockKV`` classes)
+allocate outputs with torch and call the entry points.
 """
 from __future__ import annotations
 
@@ -82,6 +82,28 @@ class PromptShape(ctypes.Structure):
                 ("out_dtype", ctypes.c_int), ("scale", ctypes.c_float)]
 
 
+class QKShape(ctypes.Structure):
+    """ptd_qk_shape"""
+    _fields_ = [("N", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("pairing", ctypes.c_int32),
+                ("norm", ctypes.c_int32), ("dtype", ctypes.c_int), ("w_dtype", ctypes.c_int),
+                ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64),
+                ("ldqo", ctypes.c_int64), ("ldko", ctypes.c_int64), ("eps", ctypes.c_double),
+                ("theta", ctypes.c_double)]
+
+
+class KVStore(ctypes.Structure):
+    """ptd_kv_store"""
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
+class PageArray(ctypes.Structure):
+    """ptd_page_array"""
+    _fields_ = [("base", ctypes.c_void_p), ("heads", ctypes.c_int32), ("units", ctypes.c_int32),
+                ("unit_rows", ctypes.c_int32), ("unit_bytes", ctypes.c_int32)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built; run __graft_entry__.build() "
                       "(hipcc --offload-arch=gfx950)")
@@ -137,6 +159,17 @@ _SIGS = {
     "ptd_page_init": ([ctypes.POINTER(PageState), _vp], ctypes.c_int),
     "ptd_page_plan": ([ctypes.POINTER(PageState), _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp,
                        _vp], ctypes.c_int),
+    "ptd_page_plan_shared": ([ctypes.POINTER(PageState), _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp,
+                              _vp, _vp], ctypes.c_int),
+    "ptd_page_fork": ([ctypes.POINTER(PageState)] + [_vp] * 10, ctypes.c_int),
+    "ptd_page_compact": ([ctypes.POINTER(PageState), _vp, _vp, _vp, _vp, _vp], ctypes.c_int),
+    "ptd_page_copy": ([ctypes.POINTER(PageArray), _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp],
+                      ctypes.c_int),
+    "ptd_qk_norm_rope": ([_vp] * 9 + [ctypes.POINTER(KVStore), ctypes.POINTER(QKShape), _vp, _vp,
+                                      _vp], ctypes.c_int),
+    "ptd_token_logprobs_workspace_bytes": ([_i32, _i32, _i32], _sz),
+    "ptd_token_logprobs": ([_vp, ctypes.c_int, _i32, _i32, _i64, _vp, _vp, _i32, ctypes.c_double,
+                            _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp], ctypes.c_int),
     "ptd_prompt_attention": ([_vp, _vp, _vp, _vp, _vp, ctypes.POINTER(PromptShape), _vp, _vp],
                              ctypes.c_int),
     "ptd_verify_sample": ([_vp, ctypes.c_int, _i32, _i64, _vp, _vp, _vp, _i32, _i32,
@@ -292,6 +325,68 @@ def ptd_prompt_attention(q, k, v, row_start, out, shape: PromptShape, dev_status
     _check(_lib.ptd_prompt_attention(_ptr(q), _ptr(k), _ptr(v), _ptr(row_start), _ptr(out),
                                      ctypes.byref(shape), _ptr(dev_status), _stream(stream)),
            "ptd_prompt_attention")
+
+
+def ptd_page_plan_shared(state: PageState, refs, kv_len, new_len, N, rows_per_seq, row_start, slots,
+                         positions=None, dev_status=None, stream=None):
+    _check(_lib.ptd_page_plan_shared(ctypes.byref(state), _ptr(refs), _ptr(kv_len), _ptr(new_len), N,
+                                     rows_per_seq, _ptr(row_start), _ptr(slots), _ptr(positions),
+                                     _ptr(dev_status), _stream(stream)),
+           "ptd_page_plan_shared")
+
+
+def ptd_page_fork(state: PageState, refs, from_, len_, table_next, held_next, copy_src, copy_dst,
+                  copy_rows, dev_status=None, stream=None):
+    _check(_lib.ptd_page_fork(ctypes.byref(state), _ptr(refs), _ptr(from_), _ptr(len_),
+                              _ptr(table_next), _ptr(held_next), _ptr(copy_src), _ptr(copy_dst),
+                              _ptr(copy_rows), _ptr(dev_status), _stream(stream)),
+           "ptd_page_fork")
+
+
+def ptd_page_compact(state: PageState, refs, move_src, move_dst, dev_status=None, stream=None):
+    _check(_lib.ptd_page_compact(ctypes.byref(state), _ptr(refs), _ptr(move_src), _ptr(move_dst),
+                                 _ptr(dev_status), _stream(stream)),
+           "ptd_page_compact")
+
+
+def ptd_page_copy(arrays, num_pages, n, src, dst, rows=None, dev_status=None, stream=None):
+    """arrays: a ctypes array of PageArray (which a program makes once), or a sequence."""
+    if not isinstance(arrays, ctypes.Array):
+        arrays = (PageArray * len(arrays))(*arrays)
+    _check(_lib.ptd_page_copy(arrays, len(arrays), num_pages, n, _ptr(src), _ptr(dst), _ptr(rows),
+                              _ptr(dev_status), _stream(stream)),
+           "ptd_page_copy")
+
+
+def ptd_qk_norm_rope(q, k, v, q_weight, k_weight, positions, slots, q_out, k_out,
+                     store: Optional[KVStore], shape: QKShape,
+                     inv_freq: Optional[Sequence[float]] = None, dev_status=None, stream=None):
+    """inv_freq: host sequence of rot_dim/2 floats, or None for theta^(-2p/rot_dim)."""
+    f = None
+    if inv_freq is not None:
+        if len(inv_freq) != shape.rot_dim // 2:
+            raise ValueError("inv_freq needs rot_dim/2 entries")
+        f = (ctypes.c_double * max(1, len(inv_freq)))(*[float(x) for x in inv_freq])
+    _check(_lib.ptd_qk_norm_rope(_ptr(q), _ptr(k), _ptr(v), _ptr(q_weight), _ptr(k_weight),
+                                 _ptr(positions), _ptr(slots), _ptr(q_out), _ptr(k_out),
+                                 None if store is None else ctypes.byref(store),
+                                 ctypes.byref(shape), None if f is None else ctypes.cast(f, _vp),
+                                 _ptr(dev_status), _stream(stream)),
+           "ptd_qk_norm_rope")
+
+
+def ptd_token_logprobs_workspace_bytes(R: int, V: int, k: int) -> int:
+    return _lib.ptd_token_logprobs_workspace_bytes(R, V, k)
+
+
+def ptd_token_logprobs(logits, dtype, R, V, ld, tokens, nodes, T, temperature, k, logprob,
+                       entropy=None, topk_idx=None, topk_logprob=None, workspace=None,
+                       workspace_bytes=0, dev_status=None, stream=None):
+    _check(_lib.ptd_token_logprobs(_ptr(logits), dtype, R, V, ld, _ptr(tokens), _ptr(nodes), T,
+                                   float(temperature), k, _ptr(logprob), _ptr(entropy),
+                                   _ptr(topk_idx), _ptr(topk_logprob), _ptr(workspace),
+                                   workspace_bytes, _ptr(dev_status), _stream(stream)),
+           "ptd_token_logprobs")
 
 
 def ptd_topk_workspace_bytes(R: int, V: int, k: int) -> int:
@@ -750,16 +845,134 @@ def prompt_attention(q, k, v, row_start, out=None, out_dtype=None, scale: float 
     return out
 
 
+def qk_norm_rope(q, k, positions, q_weight=None, k_weight=None, eps: Optional[float] = 1e-6,
+                 rot_dim: Optional[int] = None, theta: float = 10000.0, inv_freq=None,
+                 pairing: int = PTD_ROPE_HALF, v=None, slots=None, k_pages=None, v_pages=None,
+                 q_out=None, k_out=None, dev_status=None):
+    """Norm of every head of q [N][Hq][D] and k [N][Hkv][D] (views of a wider projection are
+    taken as they are; eps None: no norm), rotation of their first rot_dim dimensions
+    (None: all) by positions int32 [N], and with slots int32 [N] the rows of k and v into k_pages,
+    v_pages [pages][Hkv][page_size][D] (a contiguous cache [B][Hkv][L_cap][D] is B pages of L_cap
+    rows).  Returns (q_out, k_out), new ones where not given (then rows at a negative position
+    hold nothing); q and k themselves are turned in place."""
+    _need_here(q, k, v, q_weight, k_weight, k_pages, v_pages, q_out, k_out)
+    _need_i32(positions, slots, dev_status)
+    if q.dim() != 3 or k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2] or k.dtype != q.dtype:
+        raise ValueError("expected q [N][Hq][D] and k [N][Hkv][D] of one dtype")
+    N, Hq, D = q.shape
+    Hkv, code = k.shape[1], _dtype_code(q)
+    rot = D if rot_dim is None else rot_dim
+    if (positions is not None and positions.numel() != N) or (slots is not None and slots.numel() != N):
+        raise ValueError("expected a position and a slot per row")
+    if eps is None and (q_weight is not None or k_weight is not None):
+        raise ValueError("weights belong to the norm")
+    w = [x for x in (q_weight, k_weight) if x is not None]
+    if any(x.shape != (D,) or not x.is_contiguous() or x.dtype != w[0].dtype for x in w):
+        raise ValueError("expected weights [D] of one dtype")
+    store = None
+    if slots is not None:
+        if v is None or k_pages is None or v_pages is None or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("expected v [N][Hkv][D], k_pages and v_pages with slots")
+        for x in (k_pages, v_pages):
+            if x.dim() != 4 or x.shape != k_pages.shape or x.shape[1] != Hkv or x.shape[3] != D \
+                    or x.dtype != k.dtype or not x.is_contiguous():
+                raise ValueError("expected contiguous pages [pages][Hkv][page_size][D] of k's dtype")
+        store = KVStore(k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[2], k_pages.shape[0])
+    elif v is not None or k_pages is not None or v_pages is not None:
+        raise ValueError("rows into pages need slots")
+    if q_out is None:
+        q_out = torch.empty((N, Hq, D), dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = torch.empty((N, Hkv, D), dtype=q.dtype, device=q.device)
+    if q_out.shape != q.shape or k_out.shape != k.shape or q_out.dtype != q.dtype or k_out.dtype != k.dtype:
+        raise ValueError("expected outputs of q's and k's shape and dtype")
+    shape = QKShape(N, Hq, Hkv, D, rot, pairing, 0 if eps is None else 1, code,
+                    _dtype_code(w[0]) if w else code, _rows(q), _rows(k), 0 if v is None else _rows(v),
+                    _rows(q_out), _rows(k_out), 0.0 if eps is None else float(eps), float(theta))
+    ptd_qk_norm_rope(q, k, v if store else None, q_weight, k_weight, positions, slots, q_out, k_out,
+                     store, shape, inv_freq, dev_status)
+    return q_out, k_out
+
+
+def token_logprobs(logits, tokens=None, k: int = 0, nodes=None, temperature: float = 1.0,
+                   with_entropy: bool = True, workspace=None, dev_status=None):
+    """logits [R][V] or [B][T+1][V] with unit stride along V (rows may lie further apart),
+    tokens int32 of R elements (-1: none) or None; with nodes int32 [B][T] (accept_nodes of
+    verify) tokens are its out_tokens [B][T+1], and each is scored in the row that emitted it.
+    Returns (logprob [R] or None, entropy [R] or None, idx [R][k], logprobs of idx [R][k]; None
+    without k)."""
+    _need_here(logits, workspace)
+    _need_i32(tokens, nodes, dev_status)
+    if logits.dim() != 2:
+        logits = logits.reshape(-1, logits.shape[-1])
+    R, V = logits.shape
+    if V > 1 and logits.stride(1) != 1 or R > 1 and logits.stride(0) < V:
+        raise ValueError("logits need unit stride along the vocabulary, and rows that do not overlap")
+    T = 0
+    if tokens is not None and tokens.numel() != R:
+        raise ValueError("expected a token per row")
+    if nodes is not None:
+        if tokens is None or nodes.dim() != 2 or nodes.shape[0] * (nodes.shape[1] + 1) != R:
+            raise ValueError("expected tokens [B][T+1] and nodes [B][T]")
+        T = nodes.shape[1]
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("expected a contiguous workspace")
+    dev = logits.device
+    lp = torch.empty(R, dtype=torch.float32, device=dev) if tokens is not None else None
+    ent = torch.empty(R, dtype=torch.float32, device=dev) if with_entropy else None
+    idx = torch.empty((R, k), dtype=torch.int32, device=dev) if k else None
+    val = torch.empty((R, k), dtype=torch.float32, device=dev) if k else None
+    nbytes = ptd_token_logprobs_workspace_bytes(R, V, k)
+    if workspace is None and nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    ptd_token_logprobs(logits, _dtype_code(logits), R, V, logits.stride(0) if R > 1 else V, tokens,
+                       nodes, T, temperature, k, lp, ent, idx, val, workspace,
+                       0 if workspace is None else workspace.numel() * workspace.element_size(), dev_status)
+    return lp, ent, idx, val
+
+
+def page_arrays(*caches):
+    """The page arrays of caches for page_copy: BlockKV objects, or tensors of pages
+    [num_pages][Hkv][page_size][D] of any dtype.  A program makes them once."""
+    got = []
+    for x in caches:
+        if isinstance(x, BlockKV):
+            got += [(y, 1) for y in (x.k_pages, x.v_pages)] + [(x.scales, x.scale_rows)]
+        else:
+            got.append((x, 1))
+    pages = {x.shape[0] for x, _ in got}
+    if len(pages) != 1 or any(x.dim() != 4 or not x.is_contiguous() for x, _ in got):
+        raise ValueError("expected contiguous pages [num_pages][Hkv][page_size][D], as many in each cache")
+    rows = [PageArray(x.data_ptr(), x.shape[1], x.shape[2], n, x.shape[3] * x.element_size()) for x, n in got]
+    arrays = (PageArray * len(rows))(*rows)
+    arrays.tensors = [x for x, _ in got]
+    return arrays
+
+
+def page_copy(arrays, src, dst, rows=None, dev_status=None):
+    """Pages src[i] to dst[i] (int32 [n], -1: none) in every array of page_arrays(), the first
+    rows[i] rows of them or (None) all."""
+    _need_here(*arrays.tensors)
+    _need_i32(src, dst, rows, dev_status)
+    n = src.numel()
+    if dst.numel() != n or (rows is not None and rows.numel() != n):
+        raise ValueError("expected as many destinations and rows as sources")
+    ptd_page_copy(arrays, arrays.tensors[0].shape[0], n, src, dst, rows, dev_status)
+
+
 class PageTables:
     """Page tables of B sequences over num_pages pages of page_size rows, on the
-    GPU: plan() gives every sequence the pages its lengths ask for."""
+    GPU: plan() gives every sequence the pages its lengths ask for.  With shared=True
+    sequences may hold pages together: fork() and compact()."""
 
-    def __init__(self, B: int, page_size: int, max_pages: int, num_pages: int, device="cuda"):
+    def __init__(self, B: int, page_size: int, max_pages: int, num_pages: int, device="cuda",
+                 shared: bool = False):
         def i32(*shape):
             return torch.empty(shape, dtype=torch.int32, device=device)
 
         self.page_table, self.num_held = i32(B, max_pages), i32(B)
         self.free_pages, self.num_free = i32(num_pages), i32(1)
+        self.refs = torch.zeros(num_pages, dtype=torch.int32, device=device) if shared else None
         self.B, self.page_size = B, page_size
         self.max_pages, self.num_pages = max_pages, num_pages
         _need_here(self.page_table)
@@ -779,8 +992,41 @@ class PageTables:
         dev = self.page_table.device
         start = None if rows_per_seq else torch.empty(self.B + 1, dtype=torch.int32, device=dev)
         slots, pos = (torch.empty(N, dtype=torch.int32, device=dev) for _ in range(2))
-        ptd_page_plan(self.state(), kv_len, new_len, N, rows_per_seq, start, slots, pos, dev_status)
+        if self.refs is None:
+            ptd_page_plan(self.state(), kv_len, new_len, N, rows_per_seq, start, slots, pos, dev_status)
+        else:
+            ptd_page_plan_shared(self.state(), self.refs, kv_len, new_len, N, rows_per_seq, start,
+                                 slots, pos, dev_status)
         return start, slots, pos
+
+    def _need_shared(self):
+        if self.refs is None:
+            raise ValueError("tables of one holder per page: make them with shared=True")
+
+    def fork(self, from_, len_, dev_status=None):
+        """Sequence b goes on from the first len_[b] rows of sequence from_[b] (-1: it ends);
+        returns (copy_src, copy_dst, copy_rows) int32 [B] for page_copy, which has to follow before
+        rows are written.  page_table and num_held are new tensors afterwards."""
+        self._need_shared()
+        _need_i32(from_, len_, dev_status, self.page_table)
+        if from_.numel() != self.B or len_.numel() != self.B:
+            raise ValueError("expected sources and lengths of B sequences")
+        dev = self.page_table.device
+        table, held = torch.full_like(self.page_table, -1), torch.empty_like(self.num_held)
+        src, dst, rows = (torch.empty(self.B, dtype=torch.int32, device=dev) for _ in range(3))
+        ptd_page_fork(self.state(), self.refs, from_, len_, table, held, src, dst, rows, dev_status)
+        self.page_table, self.num_held = table, held
+        return src, dst, rows
+
+    def compact(self, dev_status=None):
+        """Moves the held pages to the lowest ids; returns (move_src, move_dst) int32
+        [num_pages / 2] for page_copy, which has to follow."""
+        self._need_shared()
+        _need_i32(dev_status, self.page_table)
+        dev = self.page_table.device
+        src, dst = (torch.empty(self.num_pages // 2, dtype=torch.int32, device=dev) for _ in range(2))
+        ptd_page_compact(self.state(), self.refs, src, dst, dev_status)
+        return src, dst
 
 
 class BlockKV:

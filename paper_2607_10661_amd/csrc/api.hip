@@ -17,7 +17,7 @@ extern "C" const char* ptd_status_string(int status) {
     case PTD_ERR_SCRATCH: return "problem needs more than the 64 MiB scratch of ptd_tree_attention_noalloc";
     case PTD_ERR_NO_PAGES: return "the free list has too few pages";
     case PTD_ERR_ROWS: return "row starts, row counts, source rows or slot order out of range";
-    case PTD_ERR_VALUE: return "a key or value that is not finite";
+    case PTD_ERR_VALUE: return "a key or value that is not finite, or a token outside the vocabulary";
     default: return "unknown status";
   }
 }

@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "ptd_common.hpp"
+#include "ptd_internal.hpp"
 
 namespace {
 
@@ -18,6 +19,7 @@ struct PlanParams {
   int32_t* slots;
   int32_t* positions;
   int32_t* dev_status;
+  int32_t* refs;  // sequences that hold a page (ptd_page_plan_shared), or null
   int N, rows_per_seq, page_shift;
 };
 
@@ -105,6 +107,18 @@ __device__ __forceinline__ int slot_at(const PlanParams& p, int id, int pos) {
   ptd::report(p.dev_status, PTD_ERR_PAGE);
   return -1;
 }
+// Slot of a new row in a page that its sequence held before the call: none, where another
+// sequence holds that page too.
+template <bool SHARED>
+__device__ __forceinline__ int slot_in_held(const PlanParams& p, int id, int pos) {
+  if constexpr (SHARED) {
+    if (static_cast<uint32_t>(id) < static_cast<uint32_t>(p.s.num_pages) && ptd::load_count(p.refs + id) != 1) {
+      ptd::report(p.dev_status, PTD_ERR_PAGE);
+      return -1;
+    }
+  }
+  return slot_at(p, id, pos);
+}
 __device__ __forceinline__ const int32_t* table_of(const PlanParams& p, int b) {
   return p.s.page_table + static_cast<size_t>(b) * p.s.max_pages;
 }
@@ -112,7 +126,7 @@ __device__ __forceinline__ const int32_t* table_of(const PlanParams& p, int b) {
 // Rows [i0, i1) by `step` when the tables are written.  starts: of packed rows, in LDS
 // where they fit, else in memory.  (Rows and pages are counted without a sign: up to 2^31
 // of either, a step past the last one does not wrap.)
-template <typename Starts>
+template <bool SHARED, typename Starts>
 __device__ __forceinline__ void put_rows(const PlanParams& p, const Starts& starts, int i0, int i1, int step) {
   for (uint32_t u = i0; u < static_cast<uint32_t>(i1); u += step) {
     const int i = static_cast<int>(u);
@@ -128,9 +142,14 @@ __device__ __forceinline__ void put_rows(const PlanParams& p, const Starts& star
     const bool row = r < w.rows;
     const int pos = w.kv + r;
     const bool page = row && (pos >> p.page_shift) < w.held;
-    put_row(p, i, page ? slot_at(p, table_of(p, b)[pos >> p.page_shift], pos) : -1, row ? pos : -1);
+    put_row(p, i, page ? slot_in_held<SHARED>(p, table_of(p, b)[pos >> p.page_shift], pos) : -1, row ? pos : -1);
   }
 }
+
+// A page that the planning workgroup is about to give back: the lowest sequence that gives it
+// up puts it on the list, marked by kGiver + its number in the page's count.
+constexpr int kGiver = -0x7FFFFFFF - 1;
+__device__ __forceinline__ bool is_giver(int v) { return v < kGiver + 65536; }
 
 // One workgroup: a thread per sequence (in rounds of the workgroup's size) counts pages, sums over
 // the workgroup give every sequence its places on the free list and in the rows,
@@ -139,7 +158,11 @@ __device__ __forceinline__ void put_rows(const PlanParams& p, const Starts& star
 // and 4200 pages): with ONE round of sequences, the lengths are loaded
 // once, new rows take their page ids from where the tables get them, and a step of 16
 // sequences waits three times for memory: lengths, ids, stores.
-template <bool ONE, int NT>
+//
+// With SHARED pages, surplus ones are counted down first, then claimed by the lowest sequence
+// that gave them up where nobody is left, then moved by those; the counts are changed and read past the
+// first-level cache.
+template <bool ONE, int NT, bool SHARED>
 __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
   __shared__ Sums s_scan[NT / PTD_WAVE];
   __shared__ int s_back[NT], s_need[NT], s_off[NT], s_grow[NT];
@@ -169,13 +192,70 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
     }
   }
   long long total = all.back;
-  if (total > p.s.num_pages - count) {  // pages held twice: the list cannot take them
+  if constexpr (SHARED) {
+    // every surplus page of every sequence, in order: f(round's sequence, its page, whether there is one)
+    auto each = [&](auto&& f) __attribute__((always_inline)) {
+      for (int b0 = 0; b0 < B; b0 += NT) {  // uniform
+        Sums t = all;
+        if (!ONE) {
+          w = b0 + tid < B ? want_of(p, b0 + tid, nullptr) : none;
+          at = block_scan<NT>(sums_of(w), s_scan, &t);
+        }
+        s_back[tid] = static_cast<int>(min(at.back, static_cast<long long>(0x7FFFFFFF)));
+        s_need[tid] = w.need;
+        __syncthreads();
+        const int n = min(B - b0, NT);
+        for (long long j0 = 0; j0 < t.back; j0 += NT) {  // uniform
+          const bool has = j0 + tid < t.back;
+          const int x = has ? upper(s_back, n, j0 + tid) : 0;
+          const int id = has ? table_of(p, b0 + x)[s_need[x] + (j0 + tid - s_back[x])] : -1;
+          f(b0 + x, id, has && static_cast<uint32_t>(id) < static_cast<uint32_t>(p.s.num_pages), has);
+        }
+        __syncthreads();
+      }
+    };
+    long long freed = 0;
+    if (all.back > 0) {  // uniform
+      each([&](int, int id, bool ok, bool has) __attribute__((always_inline)) {
+        if (ok ? ptd::add_count(p.refs + id, -1) <= 0 : has) ptd::report(p.dev_status, PTD_ERR_PAGE);
+      });
+      ptd::drained_barrier();
+      each([&](int b, int id, bool ok, bool) __attribute__((always_inline)) {
+        if (!ok) return;
+        const int v = ptd::load_count(p.refs + id);
+        if (v == 0 || is_giver(v)) ptd::min_count(p.refs + id, kGiver + b);
+      });
+      ptd::drained_barrier();
+      each([&](int b, int id, bool ok, bool) __attribute__((always_inline)) {
+        freed += __syncthreads_count(ok && ptd::load_count(p.refs + id) == kGiver + b);
+      });
+    }
+    if (freed > p.s.num_pages - count) {  // pages held and free: the list cannot take them
+      if (tid == 0) ptd::report(p.dev_status, PTD_ERR_PAGE);
+    }
+    total = min(freed, static_cast<long long>(p.s.num_pages - count));
+    long long done = 0;
+    if (freed > 0) {  // uniform
+      const int count1 = count + static_cast<int>(total);
+      each([&](int b, int id, bool ok, bool) __attribute__((always_inline)) {
+        const bool mine = ok && ptd::load_count(p.refs + id) == kGiver + b;
+        Sums t;
+        const long long j = done + block_scan<NT>({mine, 0, 0}, s_scan, &t).back;
+        if (mine) {
+          if (count1 - 1 - j >= count) p.s.free_pages[count1 - 1 - j] = id;
+          p.refs[id] = 0;
+        }
+        done += t.back;
+      });
+      ptd::drained_barrier();
+    }
+  } else if (total > p.s.num_pages - count) {  // pages held twice: the list cannot take them
     if (tid == 0) ptd::report(p.dev_status, PTD_ERR_PAGE);
     total = p.s.num_pages - count;
   }
   const int count1 = count + static_cast<int>(total);
   long long done = 0;
-  for (int b0 = 0; b0 < B && total > 0; b0 += NT) {  // uniform
+  for (int b0 = 0; !SHARED && b0 < B && total > 0; b0 += NT) {  // uniform
     Sums t = all;
     if (!ONE) {
       w = b0 + tid < B ? want_of(p, b0 + tid, nullptr) : none;
@@ -233,9 +313,13 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
       const int j = static_cast<int>(u);
       const int x = upper(s_off, n, j);
       const int k = j - s_off[x];
-      if (k < s_grow[x])
-        p.s.page_table[static_cast<size_t>(b0 + x) * p.s.max_pages + s_held[x] + k] =
-            p.s.free_pages[count1 - 1 - (taken + j)];
+      if (k < s_grow[x]) {
+        const int id = p.s.free_pages[count1 - 1 - (taken + j)];
+        p.s.page_table[static_cast<size_t>(b0 + x) * p.s.max_pages + s_held[x] + k] = id;
+        if constexpr (SHARED) {
+          if (static_cast<uint32_t>(id) < static_cast<uint32_t>(p.s.num_pages)) p.refs[id] = 1;
+        }
+      }
     }
     // (a sequence refused above keeps num_held as it is, whatever it says)
     if (live && now != w.held) p.s.num_held[b0 + tid] = now;
@@ -279,17 +363,19 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
       const int pg = pos >> p.page_shift;
       const bool page = row && pg < s_need[b];
       const int32_t* from = pg < s_held[b] ? table_of(p, b) + pg : p.s.free_pages + (count1 - 1 - (s_off[b] + pg - s_held[b]));
-      put_row(p, i, page ? slot_at(p, *from, pos) : -1, row ? pos : -1);
+      put_row(p, i, !page ? -1 : pg < s_held[b] ? slot_in_held<SHARED>(p, *from, pos) : slot_at(p, *from, pos), row ? pos : -1);
     }
   } else {
-    __syncthreads();
-    put_rows(p, p.row_start, tid, p.N, NT);
+    if constexpr (SHARED) ptd::drained_barrier();
+    else __syncthreads();
+    put_rows<SHARED>(p, p.row_start, tid, p.N, NT);
   }
 }
 
 constexpr int kSlotThreads = 256;
 constexpr int kSlotRows = kSlotThreads;  // rows per workgroup
 
+template <bool SHARED>
 __global__ void __launch_bounds__(kSlotThreads) k_page_slots(PlanParams p) {
   __shared__ int s_start[kPlanLarge];
   const int i0 = blockIdx.x * kSlotRows + threadIdx.x;
@@ -297,9 +383,9 @@ __global__ void __launch_bounds__(kSlotThreads) k_page_slots(PlanParams p) {
   if (p.rows_per_seq == 0 && p.s.B <= kPlanLarge) {
     for (int x = threadIdx.x; x < p.s.B; x += kSlotThreads) s_start[x] = p.row_start[x];
     __syncthreads();
-    put_rows(p, s_start, i0, i1, kSlotThreads);
+    put_rows<SHARED>(p, s_start, i0, i1, kSlotThreads);
   } else {
-    put_rows(p, p.row_start, i0, i1, kSlotThreads);
+    put_rows<SHARED>(p, p.row_start, i0, i1, kSlotThreads);
   }
 }
 
@@ -311,20 +397,6 @@ __global__ void __launch_bounds__(256) k_page_init(ptd_page_state s) {
   for (long long i = first; i < s.num_pages; i += step) s.free_pages[i] = s.num_pages - 1 - static_cast<int>(i);
   for (long long i = first; i < s.B; i += step) s.num_held[i] = 0;
   if (first == 0) s.num_free[0] = s.num_pages;
-}
-
-int check_state(const ptd_page_state* s, int* shift) {
-  PTD_RETURN_IF(!s || !s->page_table || !s->num_held || !s->free_pages || !s->num_free, PTD_ERR_NULL);
-  const int ps = s->page_size;
-  PTD_RETURN_IF(ps < 1 || ps > (1 << 20) || (ps & (ps - 1)) != 0, PTD_ERR_SHAPE);
-  PTD_RETURN_IF(s->B < 1 || s->B > 65536 || s->max_pages < 1 || s->num_pages < 1, PTD_ERR_SHAPE);
-  PTD_RETURN_IF(static_cast<long long>(s->max_pages) * ps > 0x7FFFFFFFLL ||
-                    static_cast<long long>(s->num_pages) * ps > 0x7FFFFFFFLL,
-                PTD_ERR_SHAPE);
-  int sh = 0;
-  while ((1 << sh) < ps) ++sh;
-  *shift = sh;
-  return PTD_OK;
 }
 
 // ===========================================================================
@@ -614,7 +686,7 @@ void launch_write(const WriteParams& prm, int scale_rows, dim3 grid, hipStream_t
 
 extern "C" int ptd_page_init(const ptd_page_state* state, void* stream) {
   int shift = 0;
-  const int rc = check_state(state, &shift);
+  const int rc = ptd_check_state(state, &shift);
   if (rc != PTD_OK) return rc;
   const long long n = std::max(static_cast<long long>(state->B) * state->max_pages,
                                static_cast<long long>(state->num_pages));
@@ -623,12 +695,25 @@ extern "C" int ptd_page_init(const ptd_page_state* state, void* stream) {
   return ptd_launch_status();
 }
 
-extern "C" int ptd_page_plan(const ptd_page_state* state, const int32_t* kv_len,
-                             const int32_t* new_len, int32_t N, int32_t rows_per_seq,
-                             int32_t* row_start, int32_t* slots, int32_t* positions,
-                             int32_t* dev_status, void* stream) {
+namespace {
+
+template <bool SHARED>
+void launch_plan(const PlanParams& prm, hipStream_t st) {
+  const bool large = (prm.N >> prm.page_shift) > kPlanPages || prm.s.B > kPlanSmall;
+  if (!large) hipLaunchKernelGGL((k_page_plan<true, kPlanSmall, SHARED>), dim3(1), dim3(kPlanSmall), 0, st, prm);
+  else if (prm.s.B <= kPlanLarge) hipLaunchKernelGGL((k_page_plan<true, kPlanLarge, SHARED>), dim3(1), dim3(kPlanLarge), 0, st, prm);
+  else hipLaunchKernelGGL((k_page_plan<false, kPlanLarge, SHARED>), dim3(1), dim3(kPlanLarge), 0, st, prm);
+  if (prm.N > kPlanRows) {
+    const unsigned grid = static_cast<unsigned>((static_cast<long long>(prm.N) + kSlotRows - 1) / kSlotRows);
+    hipLaunchKernelGGL((k_page_slots<SHARED>), dim3(grid), dim3(kSlotThreads), 0, st, prm);
+  }
+}
+
+int page_plan(const ptd_page_state* state, int32_t* refs, const int32_t* kv_len, const int32_t* new_len, int32_t N,
+              int32_t rows_per_seq, int32_t* row_start, int32_t* slots, int32_t* positions, int32_t* dev_status,
+              void* stream) {
   PlanParams prm;
-  const int rc = check_state(state, &prm.page_shift);
+  const int rc = ptd_check_state(state, &prm.page_shift);
   if (rc != PTD_OK) return rc;
   PTD_RETURN_IF(!kv_len || !new_len || (N > 0 && !slots) || (rows_per_seq == 0 && !row_start), PTD_ERR_NULL);
   PTD_RETURN_IF(N < 0 || rows_per_seq < 0, PTD_ERR_SHAPE);
@@ -640,18 +725,29 @@ extern "C" int ptd_page_plan(const ptd_page_state* state, const int32_t* kv_len,
   prm.slots = slots;
   prm.positions = positions;
   prm.dev_status = dev_status;
+  prm.refs = refs;
   prm.N = N;
   prm.rows_per_seq = rows_per_seq;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool large = (N >> prm.page_shift) > kPlanPages || state->B > kPlanSmall;
-  if (!large) hipLaunchKernelGGL((k_page_plan<true, kPlanSmall>), dim3(1), dim3(kPlanSmall), 0, st, prm);
-  else if (state->B <= kPlanLarge) hipLaunchKernelGGL((k_page_plan<true, kPlanLarge>), dim3(1), dim3(kPlanLarge), 0, st, prm);
-  else hipLaunchKernelGGL((k_page_plan<false, kPlanLarge>), dim3(1), dim3(kPlanLarge), 0, st, prm);
-  if (N > kPlanRows) {
-    const unsigned grid = static_cast<unsigned>((static_cast<long long>(N) + kSlotRows - 1) / kSlotRows);
-    hipLaunchKernelGGL(k_page_slots, dim3(grid), dim3(kSlotThreads), 0, st, prm);
-  }
+  refs ? launch_plan<true>(prm, st) : launch_plan<false>(prm, st);
   return ptd_launch_status();
+}
+
+}  // namespace
+
+extern "C" int ptd_page_plan(const ptd_page_state* state, const int32_t* kv_len,
+                             const int32_t* new_len, int32_t N, int32_t rows_per_seq,
+                             int32_t* row_start, int32_t* slots, int32_t* positions,
+                             int32_t* dev_status, void* stream) {
+  return page_plan(state, nullptr, kv_len, new_len, N, rows_per_seq, row_start, slots, positions, dev_status, stream);
+}
+
+extern "C" int ptd_page_plan_shared(const ptd_page_state* state, int32_t* refs, const int32_t* kv_len,
+                                    const int32_t* new_len, int32_t N, int32_t rows_per_seq,
+                                    int32_t* row_start, int32_t* slots, int32_t* positions,
+                                    int32_t* dev_status, void* stream) {
+  PTD_RETURN_IF(!refs, PTD_ERR_NULL);
+  return page_plan(state, refs, kv_len, new_len, N, rows_per_seq, row_start, slots, positions, dev_status, stream);
 }
 
 extern "C" int ptd_kv_write_fp8blk(const void* k, const void* v, ptd_dtype dtype, int64_t ldk,

@@ -42,6 +42,31 @@ __device__ __forceinline__ void report(int32_t* dev_status, int32_t code) {
 }
 
 // ---------------------------------------------------------------------------
+// counts in memory that several threads change: past the first-level cache
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ int load_count(const int32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void store_count(int32_t* p, int v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ int add_count(int32_t* p, int v) {  // the value before
+  return __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void min_count(int32_t* p, int v) {
+  __hip_atomic_fetch_min(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void max_count(int32_t* p, int v) {
+  __hip_atomic_fetch_max(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// A barrier of the workgroup that every thread's stores and atomics have passed: they
+// are in the second-level cache, which all of a workgroup's waves share.
+__device__ __forceinline__ void drained_barrier() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// ---------------------------------------------------------------------------
 // wave (64-lane) reductions
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ float wave_max(float v) {

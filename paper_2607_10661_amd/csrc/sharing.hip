@@ -1,0 +1,432 @@
+// Pages that several sequences hold: sequences that go on from others' rows
+// (ptd_page_fork), live pages moved to the front (ptd_page_compact), and the pages' data
+// (ptd_page_copy).  refs[p] is the number of sequences that hold page p, 0 for a free one.
+#include <algorithm>
+
+#include "ptd_common.hpp"
+#include "ptd_internal.hpp"
+
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kWaves = kThreads / PTD_WAVE;
+
+// Exclusive sum of v over the workgroup; the total to every thread.
+__device__ __forceinline__ int block_scan(int v, int* lds, int* total) {
+  const int wave = threadIdx.x >> 6;
+  const int in = ptd::wave_scan_i32(v, [](int a, int b) { return a + b; });
+  __syncthreads();  // lds of the call before is read
+  if ((threadIdx.x & 63) == 63) lds[wave] = in;
+  __syncthreads();
+  int base = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const int x = lds[w];
+    if (w < wave) base += x;
+    all += x;
+  }
+  *total = all;
+  return base + in - v;
+}
+
+struct ForkArgs {
+  ptd_page_state s;
+  int32_t* refs;
+  const int32_t* from;
+  const int32_t* len;
+  int32_t* table_next;
+  int32_t* held_next;
+  int32_t* copy_src;
+  int32_t* copy_dst;
+  int32_t* copy_rows;
+  int32_t* dev_status;
+  int page_shift;
+};
+
+// A page's count while a fork is worked out: whether any sequence held it, then either how many
+// sequences hold it as a whole one, or (kPart) 65535 - the lowest sequence that goes on in it.
+constexpr int kHeld = 1 << 30, kPart = 1 << 29, kCount = kPart - 1;
+
+// What sequence b is to hold: whole pages of sequence a, and the rows of a page in part.
+struct Fork {
+  int a, whole, part;
+};
+__device__ __forceinline__ Fork fork_of(const ForkArgs& g, int b) {
+  const int a = g.from[b];
+  const int n = a < 0 ? 0 : g.len[b];
+  return {a, n >> g.page_shift, n & ((1 << g.page_shift) - 1)};
+}
+__device__ __forceinline__ const int32_t* table_of(const ForkArgs& g, int b) {
+  return g.s.page_table + static_cast<size_t>(b) * g.s.max_pages;
+}
+
+// One workgroup, a wave per sequence where tables are read and a thread per page where counts
+// are.  Everything is checked before anything is changed.  Which of several sequences keeps a page
+// that they all go on in is settled by the largest of 65535 - b, so no output depends on the
+// order of the atomics.
+__global__ void __launch_bounds__(kThreads) k_page_fork(ForkArgs g) {
+  __shared__ int s_scan[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int B = g.s.B, n = g.s.num_pages;
+  const int count = g.s.num_free[0];
+  // ---- checks
+  int bad = count < 0 || count > n ? PTD_ERR_PAGE : 0;
+  for (int b = wave; b < B; b += kWaves) {
+    const int a = g.from[b], held = g.s.num_held[b];
+    if (held < 0 || held > g.s.max_pages) bad = PTD_ERR_PAGE;
+    if (a < -1 || a >= B) bad = PTD_ERR_ROWS;
+    if (bad || a < 0) continue;
+    const int have = g.s.num_held[a];
+    const long long rows = static_cast<long long>(have) << g.page_shift;
+    if (have < 0 || have > g.s.max_pages) bad = PTD_ERR_PAGE;
+    else if (g.len[b] < 0 || g.len[b] > rows) bad = PTD_ERR_KV_LEN;
+    if (bad) continue;
+    const Fork f = fork_of(g, b);
+    const int32_t* row = table_of(g, a);
+    for (int k = lane; k < f.whole + (f.part > 0); k += PTD_WAVE)
+      if (static_cast<uint32_t>(row[k]) >= static_cast<uint32_t>(n)) bad = PTD_ERR_PAGE;
+  }
+  if (bad) ptd::report(g.dev_status, bad);
+  bool refused = __syncthreads_or(bad != 0);
+  int copies = 0;
+  if (!refused) {
+    // ---- who holds a page as a whole one
+    for (int p = tid; p < n; p += kThreads) ptd::store_count(g.refs + p, g.refs[p] > 0 ? kHeld : 0);
+    ptd::drained_barrier();
+    for (int b = wave; b < B; b += kWaves) {
+      const Fork f = fork_of(g, b);
+      if (f.whole == 0) continue;
+      const int32_t* row = table_of(g, f.a);
+      for (int k = lane; k < f.whole; k += PTD_WAVE) ptd::add_count(g.refs + row[k], 1);
+    }
+    ptd::drained_barrier();
+    // ---- who goes on in a page that nobody holds as a whole one: the lowest
+    for (int b = tid; b < B; b += kThreads) {
+      const Fork f = fork_of(g, b);
+      if (f.part == 0) continue;
+      int32_t* r = g.refs + table_of(g, f.a)[f.whole];
+      const int v = ptd::load_count(r);
+      if ((v & kPart) || (v & kCount) == 0) ptd::max_count(r, kHeld | kPart | (65535 - b));
+    }
+    ptd::drained_barrier();
+    for (int b0 = 0; b0 < B; b0 += kThreads) {  // uniform
+      bool copy = false;
+      if (b0 + tid < B) {
+        const Fork f = fork_of(g, b0 + tid);
+        copy = f.part > 0 && ptd::load_count(g.refs + table_of(g, f.a)[f.whole]) != (kHeld | kPart | (65535 - b0 - tid));
+      }
+      copies += __syncthreads_count(copy);
+    }
+    // the pages that are taken have to be there, and are checked as the tables were
+    bool short_of = copies > count;
+    if (!short_of) {
+      int odd = 0;
+      for (int i = tid; i < copies; i += kThreads)
+        if (static_cast<uint32_t>(g.s.free_pages[count - 1 - i]) >= static_cast<uint32_t>(n)) odd = 1;
+      if (odd) ptd::report(g.dev_status, PTD_ERR_PAGE);
+      refused = __syncthreads_or(odd);
+    } else {
+      if (tid == 0) ptd::report(g.dev_status, PTD_ERR_NO_PAGES);
+      refused = true;
+    }
+    if (refused) {  // the counts as they were: by the tables
+      for (int p = tid; p < n; p += kThreads) ptd::store_count(g.refs + p, 0);
+      ptd::drained_barrier();
+      for (int b = wave; b < B; b += kWaves) {
+        const int32_t* row = table_of(g, b);
+        for (int k = lane; k < g.s.num_held[b]; k += PTD_WAVE)
+          if (static_cast<uint32_t>(row[k]) < static_cast<uint32_t>(n)) ptd::add_count(g.refs + row[k], 1);
+      }
+    }
+  }
+  if (refused) {  // nothing changes
+    for (int b = wave; b < B; b += kWaves) {
+      const int held = min(max(g.s.num_held[b], 0), g.s.max_pages);
+      for (int k = lane; k < held; k += PTD_WAVE)
+        g.table_next[static_cast<size_t>(b) * g.s.max_pages + k] = table_of(g, b)[k];
+      if (lane == 0) {
+        g.held_next[b] = g.s.num_held[b];
+        g.copy_src[b] = g.copy_dst[b] = -1;
+        g.copy_rows[b] = 0;
+      }
+    }
+    return;
+  }
+  // ---- tables, copies
+  for (int b = wave; b < B; b += kWaves) {
+    const Fork f = fork_of(g, b);
+    if (f.whole == 0) continue;
+    const int32_t* row = table_of(g, f.a);
+    for (int k = lane; k < f.whole; k += PTD_WAVE) g.table_next[static_cast<size_t>(b) * g.s.max_pages + k] = row[k];
+  }
+  int taken = 0;
+  for (int b0 = 0; b0 < B; b0 += kThreads) {  // uniform
+    const int b = b0 + tid;
+    Fork f = {-1, 0, 0};
+    int page = -1;
+    bool copy = false;
+    if (b < B) {
+      f = fork_of(g, b);
+      if (f.part > 0) {
+        page = table_of(g, f.a)[f.whole];
+        copy = ptd::load_count(g.refs + page) != (kHeld | kPart | (65535 - b));
+      }
+    }
+    int all;
+    const int at = taken + block_scan(copy, s_scan, &all);
+    if (b < B) {
+      int mine = page;
+      if (copy) {
+        mine = g.s.free_pages[count - 1 - at];
+        ptd::store_count(g.refs + mine, 1);
+      }
+      if (f.part > 0) g.table_next[static_cast<size_t>(b) * g.s.max_pages + f.whole] = mine;
+      g.held_next[b] = f.whole + (f.part > 0);
+      g.copy_src[b] = copy ? page : -1;
+      g.copy_dst[b] = copy ? mine : -1;
+      g.copy_rows[b] = copy ? f.part : 0;
+    }
+    taken += all;
+  }
+  ptd::drained_barrier();
+  // ---- counts, and the pages that nobody holds any more, from the highest id down
+  int at = count - copies;
+  for (int p0 = 0; p0 < n; p0 += kThreads) {  // uniform
+    const int p = n - 1 - p0 - tid;
+    bool gone = false;
+    if (p >= 0) {
+      const int v = ptd::load_count(g.refs + p);
+      const int now = (v & kPart) ? 1 : v & kCount;
+      gone = (v & kHeld) && now == 0;
+      g.refs[p] = now;
+    }
+    int all;
+    const int to = at + block_scan(gone, s_scan, &all);
+    if (gone && to < n) g.s.free_pages[to] = p;
+    at += all;
+  }
+  if (tid == 0) {
+    if (at > n) ptd::report(g.dev_status, PTD_ERR_PAGE);  // pages that were held and free
+    g.s.num_free[0] = min(at, n);
+  }
+}
+
+struct CompactArgs {
+  ptd_page_state s;
+  int32_t* refs;
+  int32_t* move_src;
+  int32_t* move_dst;
+  int32_t* dev_status;
+};
+
+// One workgroup.  With L live pages, the k-th free id below L takes the k-th live page from L on
+// (there are as many of both); a moved page's count holds -1 - its new id while the tables are
+// changed.
+__global__ void __launch_bounds__(kThreads) k_page_compact(CompactArgs g) {
+  __shared__ int s_scan[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = g.s.num_pages;
+  int live = 0;
+  for (int p0 = 0; p0 < n; p0 += kThreads) {  // uniform
+    const int p = p0 + tid;
+    const int v = p < n ? g.refs[p] : 0;
+    if (v < 0) {  // (no count: free)
+      g.refs[p] = 0;
+      ptd::report(g.dev_status, PTD_ERR_PAGE);
+    }
+    live += __syncthreads_count(v > 0);
+  }
+  int holes = 0, movers = 0;
+  for (int p0 = 0; p0 < n; p0 += kThreads) {
+    const int p = p0 + tid;
+    const int v = p < n ? g.refs[p] : 0;
+    const bool hole = p < live && v <= 0, mover = p < n && p >= live && v > 0;
+    int all;
+    const int i = holes + block_scan(hole, s_scan, &all);
+    if (hole) g.move_dst[i] = p;
+    holes += all;
+    const int j = movers + block_scan(mover, s_scan, &all);
+    if (mover) g.move_src[j] = p;
+    movers += all;
+  }
+  __syncthreads();
+  for (int i = tid; i < n / 2; i += kThreads) {
+    if (i < movers) {
+      const int a = g.move_src[i], b = g.move_dst[i];
+      g.refs[b] = g.refs[a];
+      g.refs[a] = -1 - b;
+    } else {
+      g.move_src[i] = g.move_dst[i] = -1;
+    }
+  }
+  __syncthreads();
+  for (int b = wave; b < g.s.B; b += kWaves) {
+    const int held = g.s.num_held[b];
+    if (held < 0 || held > g.s.max_pages) {
+      if (lane == 0) ptd::report(g.dev_status, PTD_ERR_PAGE);
+      continue;
+    }
+    int32_t* row = g.s.page_table + static_cast<size_t>(b) * g.s.max_pages;
+    for (int k = lane; k < held; k += PTD_WAVE) {
+      const int id = row[k];
+      if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(n)) {
+        ptd::report(g.dev_status, PTD_ERR_PAGE);
+      } else {
+        const int v = g.refs[id];
+        if (v < 0) row[k] = -1 - v;
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < movers; i += kThreads) g.refs[g.move_src[i]] = 0;
+  for (int i = tid; i < n - live; i += kThreads) g.s.free_pages[i] = n - 1 - i;
+  if (tid == 0) g.s.num_free[0] = n - live;
+}
+
+// ===========================================================================
+// the pages' data
+// ===========================================================================
+constexpr int kCopyThreads = 256;
+constexpr int kArrays = 96;  // of one launch
+constexpr int kPiece = 32768;  // bytes that a workgroup copies in one turn
+
+struct CopyArray {
+  char* base;
+  int32_t heads, units, unit_rows, unit_bytes, granule;
+};
+struct CopyArgs {
+  CopyArray arrays[kArrays];
+  const int32_t* src;
+  const int32_t* dst;
+  const int32_t* rows;
+  int32_t* dev_status;
+  int n, num_pages, pieces;  // of a page of the largest array
+};
+
+// `bytes` bytes from each of `heads` places `step` apart, from the piece's first byte on.
+template <typename V>
+__device__ __forceinline__ void copy_runs(const char* from, char* to, int heads, long long step, int run, long long first,
+                                          long long last) {
+  (void)heads;
+  // first, last: in bytes of the runs laid end to end
+  for (long long i = first + static_cast<long long>(threadIdx.x) * sizeof(V); i < last; i += kCopyThreads * sizeof(V)) {
+    const long long h = i / run;
+    const long long at = h * step + (i - h * run);
+    *reinterpret_cast<V*>(to + at) = *reinterpret_cast<const V*>(from + at);
+  }
+}
+
+__global__ void __launch_bounds__(kCopyThreads) k_page_copy(CopyArgs g) {
+  const CopyArray a = g.arrays[blockIdx.y];
+  const long long items = static_cast<long long>(g.n) * g.pieces;
+  for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+    const int i = static_cast<int>(item / g.pieces), piece = static_cast<int>(item - static_cast<long long>(i) * g.pieces);
+    const int s = g.src[i], d = g.dst[i];
+    if (s == -1 || d == -1 || s == d) continue;
+    if (static_cast<uint32_t>(s) >= static_cast<uint32_t>(g.num_pages) || static_cast<uint32_t>(d) >= static_cast<uint32_t>(g.num_pages)) {
+      if (threadIdx.x == 0) ptd::report(g.dev_status, PTD_ERR_PAGE);
+      continue;
+    }
+    const long long step = static_cast<long long>(a.units) * a.unit_bytes;  // of a head
+    int units = a.units;
+    if (g.rows) {
+      const int r = g.rows[i];
+      if (r < 0 || r > static_cast<long long>(a.units) * a.unit_rows) {
+        if (threadIdx.x == 0) ptd::report(g.dev_status, PTD_ERR_ROWS);
+        continue;
+      }
+      units = (r + a.unit_rows - 1) / a.unit_rows;
+    }
+    const bool all = units == a.units;
+    const long long bytes = static_cast<long long>(a.heads) * units * a.unit_bytes;
+    const int run = all ? 0x7FFFFFFF : units * a.unit_bytes;
+    const long long first = static_cast<long long>(piece) * kPiece, last = min(bytes, first + kPiece);
+    const char* from = a.base + static_cast<long long>(s) * a.heads * step;
+    char* to = a.base + static_cast<long long>(d) * a.heads * step;
+    if (a.granule == 16) copy_runs<uint4>(from, to, a.heads, step, run, first, last);
+    else if (a.granule == 4) copy_runs<uint32_t>(from, to, a.heads, step, run, first, last);
+    else if (a.granule == 2) copy_runs<uint16_t>(from, to, a.heads, step, run, first, last);
+    else copy_runs<uint8_t>(from, to, a.heads, step, run, first, last);
+  }
+}
+
+}  // namespace
+
+extern "C" int ptd_page_fork(const ptd_page_state* state, int32_t* refs, const int32_t* from, const int32_t* len,
+                             int32_t* table_next, int32_t* held_next, int32_t* copy_src, int32_t* copy_dst,
+                             int32_t* copy_rows, int32_t* dev_status, void* stream) {
+  ForkArgs g = {};
+  const int rc = ptd_check_state(state, &g.page_shift);
+  if (rc != PTD_OK) return rc;
+  PTD_RETURN_IF(!refs || !from || !len || !table_next || !held_next || !copy_src || !copy_dst || !copy_rows, PTD_ERR_NULL);
+  PTD_RETURN_IF(table_next == state->page_table || held_next == state->num_held, PTD_ERR_SHAPE);
+  g.s = *state;
+  g.refs = refs;
+  g.from = from;
+  g.len = len;
+  g.table_next = table_next;
+  g.held_next = held_next;
+  g.copy_src = copy_src;
+  g.copy_dst = copy_dst;
+  g.copy_rows = copy_rows;
+  g.dev_status = dev_status;
+  hipLaunchKernelGGL(k_page_fork, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), g);
+  return ptd_launch_status();
+}
+
+extern "C" int ptd_page_compact(const ptd_page_state* state, int32_t* refs, int32_t* move_src, int32_t* move_dst,
+                                int32_t* dev_status, void* stream) {
+  CompactArgs g = {};
+  int shift = 0;
+  const int rc = ptd_check_state(state, &shift);
+  if (rc != PTD_OK) return rc;
+  PTD_RETURN_IF(!refs || (state->num_pages > 1 && (!move_src || !move_dst)), PTD_ERR_NULL);
+  g.s = *state;
+  g.refs = refs;
+  g.move_src = move_src;
+  g.move_dst = move_dst;
+  g.dev_status = dev_status;
+  hipLaunchKernelGGL(k_page_compact, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), g);
+  return ptd_launch_status();
+}
+
+extern "C" int ptd_page_copy(const ptd_page_array* arrays, int32_t num_arrays, int32_t num_pages, int32_t n,
+                             const int32_t* src, const int32_t* dst, const int32_t* rows, int32_t* dev_status,
+                             void* stream) {
+  PTD_RETURN_IF(num_arrays < 0 || num_pages < 1 || n < 0, PTD_ERR_SHAPE);
+  if (num_arrays == 0 || n == 0) return PTD_OK;
+  PTD_RETURN_IF(!arrays || !src || !dst, PTD_ERR_NULL);
+  for (int i = 0; i < num_arrays; ++i) {
+    const ptd_page_array& x = arrays[i];
+    PTD_RETURN_IF(!x.base, PTD_ERR_NULL);
+    PTD_RETURN_IF(x.heads < 1 || x.units < 1 || x.unit_rows < 1 || x.unit_bytes < 1, PTD_ERR_SHAPE);
+    // a page is below 2^31 bytes
+    PTD_RETURN_IF(static_cast<long long>(x.units) * x.unit_bytes > 0x7FFFFFFFLL / x.heads, PTD_ERR_SHAPE);
+  }
+  for (int first = 0; first < num_arrays; first += kArrays) {
+    CopyArgs g = {};
+    const int m = std::min(kArrays, num_arrays - first);
+    long long most = 0;
+    for (int i = 0; i < m; ++i) {
+      const ptd_page_array& x = arrays[first + i];
+      // the widest loads that every unit of every page is aligned for
+      const uintptr_t any = reinterpret_cast<uintptr_t>(x.base) | static_cast<uintptr_t>(x.unit_bytes);
+      g.arrays[i] = {static_cast<char*>(x.base), x.heads, x.units, x.unit_rows, x.unit_bytes,
+                     any % 16 == 0 ? 16 : any % 4 == 0 ? 4 : any % 2 == 0 ? 2 : 1};
+      most = std::max(most, static_cast<long long>(x.heads) * x.units * x.unit_bytes);
+    }
+    g.src = src;
+    g.dst = dst;
+    g.rows = rows;
+    g.dev_status = dev_status;
+    g.n = n;
+    g.num_pages = num_pages;
+    g.pieces = static_cast<int>((most + kPiece - 1) / kPiece);
+    const long long items = static_cast<long long>(n) * g.pieces;
+    const unsigned gx = static_cast<unsigned>(std::min<long long>(items, std::max(1, 4096 / m)));
+    hipLaunchKernelGGL(k_page_copy, dim3(gx, m), dim3(kCopyThreads), 0, static_cast<hipStream_t>(stream), g);
+    const int rc = ptd_launch_status();
+    if (rc != PTD_OK) return rc;
+  }
+  return PTD_OK;
+}

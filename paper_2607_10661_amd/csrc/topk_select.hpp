@@ -1,0 +1,403 @@
+// Selection of the best entries of a slice of a row whose elements a workgroup holds in
+// registers (ptd_topk_argmax, ptd_token_logprobs).
+//
+// Order: value descending, equal values by the lower vocabulary index, -0.0
+// equal to +0.0.  Each element becomes one 64-bit key
+//   key = orderable(value) << 32 | ~index
+// so the required order is plain unsigned comparison of keys, and every key of
+// a row is distinct.
+#pragma once
+
+#include "ptd_async.hpp"
+#include "ptd_common.hpp"
+
+namespace ptd {
+
+__device__ __forceinline__ uint64_t make_key(uint32_t bits, uint32_t idx) {
+  if (bits == 0x80000000u) bits = 0u;  // -0.0 ties with +0.0
+  const uint32_t ord = (bits & 0x80000000u) ? ~bits : (bits | 0x80000000u);
+  return (static_cast<uint64_t>(ord) << 32) | static_cast<uint32_t>(~idx);
+}
+__device__ __forceinline__ uint32_t key_index(uint64_t key) {
+  return ~static_cast<uint32_t>(key);
+}
+
+// Order-preserving image of a float (the upper half of a key): larger value
+// <=> larger image, -0 maps like +0.  Empty list slots hold 0, below every
+// real value (including -inf).
+__device__ __forceinline__ uint32_t ord_of(float x) {
+  uint32_t bits = __float_as_uint(x);
+  if (bits == 0x80000000u) bits = 0u;
+  return (bits & 0x80000000u) ? ~bits : (bits | 0x80000000u);
+}
+template <int KMAX>
+__device__ __forceinline__ void insert(uint64_t (&l)[KMAX], uint64_t key) {
+  if (key > l[KMAX - 1]) {
+    l[KMAX - 1] = key;
+#pragma unroll
+    for (int j = KMAX - 1; j > 0; --j) {
+      if (l[j] > l[j - 1]) {
+        const uint64_t t = l[j];
+        l[j] = l[j - 1];
+        l[j - 1] = t;
+      }
+    }
+  }
+}
+
+// Top-KMAX of two descending lists, left in `a` (descending): the
+// elementwise max of a and reversed b is a bitonic sequence holding the top
+// KMAX, which a bitonic merge network sorts.
+template <int KMAX>
+__device__ __forceinline__ void merge_lists(uint64_t (&a)[KMAX], const uint64_t (&b)[KMAX]) {
+#pragma unroll
+  for (int i = 0; i < KMAX; ++i) a[i] = a[i] > b[KMAX - 1 - i] ? a[i] : b[KMAX - 1 - i];
+#pragma unroll
+  for (int j = KMAX / 2; j > 0; j >>= 1)
+#pragma unroll
+    for (int i = 0; i < KMAX; ++i)
+      if ((i & j) == 0 && a[i] < a[i + j]) {
+        const uint64_t t = a[i];
+        a[i] = a[i + j];
+        a[i + j] = t;
+      }
+}
+
+// After the butterfly every lane holds the wave's top KMAX, descending.
+template <int KMAX>
+__device__ __forceinline__ void wave_merge(uint64_t (&l)[KMAX]) {
+#pragma unroll
+  for (int o = 1; o < PTD_WAVE; o <<= 1) {
+    uint64_t other[KMAX];
+#pragma unroll
+    for (int i = 0; i < KMAX; ++i) other[i] = ptd::shfl_xor_u64(l[i], o);
+    merge_lists<KMAX>(l, other);
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t elem_bits(const void* base, size_t i) {
+  if constexpr (BF16) return static_cast<uint32_t>(static_cast<const uint16_t*>(base)[i]) << 16;
+  else return static_cast<const uint32_t*>(base)[i];
+}
+
+// Where the slice of a row lies that a workgroup of NT threads holds: whole 16-byte chunks,
+// chunk u of a thread being u * NT + tid, and the elements before the first 16-byte boundary
+// and after the last whole chunk, one per thread.
+struct Slice {
+  int v0, v1;   // elements of the row
+  int head;     // elements before the first boundary
+  int vb;       // first element of chunk 0
+  int nfull;    // whole chunks
+  int vt;       // the thread's edge element, ...
+  bool tail;    // ... if it has one
+};
+template <bool BF16>
+__device__ __forceinline__ Slice slice_at(const char* rb, int v0, int v1, int tid) {
+  constexpr int E = BF16 ? 8 : 4, ES = BF16 ? 2 : 4;
+  Slice s;
+  s.v0 = v0;
+  s.v1 = v1;
+  // elements before the slice's first 16-byte boundary (0 for aligned rows).
+  // Rows of an odd length, or a view, start anywhere; the chunks stay aligned
+  // loads and only the edges are read by element (65 rows x 32003 bf16, per
+  // call: 5.5 us against 98 for a wave per row reading elements)
+  const char* sb = rb + static_cast<size_t>(v0) * ES;
+  s.head = min(v1 - v0, static_cast<int>((0u - static_cast<uint32_t>(reinterpret_cast<uintptr_t>(sb))) & 15u) / ES);
+  s.vb = v0 + s.head;
+  s.nfull = (v1 - s.vb) / E;
+  // the edge elements, one per lane: the head, then the last partial chunk
+  s.vt = tid < s.head ? v0 + tid : s.vb + s.nfull * E + (tid - s.head);
+  s.tail = s.vt < v1;
+  return s;
+}
+// The thread's chunks; all loads are issued before any wait (past the end: the slice's last
+// chunk, never examined).
+template <bool BF16, int NT, int NL>
+__device__ __forceinline__ void load_chunks(uint4 (&cw)[NL], const char* rb, const Slice& s, int tid) {
+  constexpr int ES = BF16 ? 2 : 4;
+  if (s.nfull > 0) {
+    const uint4* src = reinterpret_cast<const uint4*>(rb + static_cast<size_t>(s.vb) * ES);
+#pragma unroll
+    for (int u = 0; u < NL; ++u) cw[u] = src[min(u * NT + tid, s.nfull - 1)];
+  } else {
+#pragma unroll
+    for (int u = 0; u < NL; ++u) cw[u] = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+constexpr int kCandCap = 256;                            // LDS candidate list
+constexpr int kListCap = 256;                            // LDS chunk list
+
+using s16x2 = short __attribute__((ext_vector_type(2)));
+
+// Images: order-preserving integers, 0 reserved for "no element".
+//   fp32: ord_of (-0 maps like +0).
+//   bf16: 0x8001 + v, v the 16-bit signed-order value (sign-magnitude turned
+//         into two's complement order by flipping the magnitude bits of
+//         negative values).  -0 maps one below +0, so a bound equal to the
+//         image of +0 is lowered to that of -0 before elements are compared.
+constexpr uint32_t kImgPosZeroBf16 = 0x8001u;
+__device__ __forceinline__ s16x2 sorder2(uint32_t d) {
+  const s16x2 v = __builtin_bit_cast(s16x2, d);
+  const s16x2 sg = v >> static_cast<short>(15);
+  return __builtin_bit_cast(s16x2, d ^ (__builtin_bit_cast(uint32_t, sg) & 0x7FFF7FFFu));
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t elem_img(uint32_t bits32) {  // bits of the fp32 value
+  if constexpr (BF16) {
+    const short h = static_cast<short>(bits32 >> 16);
+    const short o = static_cast<short>(h ^ ((h >> 15) & 0x7FFF));
+    return static_cast<uint32_t>(static_cast<int>(o) + 0x8001);
+  } else {
+    return ord_of(__uint_as_float(bits32));
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t chunk_img(const uint4& c) {
+  if constexpr (BF16) {
+    const s16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(sorder2(c.x), sorder2(c.y)),
+                                              __builtin_elementwise_max(sorder2(c.z), sorder2(c.w)));
+    return static_cast<uint32_t>(max(static_cast<int>(m.x), static_cast<int>(m.y)) + 0x8001);
+  } else {
+    return ord_of(fmaxf(fmaxf(__uint_as_float(c.x), __uint_as_float(c.y)),
+                        fmaxf(__uint_as_float(c.z), __uint_as_float(c.w))));
+  }
+}
+// fp32 bits of element e of a chunk
+template <bool BF16>
+__device__ __forceinline__ uint32_t chunk_bits(const uint4& c, int e) {
+  const uint32_t ws[4] = {c.x, c.y, c.z, c.w};
+  if constexpr (BF16) return (e & 1) ? (ws[e >> 1] & 0xFFFF0000u) : (ws[e >> 1] << 16);
+  else return ws[e];
+}
+// bound used in comparisons (see the bf16 image above)
+template <bool BF16>
+__device__ __forceinline__ uint32_t cmp_bound(uint32_t tau) {
+  return (BF16 && tau == kImgPosZeroBf16) ? tau - 1 : tau;
+}
+
+// Cross-lane steps of a wave on the vector ALU, level j pairing lanes that
+// differ in bit j: quad permutes (j = 0, 1), the half-row and row mirrors
+// (j = 2, 3: once the value is uniform over blocks of 2^j lanes, the mirror
+// partner lies in the other block), v_permlane16_swap / v_permlane32_swap
+// (j = 4, 5: with both operands holding the value, the two results are the
+// lane's value and its partner's).
+template <bool MAX, int J>
+__device__ __forceinline__ uint32_t lane_step(uint32_t x) {
+  constexpr int kCtrl[4] = {0xB1, 0x4E, 0x141, 0x140};  // quad_perm 1032, 2301, half-row, row mirror
+  if constexpr (J < 4) {
+    const uint32_t y = static_cast<uint32_t>(
+        __builtin_amdgcn_update_dpp(static_cast<int>(x), static_cast<int>(x), kCtrl[J], 0xF, 0xF, false));
+    return MAX ? max(x, y) : min(x, y);
+  } else {
+    const auto r = J == 4 ? __builtin_amdgcn_permlane16_swap(x, x, false, false)
+                          : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return MAX ? max(r[0], r[1]) : min(r[0], r[1]);
+  }
+}
+// Maximum over aligned groups of GL lanes, then minimum over the groups.
+template <int GL>
+__device__ __forceinline__ uint32_t group_max_min(uint32_t x) {
+  if constexpr (GL > 1) x = lane_step<true, 0>(x); else x = lane_step<false, 0>(x);
+  if constexpr (GL > 2) x = lane_step<true, 1>(x); else x = lane_step<false, 1>(x);
+  if constexpr (GL > 4) x = lane_step<true, 2>(x); else x = lane_step<false, 2>(x);
+  if constexpr (GL > 8) x = lane_step<true, 3>(x); else x = lane_step<false, 3>(x);
+  if constexpr (GL > 16) x = lane_step<true, 4>(x); else x = lane_step<false, 4>(x);
+  if constexpr (GL > 32) x = lane_step<true, 5>(x); else x = lane_step<false, 5>(x);
+  return x;
+}
+
+// LDS of the selection.
+template <int NT>
+struct TopkLds {
+  __attribute__((aligned(16))) uint4 ldata[kListCap];
+  uint64_t cand[kCandCap];
+  uint32_t bits[kCandCap];
+  uint32_t rank[kCandCap];
+  uint16_t list[kListCap];
+  __attribute__((aligned(16))) uint32_t tau[NT / PTD_WAVE];
+  __attribute__((aligned(16))) uint32_t tau2[NT / PTD_WAVE];
+  int nlist, cnt;
+};
+
+// The KMAX best entries of a slice that a workgroup of NT threads holds, NL chunks of 16 bytes
+// per lane: put(rank, key, bits of the fp32 value) is called once for each rank < KMAX (key 0: none).
+//   1. Every lane takes the image of each of its chunks (bf16 images are 16
+//      bits wide and computed two at a time with packed 16-bit integer
+//      operations) and their maximum.
+//   2. A lower bound tau of the slice's KMAX-th best value: the lanes of a
+//      wave form KMAX groups; each group's largest lane maximum is a distinct
+//      element, so the least of the KMAX group maxima is at most the KMAX-th
+//      best value.  The bound of the slice is the largest bound of its waves.
+//   3. Chunks whose image reaches tau are copied with their index to a list
+//      in LDS, then the workgroup examines the listed chunks a thread per
+//      element and appends the elements that reach tau to a candidate list.
+//      The edges of the slice (the elements before its first 16-byte
+//      boundary and after its last whole chunk, fewer than two chunks) are
+//      read with plain loads, one per lane, and checked the same way.
+//   4. The candidates are ranked by counting: the list is cut into parts,
+//      each thread counts the keys of one part above one candidate, and the
+//      counts are summed in LDS.  The candidates of rank below k are the
+//      result.  If either list overflows (many values tied at the top), every
+//      lane keeps a sorted list of its best keys among its own elements that
+//      reach tau, and the lists are merged.
+// Only listed chunks pass through LDS, so the slice is read from memory once
+// and LDS carries a few KB.  The kernel's loops stay rolled, which keeps its
+// code small: its instructions are fetched once per CU, cold.
+template <int KMAX, bool BF16, int NT, int NL, typename Put>
+__device__ __forceinline__ void topk_of_slice(TopkLds<NT>& sh, const uint4 (&cw)[NL], const char* rb, const Slice& s,
+                                              uint32_t bt, int tid, Put put) {
+  constexpr int E = BF16 ? 8 : 4;  // elements per 16-byte chunk
+  constexpr int NW = NT / PTD_WAVE;
+  static_assert(NT >= kCandCap && NW % 4 == 0 && NT * NL <= 65536, "workgroup shape");
+  static_assert((NT & (NT - 1)) == 0, "KMAX groups of NT / KMAX lanes");
+  constexpr int GL = PTD_WAVE / KMAX;  // lanes per group inside a wave
+  constexpr int GW = NT / KMAX;        // lanes per group across the workgroup
+  constexpr int GWL = GW < PTD_WAVE ? GW : PTD_WAVE;  // ... of them inside one wave
+  constexpr int WPG = GW / GWL;        // waves per workgroup-wide group
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (tid < kCandCap) sh.rank[tid] = 0;
+  if (tid == 0) {
+    sh.cnt = 0;
+    sh.nlist = 0;
+  }
+
+  // 1. chunk images and the lane maximum
+  uint32_t cm[NL];
+  uint32_t lm = s.tail ? elem_img<BF16>(bt) : 0u;
+#pragma unroll
+  for (int u = 0; u < NL; ++u) {
+    cm[u] = u * NT + tid < s.nfull ? chunk_img<BF16>(cw[u]) : 0u;
+    lm = max(lm, cm[u]);
+  }
+  // 2. the bound, the larger of two: per wave, max over groups of GL lanes
+  //    then min over the wave's KMAX groups, and the largest of these over
+  //    the waves; and min over KMAX groups of NT / KMAX lanes spanning the
+  //    workgroup of the group maxima (much closer to the KMAX-th best value
+  //    of the slice, hence few candidates; the first stays positive where a
+  //    short slice leaves whole workgroup-wide groups empty)
+  const uint32_t g = group_max_min<GL>(lm);
+  const uint32_t g2 = group_max_min<GWL>(lm);  // GWL = 64: the wave's maximum
+  if (lane == 0) {
+    sh.tau[wave] = g;
+    sh.tau2[wave] = g2;
+  }
+  ptd::lds_barrier();
+  uint32_t tau = 0;
+#pragma unroll
+  for (int i = 0; i < NW; i += 4) {
+    const uint4 t4 = *reinterpret_cast<const uint4*>(sh.tau + i);
+    tau = max(max(tau, max(t4.x, t4.y)), max(t4.z, t4.w));
+  }
+  uint32_t tau2 = ~0u;
+#pragma unroll
+  for (int j = 0; j < NW / WPG; ++j) {
+    uint32_t gm = 0;
+#pragma unroll
+    for (int w = 0; w < WPG; ++w) gm = max(gm, sh.tau2[j * WPG + w]);
+    tau2 = min(tau2, gm);
+  }
+  tau = max(tau, tau2);
+  const uint32_t tc = cmp_bound<BF16>(tau);
+
+  // 3. list the chunks that reach the bound, then examine them
+  auto append = [&](uint32_t bits, int v) {
+    const int pos = atomicAdd(&sh.cnt, 1);
+    if (pos < kCandCap) {
+      sh.cand[pos] = make_key(bits, static_cast<uint32_t>(v));
+      sh.bits[pos] = bits;
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < NL; ++u) {
+    if (cm[u] != 0 && cm[u] >= tc) {
+      const int pos = atomicAdd(&sh.nlist, 1);
+      if (pos < kListCap) {
+        sh.ldata[pos] = cw[u];
+        sh.list[pos] = static_cast<uint16_t>(u * NT + tid);
+      }
+    }
+  }
+  if (s.tail && elem_img<BF16>(bt) >= tc) append(bt, s.vt);
+  ptd::lds_barrier();
+  const int nl = sh.nlist;
+  if (nl <= kListCap) {  // uniform
+    for (int i0 = 0; i0 < nl; i0 += NT / E) {
+      const int i = i0 + tid / E;
+      if (i < nl) {
+        const int c = sh.list[i], e = tid & (E - 1);
+        const uint32_t bits = BF16 ? static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(sh.ldata + i)[e]) << 16
+                                   : reinterpret_cast<const uint32_t*>(sh.ldata + i)[e];
+        if (elem_img<BF16>(bits) >= tc) append(bits, s.vb + c * E + e);
+      }
+    }
+  }
+  __syncthreads();
+  const int n = sh.cnt;
+
+  // 4. selection
+  if (nl <= kListCap && n <= kCandCap) {  // uniform over the workgroup
+    int n2 = PTD_WAVE;  // candidates per part-set: a power of two >= n
+    while (n2 < n) n2 <<= 1;
+    const int parts = NT / n2;
+    const int i = tid & (n2 - 1), p = tid / n2;  // p is uniform over a wave
+    const int len = (n + parts - 1) / parts;
+    const int j0 = p * len, j1 = min(n, j0 + len);
+    const uint64_t mine = i < n ? sh.cand[i] : ~0ull;
+    uint32_t above = 0;
+    for (int j = j0; j < j1; ++j) above += sh.cand[j] > mine ? 1u : 0u;
+    if (above) atomicAdd(&sh.rank[i], above);
+    __syncthreads();
+    if (tid < n) {
+      const uint32_t rank = sh.rank[tid];
+      const uint64_t key = sh.cand[tid];
+      if (rank < static_cast<uint32_t>(KMAX)) put(static_cast<int>(rank), key, sh.bits[tid]);
+    } else if (tid < KMAX) {  // fewer candidates than KMAX
+      put(tid, 0ull, 0u);
+    }
+    return;
+  }
+
+  // overflow: per-lane sorted lists of the lane's own elements that reach tau
+  uint64_t l[KMAX];
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j) l[j] = 0;
+#pragma unroll
+  for (int u = 0; u < NL; ++u) {
+    const int c = u * NT + tid;
+    if (c < s.nfull) {
+      const int v = s.vb + c * E;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint32_t bits = chunk_bits<BF16>(cw[u], e);
+        const uint64_t key = make_key(bits, static_cast<uint32_t>(v + e));
+        if (elem_img<BF16>(bits) >= tc && key > l[KMAX - 1]) insert<KMAX>(l, key);
+      }
+    }
+  }
+  if (s.tail) {
+    const uint64_t key = make_key(bt, static_cast<uint32_t>(s.vt));
+    if (key > l[KMAX - 1]) insert<KMAX>(l, key);
+  }
+  wave_merge<KMAX>(l);
+  if (lane < KMAX) {
+    uint64_t mine = 0;
+#pragma unroll
+    for (int r = 0; r < KMAX; ++r) mine = (lane == r) ? l[r] : mine;
+    sh.cand[wave * KMAX + lane] = mine;  // every wave is past its reads of sh.cand
+  }
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int j = 0; j < KMAX; ++j) l[j] = 0;
+  for (int i = lane; i < NW * KMAX; i += PTD_WAVE) insert<KMAX>(l, sh.cand[i]);
+  wave_merge<KMAX>(l);
+  uint64_t mine = 0;
+#pragma unroll
+  for (int r = 0; r < KMAX; ++r) mine = (lane == r) ? l[r] : mine;
+  if (lane < KMAX) put(lane, mine, mine ? elem_bits<BF16>(rb, key_index(mine)) : 0u);
+}
+
+}  // namespace ptd
