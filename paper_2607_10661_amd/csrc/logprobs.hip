@@ -26,9 +26,11 @@ namespace {
 
 using namespace ptd;
 
-constexpr int kThreads = 512;       // of k_logp_row
+constexpr int kThreads = 256;       // of k_logp_row
 constexpr int kMergeThreads = 256;  // of k_logp_merge: the most (slices x best entries) of a row
+constexpr int kMergeSlices = 8;
 constexpr int kMaxVocab = 262144;
+constexpr int kPartChunks = 4;      // k_logp_path: tokens of a lane at once
 
 struct LogpArgs {
   const void* logits;
@@ -45,34 +47,37 @@ struct LogpArgs {
   double unscale;          // inv_tau / scale
   float scale;             // log2(e) / temperature, rounded
   int R, V, T, k, slices, slice_len;
+  int part_rows, ways;     // k_logp_path
 };
 
-// Sums of a slice: its maximum, how many entries equal it, sum e^d of the others and sum d e^d.
+// Sums of a slice: its maximum, how many entries equal it, sum e^d of the others and sum d e^d, and
+// the given token's logit where the slice holds it.
 struct Sums {
   float m, ones;
   double rest, weighted;
+  float token_logit;
 };
 
 // Row of logits that entry r reads, and its token; row -1: the entry stands for nothing.
 __device__ __forceinline__ int entry_row(const LogpArgs& a, int r, int* token, bool tell) {
   *token = -1;
   if (!a.tokens) return r;
-  const int t = a.tokens[r];
-  if (t < 0 || t >= a.V) {
+  int t = a.tokens[r], row = r;
+  if (a.nodes) {  // (loaded whether it is needed or not: the token is one more wait)
+    const int b = r / (a.T + 1), j = r - b * (a.T + 1);
+    const int n = j > 0 ? a.nodes[r - b - 1] : -1;
+    row = r - j + n + 1;
+    if (j > 0 && static_cast<uint32_t>(n) >= static_cast<uint32_t>(a.T) && static_cast<uint32_t>(t) < static_cast<uint32_t>(a.V)) {
+      if (tell) report(a.dev_status, PTD_ERR_ROWS);
+      t = -1;
+    }
+  }
+  if (static_cast<uint32_t>(t) >= static_cast<uint32_t>(a.V)) {
     if (t != -1 && tell) report(a.dev_status, PTD_ERR_VALUE);
     return -1;
   }
   *token = t;
-  if (!a.nodes) return r;
-  const int b = r / (a.T + 1), j = r - b * (a.T + 1);
-  if (j == 0) return r;
-  const int n = a.nodes[static_cast<size_t>(b) * a.T + j - 1];
-  if (n < 0 || n >= a.T) {
-    if (tell) report(a.dev_status, PTD_ERR_ROWS);
-    *token = -1;
-    return -1;
-  }
-  return r - j + n + 1;
+  return row;
 }
 
 // The value that an image stands for (elem_img, chunk_img).
@@ -86,6 +91,32 @@ __device__ __forceinline__ float image_value(uint32_t img) {
   }
 }
 
+__device__ __forceinline__ double reciprocal(double x) {
+  const double r = __builtin_amdgcn_rcp(x);
+  return fma(fma(-x, r, 1.0), r, r);
+}
+// log(1 + t), t >= 0 (the results are fp32; the device library's takes several times the instructions,
+// which a workgroup that runs once fetches from memory): the series of log((1 + z) / (1 - z)) = 2
+// (z + z^3 / 3 + ...), with z = t / (2 + t) below 1/5 where t is below 1/2, else of the mantissa
+// of 1 + t; what follows z^13 is below 2^-32 of z.
+__device__ __forceinline__ double log1p_of(double t) {
+  const bool small = t < 0.5;
+  const double s = 1.0 + t;
+  double f = __builtin_amdgcn_frexp_mant(s);
+  int e = __builtin_amdgcn_frexp_exp(s);
+  if (f < 0.70710678118654752) f *= 2.0, e -= 1;
+  const double z = (small ? t : f - 1.0) * reciprocal(small ? 2.0 + t : f + 1.0);
+  const double q = z * z;
+  double p = 1.0 / 13.0;
+  p = fma(p, q, 1.0 / 11.0);
+  p = fma(p, q, 1.0 / 9.0);
+  p = fma(p, q, 1.0 / 7.0);
+  p = fma(p, q, 1.0 / 5.0);
+  p = fma(p, q, 1.0 / 3.0);
+  const double l = 2.0 * fma(p * q, z, z);
+  return small ? l : fma(static_cast<double>(e), 0.69314718055994531, l);
+}
+
 // One entry's results from its row's sums.
 struct Totals {
   double log_s, total;
@@ -95,7 +126,7 @@ __device__ __forceinline__ Totals totals_of(const Sums& s) {
   Totals t;
   t.m = s.m;
   t.total = s.ones + s.rest;
-  t.log_s = log1p(static_cast<double>(s.ones) - 1.0 + s.rest);
+  t.log_s = log1p_of(static_cast<double>(s.ones) - 1.0 + s.rest);
   if (s.m == INFINITY) t.log_s = NAN;  // (the infinities' own terms are no numbers)
   return t;
 }
@@ -105,7 +136,12 @@ __device__ __forceinline__ float logprob_of(const LogpArgs& a, const Totals& t, 
 }
 __device__ __forceinline__ void put_entry(const LogpArgs& a, int r, const Totals& t, double weighted, float x) {
   if (a.logprob) a.logprob[r] = logprob_of(a, t, x);
-  if (a.entropy) a.entropy[r] = t.m == -INFINITY ? 0.f : static_cast<float>(t.log_s - weighted / t.total);
+  if (a.entropy) a.entropy[r] = t.m == -INFINITY ? 0.f : static_cast<float>(t.log_s - weighted * reciprocal(t.total));
+}
+__device__ __forceinline__ void put_best(const LogpArgs& a, int r, int rank, const Totals& t, uint64_t key, uint32_t bits) {
+  const size_t at = static_cast<size_t>(r) * a.k + rank;
+  if (a.topk_idx) a.topk_idx[at] = static_cast<int32_t>(key_index(key));  // (no key: -1)
+  if (a.topk_val) a.topk_val[at] = key ? logprob_of(a, t, __uint_as_float(bits)) : NAN;
 }
 __device__ __forceinline__ void put_nothing(const LogpArgs& a, int r, int tid) {
   if (tid == 0 && a.logprob) a.logprob[r] = 0.f;
@@ -124,96 +160,210 @@ __device__ __forceinline__ uint64_t* keys_of(const LogpArgs& a, long long item) 
 
 struct NoLds {};
 
-template <int KMAX, bool BF16, int NL>
-__global__ void __launch_bounds__(kThreads) k_logp_row(LogpArgs a) {
-  constexpr int E = BF16 ? 8 : 4, NW = kThreads / PTD_WAVE;
-  __shared__ typename std::conditional<(KMAX > 0), TopkLds<kThreads>, NoLds>::type sh;
-  __shared__ uint32_t s_max[NW];
-  __shared__ Sums s_sums[NW];
-  __shared__ Totals s_tot;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
-  int token;
-  const int row = entry_row(a, r, &token, tid == 0 && slice == 0);
-  if (row < 0) {  // uniform
-    if (a.slices == 1) put_nothing(a, r, tid);
-    return;
+// A wave's sums: of 2^(l * scale - c) and of that times the exponent, its largest entry, and
+// (ones > 0) how many entries equal to the slice's largest were taken out of them.
+struct WaveSums {
+  float c, sum, weighted, top, ones;
+};
+
+// What a workgroup keeps of the entry that it works on.
+template <int KMAX>
+struct RowLds {
+  typename std::conditional<(KMAX > 0), TopkLds<kThreads>, NoLds>::type topk;
+  WaveSums sums[kThreads / PTD_WAVE];
+  Totals totals;
+};
+
+template <bool BF16, int NL, typename Add>
+__device__ __forceinline__ void each_element(const uint4 (&cw)[NL], const Slice& sl, uint32_t bt, int tid, Add add) {
+#pragma unroll
+  for (int u = 0; u < NL; ++u) {
+    if (u * kThreads + tid < sl.nfull) {
+#pragma unroll
+      for (int e = 0; e < (BF16 ? 8 : 4); ++e) add(__uint_as_float(chunk_bits<BF16>(cw[u], e)));
+    }
   }
+  if (sl.tail) add(__uint_as_float(bt));
+}
+
+// The sums with care, relative to the wave's largest entry: entries that equal m are counted and
+// left out, and so is what lies so far below it that it has no weight (-inf; the type's lowest
+// number overflows to it).
+template <bool BF16, int NL>
+__device__ __forceinline__ WaveSums careful_sums(uint4 (&cw)[NL], const Slice& sl, uint32_t bt, int tid, float top, float m, float scale) {
+  float r = 0.f, w = 0.f, n = 0.f;
+  const float c = top * scale;
+  const float none = __uint_as_float(__float_as_uint(-1.2e6f / scale) & 0xFFFF0000u);  // its exponent is -1.1e6 or less
+  // (where c is larger no entry but the largest has a weight: its distance is at least 2^-23 of c)
+  const bool near = fabsf(c) < 0x1p30f;
+  each_element<BF16, NL>(cw, sl, bt, tid, [&](float x) __attribute__((always_inline)) {
+    const float arg = fmaf(x < none ? none : x, scale, -c);
+    const float e = near ? __builtin_amdgcn_exp2f(arg) : x == top ? 1.f : 0.f;
+    const bool one = x == m;
+    n += one ? 1.f : 0.f;
+    r += one ? 0.f : e;
+    w += one || !near ? 0.f : e * arg;
+  });
+  if (!(fabsf(top) < INFINITY)) r = top - top;  // not a number
+  return {c, wave_sum_dpp(r), wave_sum_dpp(w), top, wave_sum_dpp(n)};
+}
+
+// One slice of the row that entry r reads.  A wave's terms are relative to the largest entry of its
+// first chunks, so they are worked out while the other chunks are on their way; a wave whose
+// later entries lie far above, or whose weighted sum is no number (masked entries), takes
+// them once more with care.  So does the wave with the row's largest entry where that makes up most of
+// its sum.
+template <int KMAX, bool BF16, int NL, bool ONE>
+__device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, int r, int row, int token, int slice, int tid) {
+  constexpr int NW = kThreads / PTD_WAVE;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const char* rb = static_cast<const char*>(a.logits) + static_cast<size_t>(row) * a.ld * (BF16 ? 2 : 4);
   const int v0 = slice * a.slice_len;
   const Slice sl = slice_at<BF16>(rb, v0, min(a.V, v0 + a.slice_len), tid);
   uint4 cw[NL];
   load_chunks<BF16, kThreads, NL>(cw, rb, sl, tid);
   const uint32_t bt = sl.tail ? elem_bits<BF16>(rb, sl.vt) : 0u;
-  const float xt = token >= 0 && a.slices == 1 ? __uint_as_float(elem_bits<BF16>(rb, token)) : 0.f;
-
-  // the largest element
+  // (by every thread, or none: a wait less where it is needed)
+  const float xt = token >= sl.v0 && token < sl.v1 ? __uint_as_float(elem_bits<BF16>(rb, token)) : 0.f;
+  // (short slices: the edge elements and the first chunk may be all that a wave has, or nothing)
+  const uint32_t first = max(tid < sl.nfull ? chunk_img<BF16>(cw[0]) : 0u, NL == 1 || sl.nfull < kThreads ? (sl.tail ? elem_img<BF16>(bt) : 0u) : 0u);
+  const float ref = image_value<BF16>(group_max_min<64>(first));
+  const float c = ref * a.scale;
+  float sum = 0.f, weighted = 0.f;
+  each_element<BF16, NL>(cw, sl, bt, tid, [&](float x) __attribute__((always_inline)) {
+    const float arg = fmaf(x, a.scale, -c);
+    const float e = __builtin_amdgcn_exp2f(arg);
+    sum += e;
+    weighted = fmaf(e, arg, weighted);
+  });
   uint32_t lm = sl.tail ? elem_img<BF16>(bt) : 0u;
 #pragma unroll
   for (int u = 0; u < NL; ++u) lm = max(lm, u * kThreads + tid < sl.nfull ? chunk_img<BF16>(cw[u]) : 0u);
-  const uint32_t wm = group_max_min<64>(lm);
-  if (lane == 0) s_max[wave] = wm;
+  const uint32_t img = group_max_min<64>(lm);
+  const float top = img ? image_value<BF16>(img) : -INFINITY;  // (a wave without an element)
+  sum = wave_sum_dpp(sum);
+  weighted = wave_sum_dpp(weighted);
+  bool care = !(weighted - weighted == 0.f) || !((top - ref) * a.scale <= 8.f) || !(fabsf(c) < 0x1p20f);
+  if (lane == 0) sh.sums[wave] = {c, sum, weighted, top, 0.f};
+  if constexpr (KMAX > 0) topk_groups<KMAX, kThreads>(sh.topk, lm, tid);
   lds_barrier();
-  uint32_t top = 0;
+  uint32_t tc = 0;
+  if constexpr (KMAX > 0) tc = topk_list<KMAX, BF16, kThreads, NL>(sh.topk, cw, sl, bt, tid);
+  float m = sh.sums[0].top;
+  bool nan = m != m;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) top = max(top, s_max[w]);
-  const float m = image_value<BF16>(top);
-
-  // the sums.  Only a wave that holds an entry equal to m looks for it.
-  float ones = 0.f, rest = 0.f, weighted = 0.f;
-  if (m != -INFINITY) {
-    auto add = [&](float x, bool find) __attribute__((always_inline)) {
-      const float arg = (x - m) * a.scale;
-      const float e = __builtin_amdgcn_exp2f(arg);
-      // (an entry at -inf has no weight, and e of a NaN is one)
-      weighted = fmaf(e, fmaxf(arg, -1e30f), weighted);
-      if (find && x == m) ones += 1.f;
-      else rest += e;
-    };
-    auto all = [&](bool find) __attribute__((always_inline)) {
-#pragma unroll
-      for (int u = 0; u < NL; ++u) {
-        if (u * kThreads + tid < sl.nfull) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) add(__uint_as_float(chunk_bits<BF16>(cw[u], e)), find);
-        }
-      }
-      if (sl.tail) add(__uint_as_float(bt), find);
-    };
-    if (wm == top) all(true);  // uniform over the wave
-    else all(false);
+  for (int w = 1; w < NW; ++w) {
+    const float x = sh.sums[w].top;
+    nan |= x != x;
+    m = fmaxf(m, x);
   }
-  ones = wave_sum(ones);
-  rest = wave_sum(rest);
-  weighted = wave_sum(weighted);
-  if (lane == 0) s_sums[wave] = {m, ones, rest, weighted};
+  if (nan) m = NAN;
+  // e of the largest entry is 2^(top * scale - c)
+  care |= top == m && !(sum >= 2.f * __builtin_amdgcn_exp2f(fmaf(top, a.scale, -c)));
+  lds_barrier();  // sh.sums is read
+  if (top == -INFINITY) {
+    if (lane == 0) sh.sums[wave] = {0.f, 0.f, 0.f, top, 0.f};
+  } else if (care) {
+    const WaveSums s = careful_sums<BF16, NL>(cw, sl, bt, tid, top, m, a.scale);
+    if (lane == 0) sh.sums[wave] = s;
+  }
+  if constexpr (KMAX > 0) topk_examine<BF16, kThreads>(sh.topk, sl, tc, tid);
   lds_barrier();
-  if (tid == 0) {
-    Sums s = s_sums[0];
+  if (wave == 0) {
+    // to the slice's largest entry: one lane per wave's sums
+    const WaveSums s = sh.sums[min(lane, NW - 1)];
+    const bool has = lane < NW && s.top != -INFINITY;
+    const double d = (fabsf(s.c) < 0x1p30f ? static_cast<double>(s.c) : static_cast<double>(s.top) * a.scale) - static_cast<double>(m) * a.scale;
+    const double f = has ? static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(d))) : 0.0;
+    double rest = has ? f * s.sum : 0.0, wt = has ? f * (s.weighted + d * s.sum) : 0.0;
+    float ones = has ? s.ones : 0.f;
+    // the largest entry, where it was not taken out: one of it, as the sums hold it
+    const uint64_t in = __ballot(has && s.top == m && s.ones == 0.f);
 #pragma unroll
-    for (int w = 1; w < NW; ++w) s.ones += s_sums[w].ones, s.rest += s_sums[w].rest, s.weighted += s_sums[w].weighted;
-    s.weighted *= a.unscale;
-    if (a.slices > 1) {
-      static_cast<Sums*>(a.part)[blockIdx.x] = s;
-    } else {
-      const Totals t = totals_of(s);
-      s_tot = t;
-      put_entry(a, r, t, s.weighted, xt);
+    for (int o = 1; o < NW; o <<= 1) {
+      rest += __shfl_xor(rest, o, PTD_WAVE);
+      wt += __shfl_xor(wt, o, PTD_WAVE);
+      ones += __shfl_xor(ones, o, PTD_WAVE);
+    }
+    if (in && ones == 0.f) ones = 1.f, rest -= 1.0;
+    if (lane == 0) {
+      const Sums t = {m, ones, rest, wt * a.unscale, xt};
+      if constexpr (ONE) {
+        sh.totals = totals_of(t);
+        put_entry(a, r, sh.totals, t.weighted, xt);
+      } else {
+        static_cast<Sums*>(a.part)[static_cast<size_t>(r) * a.slices + slice] = t;
+      }
     }
   }
   if constexpr (KMAX > 0) {
-    topk_of_slice<KMAX, BF16, kThreads, NL>(sh, cw, rb, sl, bt, tid, [&](int rank, uint64_t key, uint32_t bits) {
-      if (a.slices > 1) {
-        uint64_t* q = keys_of<KMAX>(a, blockIdx.x) + 2 * rank;
-        q[0] = key;
-        q[1] = bits;
-      } else if (rank < a.k) {
-        const size_t at = static_cast<size_t>(r) * a.k + rank;
-        if (a.topk_idx) a.topk_idx[at] = static_cast<int32_t>(key_index(key));
-        if (a.topk_val) a.topk_val[at] = key ? logprob_of(a, s_tot, __uint_as_float(bits)) : NAN;
+    topk_pick<KMAX, BF16, kThreads>(
+        sh.topk, rb, sl, tid, [&] { topk_in_turns<KMAX, BF16, kThreads>(sh.topk, rb, sl, tid); },
+        [&](int rank, uint64_t key, uint32_t bits) {
+          if constexpr (ONE) {
+            if (rank < a.k) put_best(a, r, rank, sh.totals, key, bits);
+          } else {
+            uint64_t* q = keys_of<KMAX>(a, static_cast<long long>(r) * a.slices + slice) + 2 * rank;
+            q[0] = key;
+            q[1] = bits;
+          }
+        });
+  }
+}
+
+template <int KMAX, bool BF16, int NL, bool ONE>
+__global__ void __launch_bounds__(kThreads, 4) k_logp_row(LogpArgs a) {
+  __shared__ RowLds<KMAX> sh;
+  const int tid = threadIdx.x;
+  const int r = ONE ? blockIdx.x : blockIdx.x / a.slices, slice = ONE ? 0 : blockIdx.x - r * a.slices;
+  int token;
+  const int row = entry_row(a, r, &token, tid == 0 && slice == 0);
+  if (row < 0) {  // uniform
+    if (ONE) put_nothing(a, r, tid);
+    return;
+  }
+  row_slice<KMAX, BF16, NL, ONE>(a, sh, r, row, token, slice, tid);
+}
+
+// Entries along paths: few of a sequence's T + 1 are there, and the host does not know which.
+// Workgroup (a few sequences, i, slice) takes the i-th of those that are, then every `ways`-th.
+template <int KMAX, bool BF16, int NL, bool ONE>
+__global__ void __launch_bounds__(kThreads, 4) k_logp_path(LogpArgs a) {
+  __shared__ RowLds<KMAX> sh;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int slice = ONE ? 0 : blockIdx.x % a.slices, g = ONE ? blockIdx.x : blockIdx.x / a.slices;
+  const int part = g / a.ways, way = g % a.ways;
+  const int r0 = part * a.part_rows, n = min(a.part_rows, a.R - r0);
+  const bool tell = way == 0 && slice == 0 && tid < PTD_WAVE;
+  int seen = 0;
+  for (int j0 = 0; j0 < n; j0 += kPartChunks * PTD_WAVE) {  // uniform: every wave reads the same tokens
+    int rows[kPartChunks], tokens[kPartChunks];
+#pragma unroll
+    for (int u = 0; u < kPartChunks; ++u) {
+      const int j = j0 + u * PTD_WAVE + lane;
+      rows[u] = tokens[u] = -1;
+      if (j < n) rows[u] = entry_row(a, r0 + j, &tokens[u], tell);
+      // (of several slices: k_logp_merge)
+      if (ONE && tell && j < n && rows[u] < 0) {
+        for (int k = 0; k < max(a.k, 1); ++k) put_nothing(a, r0 + j, k);
       }
-    });
+    }
+#pragma unroll 1
+    for (int u = 0; u < kPartChunks; ++u) {
+      static_assert(kPartChunks == 4, "four of them");
+      const int row = u == 0 ? rows[0] : u == 1 ? rows[1] : u == 2 ? rows[2] : rows[3];
+      const int token = u == 0 ? tokens[0] : u == 1 ? tokens[1] : u == 2 ? tokens[2] : tokens[3];
+      for (uint64_t live = __ballot(row >= 0); live; live &= live - 1) {
+        const bool mine = seen == way;
+        seen = seen + 1 == a.ways ? 0 : seen + 1;
+        if (!mine) continue;
+        const int at = __builtin_ctzll(live);
+        row_slice<KMAX, BF16, NL, ONE>(a, sh, r0 + j0 + u * PTD_WAVE + at, __builtin_amdgcn_readlane(row, at),
+                                       __builtin_amdgcn_readlane(token, at), slice, tid);
+        lds_barrier();
+      }
+    }
   }
 }
 
@@ -223,12 +373,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_logp_merge(LogpArgs a) {
   __shared__ uint64_t s_key[kMergeThreads];
   __shared__ Totals s_tot;
   const int tid = threadIdx.x, r = blockIdx.x;
-  int token;
-  const int row = entry_row(a, r, &token, false);
-  if (row < 0) {
-    put_nothing(a, r, tid);
-    return;
-  }
+  // (loaded whether the entry is there or not: the token is one more wait)
   const int n = KMAX * a.slices;
   uint64_t key = 0;
   uint32_t bits = 0;
@@ -236,30 +381,36 @@ __global__ void __launch_bounds__(kMergeThreads) k_logp_merge(LogpArgs a) {
     const uint64_t* q = keys_of<KMAX>(a, static_cast<long long>(r) * a.slices) + 2 * tid;
     key = q[0];
     bits = static_cast<uint32_t>(q[1]);
-    s_key[tid] = key;
   }
+  Sums s = {-INFINITY, 0.f, 0.0, 0.0, 0.f};
+  if (tid < a.slices) s = static_cast<const Sums*>(a.part)[static_cast<size_t>(r) * a.slices + tid];
+  int token;
+  const int row = entry_row(a, r, &token, false);
+  if (row < 0) {
+    put_nothing(a, r, tid);
+    return;
+  }
+  if (KMAX > 0) s_key[tid] = key;  // (0: none)
   if (tid < PTD_WAVE) {
-    Sums s = {-INFINITY, 0.f, 0.0, 0.0};
-    if (tid < a.slices) s = static_cast<const Sums*>(a.part)[static_cast<size_t>(r) * a.slices + tid];
-    const float xt = token >= 0 ? __uint_as_float(elem_bits<BF16>(static_cast<const char*>(a.logits) + static_cast<size_t>(row) * a.ld * (BF16 ? 2 : 4), token)) : 0.f;
+    const float xt = __shfl(s.token_logit, token >= 0 ? token / a.slice_len : 0, PTD_WAVE);
     // (a NaN maximum stays one)
     bool nan = s.m != s.m;
     const float m = __any(nan) ? NAN : wave_max(s.m);
     // a slice's sums under the row's maximum: its terms are e^(m_slice - m) of what they were
     const double d = (static_cast<double>(s.m) - m) * a.inv_tau;
     const bool live = s.m != -INFINITY;
-    const double f = live ? exp(d) : 0.0;
+    const double f = live ? static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(d * 1.4426950408889634))) : 0.0;
     const double own = s.ones + s.rest;
     double ones = s.m == m ? s.ones : 0.0;
     double rest = live ? (s.m == m ? s.rest : own * f) : 0.0;
     double weighted = live ? f * s.weighted + (f > 0.0 ? f * d * own : 0.0) : 0.0;
-    for (int o = 32; o > 0; o >>= 1) {
+    for (int o = 1; o < a.slices; o <<= 1) {  // (lanes past the slices hold nothing)
       ones += __shfl_xor(ones, o, PTD_WAVE);
       rest += __shfl_xor(rest, o, PTD_WAVE);
       weighted += __shfl_xor(weighted, o, PTD_WAVE);
     }
     if (tid == 0) {
-      const Totals t = totals_of({m, static_cast<float>(ones), rest, weighted});
+      const Totals t = totals_of({m, static_cast<float>(ones), rest, weighted, xt});
       s_tot = t;
       put_entry(a, r, t, weighted, xt);
     }
@@ -270,15 +421,27 @@ __global__ void __launch_bounds__(kMergeThreads) k_logp_merge(LogpArgs a) {
       if (a.topk_idx) a.topk_idx[static_cast<size_t>(r) * a.k + tid] = -1;
       if (a.topk_val) a.topk_val[static_cast<size_t>(r) * a.k + tid] = NAN;
     }
-    if (tid < n && key) {
-      int above = 0;
-      for (int j = 0; j < n; ++j) above += s_key[j] > key ? 1 : 0;
-      if (above < a.k) {
-        const size_t at = static_cast<size_t>(r) * a.k + above;
-        if (a.topk_idx) a.topk_idx[at] = static_cast<int32_t>(key_index(key));
-        if (a.topk_val) a.topk_val[at] = logprob_of(a, s_tot, __uint_as_float(bits));
+    // a slice's pairs are in order: the rank of one is its place plus, in every other slice, the number of
+    // larger ones, found by halving (several slices at once: each step waits for LDS)
+    int above = tid % KMAX;
+    const int own = tid / KMAX;
+    for (int j0 = 0; j0 < a.slices; j0 += kMergeSlices) {
+      int lo[kMergeSlices];
+#pragma unroll
+      for (int u = 0; u < kMergeSlices; ++u) lo[u] = 0;
+#pragma unroll
+      for (int step = KMAX / 2; step > 0; step >>= 1) {
+#pragma unroll
+        for (int u = 0; u < kMergeSlices; ++u) lo[u] += s_key[min(j0 + u, a.slices - 1) * KMAX + lo[u] + step - 1] > key ? step : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < kMergeSlices; ++u) {
+        const int j = min(j0 + u, a.slices - 1);
+        lo[u] += s_key[j * KMAX + lo[u]] > key ? 1 : 0;
+        above += j0 + u == own || j0 + u >= a.slices ? 0 : lo[u];
       }
     }
+    if (key && above < a.k) put_best(a, r, above, s_tot, key, bits);
   }
 }
 
@@ -287,7 +450,8 @@ struct LogpPlan {
   size_t ws_bytes;
 };
 
-bool make_plan(int R, int V, int k, int elem_bytes, LogpPlan* p) {
+// path: the rows that are there are about four per sequence, whatever R.
+bool make_plan(int R, int V, int k, int elem_bytes, int path_seqs, LogpPlan* p) {
   if (R < 1 || V < 1 || V > kMaxVocab || k < 0 || k > PTD_MAX_K || k > V) return false;
   const int E = 16 / elem_bytes;
   p->kmax = k == 0 ? 0 : k <= 8 ? 8 : 16;
@@ -299,10 +463,11 @@ bool make_plan(int R, int V, int k, int elem_bytes, LogpPlan* p) {
     p->slices = (V + len - 1) / len;
     p->slice_len = len;
   };
-  cut(8);
-  if (static_cast<long long>(R) * p->slices < 256) {
-    cut(2);
-    if (p->slices * std::max(p->kmax, 4) > kMergeThreads) cut(8);
+  cut(16);
+  const long long rows = path_seqs ? 4LL * path_seqs : R;
+  if (rows * p->slices < 512) {
+    cut(4);
+    if (p->slices * std::max(p->kmax, 4) > kMergeThreads) cut(16);
   }
   if (static_cast<long long>(R) * p->slices > 0x3FFFFFFFLL) return false;
   p->ws_bytes = p->slices > 1 ? static_cast<size_t>(R) * p->slices * (sizeof(Sums) + p->kmax * 16) : 0;
@@ -311,9 +476,17 @@ bool make_plan(int R, int V, int k, int elem_bytes, LogpPlan* p) {
 
 template <int KMAX, bool BF16>
 void launch(const LogpPlan& p, const LogpArgs& a, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(a.R) * a.slices);
-  if (p.nl == 8) hipLaunchKernelGGL((k_logp_row<KMAX, BF16, 8>), grid, dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((k_logp_row<KMAX, BF16, 2>), grid, dim3(kThreads), 0, st, a);
+  const bool one = p.slices == 1;
+  const unsigned n = (a.nodes ? static_cast<unsigned>(ptd_cdiv(a.R, a.part_rows)) * a.ways : static_cast<unsigned>(a.R)) * a.slices;
+#define PTD_LOGP(kernel_, nl_)                                                                                \
+  if (p.nl == nl_ && one) hipLaunchKernelGGL((kernel_<KMAX, BF16, nl_, true>), dim3(n), dim3(kThreads), 0, st, a); \
+  if (p.nl == nl_ && !one) hipLaunchKernelGGL((kernel_<KMAX, BF16, nl_, false>), dim3(n), dim3(kThreads), 0, st, a);
+  if (a.nodes) {
+    PTD_LOGP(k_logp_path, 16) PTD_LOGP(k_logp_path, 4)
+  } else {
+    PTD_LOGP(k_logp_row, 16) PTD_LOGP(k_logp_row, 4)
+  }
+#undef PTD_LOGP
   if (p.slices > 1) hipLaunchKernelGGL((k_logp_merge<KMAX, BF16>), dim3(a.R), dim3(kMergeThreads), 0, st, a);
 }
 template <bool BF16>
@@ -326,10 +499,17 @@ void dispatch(const LogpPlan& p, const LogpArgs& a, hipStream_t st) {
 }  // namespace
 
 extern "C" size_t ptd_token_logprobs_workspace_bytes(int32_t R, int32_t V, int32_t k) {
-  // the dtype is not known here: size for the larger of the bf16 and fp32 plans
-  LogpPlan p2, p4;
-  if (!make_plan(R, V, k, 2, &p2) || !make_plan(R, V, k, 4, &p4)) return 0;
-  return std::max(p2.ws_bytes, p4.ws_bytes);
+  // the dtype is not known here: size for the larger of the bf16 and fp32 plans;
+  // nor whether entries lie along paths, where a slice may be as small as with one row
+  size_t most = 0;
+  for (int es = 2; es <= 4; es += 2) {
+    for (int seqs = 0; seqs < 2; ++seqs) {
+      LogpPlan p;
+      if (!make_plan(R, V, k, es, seqs, &p)) return 0;
+      most = std::max(most, p.ws_bytes);
+    }
+  }
+  return most;
 }
 
 extern "C" int ptd_token_logprobs(const void* logits, ptd_dtype dtype, int32_t R, int32_t V, int64_t ld,
@@ -345,7 +525,7 @@ extern "C" int ptd_token_logprobs(const void* logits, ptd_dtype dtype, int32_t R
   PTD_RETURN_IF(k == 0 ? topk_idx || topk_logprob : !topk_idx && !topk_logprob, PTD_ERR_SHAPE);
   const int es = dtype == PTD_BF16 ? 2 : 4;
   LogpPlan pl;
-  PTD_RETURN_IF(!make_plan(R, V, k, es, &pl), PTD_ERR_SHAPE);
+  PTD_RETURN_IF(!make_plan(R, V, k, es, nodes ? R / (T + 1) : 0, &pl), PTD_ERR_SHAPE);
   PTD_RETURN_IF(!ptd_aligned(logits, es), PTD_ERR_ALIGN);
   if (pl.ws_bytes) {
     PTD_RETURN_IF(!workspace || workspace_bytes < pl.ws_bytes, PTD_ERR_WORKSPACE);
@@ -367,6 +547,13 @@ extern "C" int ptd_token_logprobs(const void* logits, ptd_dtype dtype, int32_t R
   a.unscale = a.inv_tau / a.scale;
   a.R = R, a.V = V, a.T = nodes ? T : 0, a.k = k;
   a.slices = pl.slices, a.slice_len = pl.slice_len;
+  if (nodes) {
+    // as many sequences as a wave reads tokens of at once, and a way for each entry of paths
+    // of three nodes (and four more)
+    const int seqs = std::max(1, std::min(kPartChunks * PTD_WAVE / (T + 1), R / (T + 1)));
+    a.part_rows = seqs * (T + 1);
+    a.ways = std::min(4 * seqs + 4, 32);
+  }
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (dtype == PTD_BF16) dispatch<true>(pl, a, st);
   else dispatch<false>(pl, a, st);

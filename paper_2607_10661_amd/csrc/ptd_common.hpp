@@ -79,6 +79,24 @@ __device__ __forceinline__ float wave_sum(float v) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, PTD_WAVE);
   return v;
 }
+// Sum over the wave to every lane, by steps of the vector ALU (the shuffles above go through
+// LDS): quad permutes, mirrors of half rows and rows, then the two swaps across rows.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float wave_sum_dpp(float v) {
+  v = dpp_add<0xB1>(v);   // quad_perm 1032
+  v = dpp_add<0x4E>(v);   // quad_perm 2301
+  v = dpp_add<0x141>(v);  // row_half_mirror
+  v = dpp_add<0x140>(v);  // row_mirror
+  const uint32_t x = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  const uint32_t y = __float_as_uint(v);
+  const auto q = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
 __device__ __forceinline__ uint64_t shfl_xor_u64(uint64_t v, int o) {
   uint32_t lo = __shfl_xor(static_cast<uint32_t>(v), o, PTD_WAVE);
   uint32_t hi = __shfl_xor(static_cast<uint32_t>(v >> 32), o, PTD_WAVE);

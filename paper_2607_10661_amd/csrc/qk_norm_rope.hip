@@ -10,6 +10,8 @@
 // of a lane's pairs stay in its registers for all heads that the wave takes.
 #include <math.h>
 
+#include <algorithm>
+
 #include "ptd_common.hpp"
 
 namespace {
@@ -97,15 +99,11 @@ struct Chunk<float> {
 };
 
 // Sum over aligned groups of G lanes (4 or 8) to each of them.
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float v) {
-  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
-}
 template <int G>
 __device__ __forceinline__ float group_sum(float v) {
-  v = dpp_add<0xB1>(v);                    // quad_perm 1032
-  v = dpp_add<0x4E>(v);                    // quad_perm 2301
-  return G == 8 ? dpp_add<0x141>(v) : v;   // half-row mirror: the other quad
+  v = ptd::dpp_add<0xB1>(v);                    // quad_perm 1032
+  v = ptd::dpp_add<0x4E>(v);                    // quad_perm 2301
+  return G == 8 ? ptd::dpp_add<0x141>(v) : v;   // half-row mirror: the other quad
 }
 
 // The weights of a lane's elements.
@@ -151,6 +149,22 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_rope(QkArgs a, int norm) {
   const int d0 = 8 * (INTERLEAVED || !turn ? 2 * c : c);
   const int d1 = INTERLEAVED || !turn ? d0 + 8 : d0 + 8 * turned;
 
+  const int gq = (a.heads[0] + H - 1) / H, gk = (a.heads[1] + H - 1) / H;
+  const int groups = gq + gk + (slot >= 0 ? gk : 0);
+  const int page = slot >= 0 ? slot / a.page_size : 0;
+  const int at = slot >= 0 ? slot - page * a.page_size : 0;
+  auto kind_of = [&](int u) { return u < gq ? 0 : u < gq + gk ? 1 : 2; };
+  auto head_of = [&](int u, int kind) { return (u - (kind == 0 ? 0 : kind == 1 ? gq : gq + gk)) * H + hl; };
+  Chunk<T> x0, x1, n0, n1;
+  auto load = [&](int u) __attribute__((always_inline)) {
+    const int kind = kind_of(u), h = head_of(u, kind);
+    if (u < groups && h < a.heads[kind > 0]) {
+      const T* src = static_cast<const T*>(a.in[kind]) + row * a.ld_in[kind] + static_cast<int64_t>(h) * D;
+      n0.load(src + d0);
+      n1.load(src + d1);
+    }
+  };
+  load(sub);
   float cs[8], sn[8];
   if (a.rot > 0) {
     if (lane < a.rot / 2) s_cs[wave][lane] = cos_sin(static_cast<double>(pos) * a.inv_freq[lane]);
@@ -162,18 +176,18 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_rope(QkArgs a, int norm) {
       cs[e] = v.x, sn[e] = v.y;
     }
   }
-  const int gq = (a.heads[0] + H - 1) / H, gk = (a.heads[1] + H - 1) / H;
-  const int groups = gq + gk + (slot >= 0 ? gk : 0);
-  const int page = slot >= 0 ? slot / a.page_size : 0;
-  const int at = slot >= 0 ? slot - page * a.page_size : 0;
+  int have = -1;  // kind whose weights are in w0, w1
+  float w0[8], w1[8];
   for (int u = sub; u < groups; u += a.waves_per_row) {
-    const int kind = u < gq ? 0 : u < gq + gk ? 1 : 2;
-    const int h = (u - (kind == 0 ? 0 : kind == 1 ? gq : gq + gk)) * H + hl;
+    const int kind = kind_of(u), h = head_of(u, kind);
+    x0 = n0, x1 = n1;
+    load(u + a.waves_per_row);
+    if (norm && kind < 2 && kind != have) {
+      load_weights(a.w[kind], a.w_bf16, d0, w0);
+      load_weights(a.w[kind], a.w_bf16, d1, w1);
+      have = kind;
+    }
     if (h >= a.heads[kind > 0]) continue;
-    const T* src = static_cast<const T*>(a.in[kind]) + row * a.ld_in[kind] + static_cast<int64_t>(h) * D;
-    Chunk<T> x0, x1;
-    x0.load(src + d0);
-    x1.load(src + d1);
     if (kind < 2) {
       float x[8], y[8];
       x0.get(x);
@@ -184,9 +198,6 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_rope(QkArgs a, int norm) {
         for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum), sum = fmaf(y[e], y[e], sum);
         sum = group_sum<G>(sum);
         const float f = 1.f / sqrtf(sum * (1.f / D) + a.eps);
-        float w0[8], w1[8];
-        load_weights(a.w[kind], a.w_bf16, d0, w0);
-        load_weights(a.w[kind], a.w_bf16, d1, w1);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = x[e] * f * w0[e], y[e] = y[e] * f * w1[e];
       }
@@ -268,8 +279,12 @@ extern "C" int ptd_qk_norm_rope(const void* q, const void* k, const void* v, con
     a.ld_in[i] = ld[i];
     if (i < 2) a.ld_out[i] = ldo[i];
   }
-  for (int p = 0; p < s.rot_dim / 2; ++p) {
-    a.inv_freq[p] = inv_freq ? inv_freq[p] : pow(s.theta, -2.0 * p / s.rot_dim);
+  // theta^(-2p / rot) as products in 64 bits of mantissa: within a step of the double (64 calls of
+  // pow take 2 us)
+  const long double ratio = s.rot_dim > 0 && !inv_freq ? powl(s.theta, -2.0L / s.rot_dim) : 1.0L;
+  long double f = 1.0L;
+  for (int p = 0; p < s.rot_dim / 2; ++p, f *= ratio) {
+    a.inv_freq[p] = inv_freq ? inv_freq[p] : static_cast<double>(f);
     PTD_RETURN_IF(!(fabs(a.inv_freq[p]) <= 0x1p20), PTD_ERR_SHAPE);
   }
   if (s.N == 0) return PTD_OK;
@@ -291,7 +306,11 @@ extern "C" int ptd_qk_norm_rope(const void* q, const void* k, const void* v, con
     a.pages[0] = store->k_pages, a.pages[1] = store->v_pages;
     a.page_size = store->page_size, a.num_pages = store->num_pages;
   }
-  a.waves_per_row = 1;
+  // A row's head groups over several waves while there are fewer than half of what the chip
+  // holds.  (32/8 heads x 128, into pages: 1024 rows 10.2 us with a wave per row, 7.9 with four; 2048
+  // rows 12.8 with four, 10.9 with two; 28000 rows 121 with one and 146 with six.)
+  const int per = s.D == 128 ? 8 : 16, groups = ptd_cdiv(s.Hq, per) + ptd_cdiv(s.Hkv, per) * (store ? 2 : 1);
+  a.waves_per_row = std::max(1, std::min(groups, 4096 / s.N));
   const int64_t grid = (static_cast<int64_t>(s.N) * a.waves_per_row + kWaves - 1) / kWaves;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool il = s.pairing == PTD_ROPE_INTERLEAVED;

@@ -288,7 +288,8 @@ __global__ void __launch_bounds__(kThreads) k_page_compact(CompactArgs g) {
 // ===========================================================================
 constexpr int kCopyThreads = 256;
 constexpr int kArrays = 96;  // of one launch
-constexpr int kPiece = 32768;  // bytes that a workgroup copies in one turn
+constexpr int kUnroll = 4;   // loads of a thread in flight
+constexpr int kCopyGroups = 8192;
 
 struct CopyArray {
   char* base;
@@ -303,31 +304,46 @@ struct CopyArgs {
   int n, num_pages, pieces;  // of a page of the largest array
 };
 
-// `bytes` bytes from each of `heads` places `step` apart, from the piece's first byte on.
+// Elements first .. first + kCopyThreads * kUnroll - 1 of `total`, in runs of `run`, `step` apart
+// (one run: both are `total`).
 template <typename V>
-__device__ __forceinline__ void copy_runs(const char* from, char* to, int heads, long long step, int run, long long first,
-                                          long long last) {
-  (void)heads;
-  // first, last: in bytes of the runs laid end to end
-  for (long long i = first + static_cast<long long>(threadIdx.x) * sizeof(V); i < last; i += kCopyThreads * sizeof(V)) {
-    const long long h = i / run;
-    const long long at = h * step + (i - h * run);
-    *reinterpret_cast<V*>(to + at) = *reinterpret_cast<const V*>(from + at);
+__device__ __forceinline__ void copy_piece(const char* from, char* to, uint32_t total, uint32_t run, uint32_t step, uint32_t first) {
+  const V* __restrict__ s = reinterpret_cast<const V*>(from);
+  V* __restrict__ d = reinterpret_cast<V*>(to);
+  const uint32_t i = first + threadIdx.x;
+  if (run == total && first + kCopyThreads * kUnroll <= total) {  // uniform
+    static_assert(kUnroll == 4, "four loads");
+    const V a = s[i], b = s[i + kCopyThreads], c = s[i + 2 * kCopyThreads], e = s[i + 3 * kCopyThreads];
+    d[i] = a, d[i + kCopyThreads] = b, d[i + 2 * kCopyThreads] = c, d[i + 3 * kCopyThreads] = e;
+    return;
+  }
+#pragma unroll 2
+  for (int u = 0; u < kUnroll; ++u) {
+    const uint32_t x = i + u * kCopyThreads;
+    if (x < total) {
+      const uint32_t h = run == total ? 0 : x / run;
+      const uint32_t at = h * step + (x - h * run);
+      d[at] = s[at];
+    }
   }
 }
 
+// One workgroup per (pair, piece of its page) in turn, an array of pages per grid row.  Bound by
+// HBM, reads and writes mixed.
 __global__ void __launch_bounds__(kCopyThreads) k_page_copy(CopyArgs g) {
   const CopyArray a = g.arrays[blockIdx.y];
   const long long items = static_cast<long long>(g.n) * g.pieces;
+  const uint32_t step = static_cast<uint32_t>(a.units) * a.unit_bytes / a.granule;  // of a head, in elements
+  const long long page = static_cast<long long>(a.heads) * a.units * a.unit_bytes;
   for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-    const int i = static_cast<int>(item / g.pieces), piece = static_cast<int>(item - static_cast<long long>(i) * g.pieces);
+    const int i = static_cast<int>(item / g.pieces);
+    const uint32_t first = static_cast<uint32_t>(item - static_cast<long long>(i) * g.pieces) * (kCopyThreads * kUnroll);
     const int s = g.src[i], d = g.dst[i];
     if (s == -1 || d == -1 || s == d) continue;
     if (static_cast<uint32_t>(s) >= static_cast<uint32_t>(g.num_pages) || static_cast<uint32_t>(d) >= static_cast<uint32_t>(g.num_pages)) {
       if (threadIdx.x == 0) ptd::report(g.dev_status, PTD_ERR_PAGE);
       continue;
     }
-    const long long step = static_cast<long long>(a.units) * a.unit_bytes;  // of a head
     int units = a.units;
     if (g.rows) {
       const int r = g.rows[i];
@@ -335,18 +351,17 @@ __global__ void __launch_bounds__(kCopyThreads) k_page_copy(CopyArgs g) {
         if (threadIdx.x == 0) ptd::report(g.dev_status, PTD_ERR_ROWS);
         continue;
       }
-      units = (r + a.unit_rows - 1) / a.unit_rows;
+      units = static_cast<int>((static_cast<long long>(r) + a.unit_rows - 1) / a.unit_rows);
     }
-    const bool all = units == a.units;
-    const long long bytes = static_cast<long long>(a.heads) * units * a.unit_bytes;
-    const int run = all ? 0x7FFFFFFF : units * a.unit_bytes;
-    const long long first = static_cast<long long>(piece) * kPiece, last = min(bytes, first + kPiece);
-    const char* from = a.base + static_cast<long long>(s) * a.heads * step;
-    char* to = a.base + static_cast<long long>(d) * a.heads * step;
-    if (a.granule == 16) copy_runs<uint4>(from, to, a.heads, step, run, first, last);
-    else if (a.granule == 4) copy_runs<uint32_t>(from, to, a.heads, step, run, first, last);
-    else if (a.granule == 2) copy_runs<uint16_t>(from, to, a.heads, step, run, first, last);
-    else copy_runs<uint8_t>(from, to, a.heads, step, run, first, last);
+    const uint32_t run = static_cast<uint32_t>(units) * a.unit_bytes / a.granule, total = run * a.heads;
+    if (first >= total) continue;
+    const char* from = a.base + s * page;
+    char* to = a.base + d * page;
+    const uint32_t one = units == a.units ? total : run;
+    if (a.granule == 16) copy_piece<uint4>(from, to, total, one, step, first);
+    else if (a.granule == 4) copy_piece<uint32_t>(from, to, total, one, step, first);
+    else if (a.granule == 2) copy_piece<uint16_t>(from, to, total, one, step, first);
+    else copy_piece<uint8_t>(from, to, total, one, step, first);
   }
 }
 
@@ -409,11 +424,11 @@ extern "C" int ptd_page_copy(const ptd_page_array* arrays, int32_t num_arrays, i
     long long most = 0;
     for (int i = 0; i < m; ++i) {
       const ptd_page_array& x = arrays[first + i];
-      // the widest loads that every unit of every page is aligned for
+      // the widest elements that every unit of every page is aligned for
       const uintptr_t any = reinterpret_cast<uintptr_t>(x.base) | static_cast<uintptr_t>(x.unit_bytes);
-      g.arrays[i] = {static_cast<char*>(x.base), x.heads, x.units, x.unit_rows, x.unit_bytes,
-                     any % 16 == 0 ? 16 : any % 4 == 0 ? 4 : any % 2 == 0 ? 2 : 1};
-      most = std::max(most, static_cast<long long>(x.heads) * x.units * x.unit_bytes);
+      const int granule = any % 16 == 0 ? 16 : any % 4 == 0 ? 4 : any % 2 == 0 ? 2 : 1;
+      g.arrays[i] = {static_cast<char*>(x.base), x.heads, x.units, x.unit_rows, x.unit_bytes, granule};
+      most = std::max(most, static_cast<long long>(x.heads) * x.units * x.unit_bytes / granule);
     }
     g.src = src;
     g.dst = dst;
@@ -421,9 +436,10 @@ extern "C" int ptd_page_copy(const ptd_page_array* arrays, int32_t num_arrays, i
     g.dev_status = dev_status;
     g.n = n;
     g.num_pages = num_pages;
+    constexpr int kPiece = kCopyThreads * kUnroll;
     g.pieces = static_cast<int>((most + kPiece - 1) / kPiece);
     const long long items = static_cast<long long>(n) * g.pieces;
-    const unsigned gx = static_cast<unsigned>(std::min<long long>(items, std::max(1, 4096 / m)));
+    const unsigned gx = static_cast<unsigned>(std::min<long long>(items, std::max(1, kCopyGroups / m)));
     hipLaunchKernelGGL(k_page_copy, dim3(gx, m), dim3(kCopyThreads), 0, static_cast<hipStream_t>(stream), g);
     const int rc = ptd_launch_status();
     if (rc != PTD_OK) return rc;

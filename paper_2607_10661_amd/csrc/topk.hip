@@ -71,7 +71,68 @@ k_topk_row(const void* __restrict__ logits, int V, long long ld, int slices, int
   uint4 cw[NL];
   load_chunks<BF16, NT, NL>(cw, rb, sl, tid);
   const uint32_t bt = sl.tail ? elem_bits<BF16>(rb, sl.vt) : 0u;
-  topk_of_slice<KMAX, BF16, NT, NL>(sh, cw, rb, sl, bt, tid, [&](int rank, uint64_t key, uint32_t bits) {
+  uint32_t lm = sl.tail ? elem_img<BF16>(bt) : 0u;
+#pragma unroll
+  for (int u = 0; u < NL; ++u) lm = max(lm, u * NT + tid < sl.nfull ? chunk_img<BF16>(cw[u]) : 0u);
+  topk_groups<KMAX, NT>(sh, lm, tid);
+  lds_barrier();
+  const uint32_t tc = topk_list<KMAX, BF16, NT, NL>(sh, cw, sl, bt, tid);
+  lds_barrier();
+  // a list that overflows (values tied at the top, or in order): every lane keeps a sorted list of
+  // the best of its own elements that reach the bound, and the lists are merged (KMAX 16: its registers
+  // would halve the workgroups of a CU, so the best are taken one after the other)
+  auto overflow = [&]() {
+    if constexpr (KMAX == 16) {
+      topk_in_turns<KMAX, BF16, NT>(sh, rb, sl, tid);
+    } else {
+      constexpr int E = BF16 ? 8 : 4;
+      const int lane = tid & 63, wave = tid >> 6;
+      uint64_t l[KMAX];
+#pragma unroll
+      for (int j = 0; j < KMAX; ++j) l[j] = 0;
+#pragma unroll
+      for (int u = 0; u < NL; ++u) {
+        const int c = u * NT + tid;
+        if (c < sl.nfull) {
+          const int v = sl.vb + c * E;
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const uint32_t bits = chunk_bits<BF16>(cw[u], e);
+            const uint64_t key = make_key(bits, static_cast<uint32_t>(v + e));
+            if (elem_img<BF16>(bits) >= tc && key > l[KMAX - 1]) insert<KMAX>(l, key);
+          }
+        }
+      }
+      if (sl.tail) {
+        const uint64_t key = make_key(bt, static_cast<uint32_t>(sl.vt));
+        if (elem_img<BF16>(bt) >= tc && key > l[KMAX - 1]) insert<KMAX>(l, key);
+      }
+      wave_merge<KMAX>(l);
+      if (lane < KMAX) {
+        uint64_t mine = 0;
+#pragma unroll
+        for (int r = 0; r < KMAX; ++r) mine = (lane == r) ? l[r] : mine;
+        sh.cand[wave * KMAX + lane] = mine;  // every wave is past its reads of sh.cand
+      }
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll
+        for (int j = 0; j < KMAX; ++j) l[j] = 0;
+        for (int i = lane; i < NT / PTD_WAVE * KMAX; i += PTD_WAVE) insert<KMAX>(l, sh.cand[i]);
+        wave_merge<KMAX>(l);
+        uint64_t mine = 0;
+#pragma unroll
+        for (int r = 0; r < KMAX; ++r) mine = (lane == r) ? l[r] : mine;
+        if (lane < KMAX) {
+          sh.out[lane] = mine;
+          sh.out_bits[lane] = mine ? elem_bits<BF16>(rb, key_index(mine)) : 0u;
+        }
+      }
+    }
+  };
+  topk_examine<BF16, NT>(sh, sl, tc, tid);
+  __syncthreads();
+  topk_pick<KMAX, BF16, NT>(sh, rb, sl, tid, overflow, [&](int rank, uint64_t key, uint32_t bits) {
     if (slices == 1) {
       const int32_t idx = static_cast<int32_t>(key_index(key));
       if (rank == 0) argmax[row] = idx;

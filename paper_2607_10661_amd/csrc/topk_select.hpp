@@ -127,6 +127,7 @@ __device__ __forceinline__ void load_chunks(uint4 (&cw)[NL], const char* rb, con
 }
 
 constexpr int kCandCap = 256;                            // LDS candidate list
+constexpr int kCandPad = 8;                              // none, for whole steps of the counting
 constexpr int kListCap = 256;                            // LDS chunk list
 
 using s16x2 = short __attribute__((ext_vector_type(2)));
@@ -138,11 +139,6 @@ using s16x2 = short __attribute__((ext_vector_type(2)));
 //         negative values).  -0 maps one below +0, so a bound equal to the
 //         image of +0 is lowered to that of -0 before elements are compared.
 constexpr uint32_t kImgPosZeroBf16 = 0x8001u;
-__device__ __forceinline__ s16x2 sorder2(uint32_t d) {
-  const s16x2 v = __builtin_bit_cast(s16x2, d);
-  const s16x2 sg = v >> static_cast<short>(15);
-  return __builtin_bit_cast(s16x2, d ^ (__builtin_bit_cast(uint32_t, sg) & 0x7FFF7FFFu));
-}
 template <bool BF16>
 __device__ __forceinline__ uint32_t elem_img(uint32_t bits32) {  // bits of the fp32 value
   if constexpr (BF16) {
@@ -153,12 +149,20 @@ __device__ __forceinline__ uint32_t elem_img(uint32_t bits32) {  // bits of the 
     return ord_of(__uint_as_float(bits32));
   }
 }
+// The largest image of a chunk.  bf16: patterns of numbers with equal signs are in order as they
+// are, so the largest as signed integers is the largest number if any is positive, else the
+// smallest without sign is: 6 packed operations in place of 15 to put all of them in order.
 template <bool BF16>
 __device__ __forceinline__ uint32_t chunk_img(const uint4& c) {
   if constexpr (BF16) {
-    const s16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(sorder2(c.x), sorder2(c.y)),
-                                              __builtin_elementwise_max(sorder2(c.z), sorder2(c.w)));
-    return static_cast<uint32_t>(max(static_cast<int>(m.x), static_cast<int>(m.y)) + 0x8001);
+    using u16x2 = unsigned short __attribute__((ext_vector_type(2)));
+    const s16x2 a = __builtin_elementwise_max(__builtin_elementwise_max(__builtin_bit_cast(s16x2, c.x), __builtin_bit_cast(s16x2, c.y)),
+                                              __builtin_elementwise_max(__builtin_bit_cast(s16x2, c.z), __builtin_bit_cast(s16x2, c.w)));
+    const u16x2 b = __builtin_elementwise_min(__builtin_elementwise_min(__builtin_bit_cast(u16x2, c.x), __builtin_bit_cast(u16x2, c.y)),
+                                              __builtin_elementwise_min(__builtin_bit_cast(u16x2, c.z), __builtin_bit_cast(u16x2, c.w)));
+    const int hi = max(static_cast<int>(a.x), static_cast<int>(a.y));
+    const int lo = min(static_cast<int>(b.x), static_cast<int>(b.y));
+    return static_cast<uint32_t>((hi >= 0 ? hi : ~(lo & 0x7FFF)) + 0x8001);
   } else {
     return ord_of(fmaxf(fmaxf(__uint_as_float(c.x), __uint_as_float(c.y)),
                         fmaxf(__uint_as_float(c.z), __uint_as_float(c.w))));
@@ -212,79 +216,87 @@ __device__ __forceinline__ uint32_t group_max_min(uint32_t x) {
 template <int NT>
 struct TopkLds {
   __attribute__((aligned(16))) uint4 ldata[kListCap];
-  uint64_t cand[kCandCap];
+  __attribute__((aligned(16))) uint64_t cand[kCandCap + kCandPad];
   uint32_t bits[kCandCap];
   uint32_t rank[kCandCap];
   uint16_t list[kListCap];
   __attribute__((aligned(16))) uint32_t tau[NT / PTD_WAVE];
   __attribute__((aligned(16))) uint32_t tau2[NT / PTD_WAVE];
+  uint64_t out[PTD_MAX_K];  // the best ones, in order
+  uint32_t out_bits[PTD_MAX_K];
   int nlist, cnt;
 };
 
 // The KMAX best entries of a slice that a workgroup of NT threads holds, NL chunks of 16 bytes
-// per lane: put(rank, key, bits of the fp32 value) is called once for each rank < KMAX (key 0: none).
-//   1. Every lane takes the image of each of its chunks (bf16 images are 16
-//      bits wide and computed two at a time with packed 16-bit integer
-//      operations) and their maximum.
+// per lane, in four parts with a barrier between them (the caller's, who may do other work
+// before it): topk_groups, topk_list, topk_examine, topk_pick.
+//   1. Every lane takes the image of each of its chunks and their maximum.
 //   2. A lower bound tau of the slice's KMAX-th best value: the lanes of a
 //      wave form KMAX groups; each group's largest lane maximum is a distinct
 //      element, so the least of the KMAX group maxima is at most the KMAX-th
-//      best value.  The bound of the slice is the largest bound of its waves.
+//      best value.  The bound of the slice is the largest bound of its waves, or the least of
+//      KMAX groups of NT / KMAX lanes spanning the workgroup where that is larger (much
+//      closer to the KMAX-th best value of the slice, hence few candidates; the first stays
+//      positive where a short slice leaves whole workgroup-wide groups empty).
 //   3. Chunks whose image reaches tau are copied with their index to a list
 //      in LDS, then the workgroup examines the listed chunks a thread per
 //      element and appends the elements that reach tau to a candidate list.
 //      The edges of the slice (the elements before its first 16-byte
 //      boundary and after its last whole chunk, fewer than two chunks) are
-//      read with plain loads, one per lane, and checked the same way.
+//      read with plain loads, one per lane, and checked the same way.  Entries at -inf are never
+//      listed: masked rows have any number of them.
 //   4. The candidates are ranked by counting: the list is cut into parts,
 //      each thread counts the keys of one part above one candidate, and the
-//      counts are summed in LDS.  The candidates of rank below k are the
-//      result.  If either list overflows (many values tied at the top), every
-//      lane keeps a sorted list of its best keys among its own elements that
-//      reach tau, and the lists are merged.
+//      counts are summed in LDS.  Where fewer than KMAX are above -inf, all others of the slice
+//      are at -inf, so the first of those in order are among its first KMAX entries.  If either list
+//      overflows (many values tied at the top, or in order), the caller's overflow() finds them.
 // Only listed chunks pass through LDS, so the slice is read from memory once
 // and LDS carries a few KB.  The kernel's loops stay rolled, which keeps its
 // code small: its instructions are fetched once per CU, cold.
-template <int KMAX, bool BF16, int NT, int NL, typename Put>
-__device__ __forceinline__ void topk_of_slice(TopkLds<NT>& sh, const uint4 (&cw)[NL], const char* rb, const Slice& s,
-                                              uint32_t bt, int tid, Put put) {
-  constexpr int E = BF16 ? 8 : 4;  // elements per 16-byte chunk
-  constexpr int NW = NT / PTD_WAVE;
-  static_assert(NT >= kCandCap && NW % 4 == 0 && NT * NL <= 65536, "workgroup shape");
+template <int KMAX, int NT>
+__device__ __forceinline__ void topk_groups(TopkLds<NT>& sh, uint32_t lm, int tid) {
+  static_assert(NT >= kCandCap && NT / PTD_WAVE % 4 == 0, "workgroup shape");
   static_assert((NT & (NT - 1)) == 0, "KMAX groups of NT / KMAX lanes");
   constexpr int GL = PTD_WAVE / KMAX;  // lanes per group inside a wave
   constexpr int GW = NT / KMAX;        // lanes per group across the workgroup
   constexpr int GWL = GW < PTD_WAVE ? GW : PTD_WAVE;  // ... of them inside one wave
-  constexpr int WPG = GW / GWL;        // waves per workgroup-wide group
-  const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (tid < kCandCap) sh.rank[tid] = 0;
+  if (tid < kCandCap) {
+    sh.rank[tid] = 0;
+    sh.cand[tid] = 0;
+  }
+  if (tid < kCandPad) sh.cand[kCandCap + tid] = 0;
   if (tid == 0) {
     sh.cnt = 0;
     sh.nlist = 0;
   }
-
-  // 1. chunk images and the lane maximum
-  uint32_t cm[NL];
-  uint32_t lm = s.tail ? elem_img<BF16>(bt) : 0u;
-#pragma unroll
-  for (int u = 0; u < NL; ++u) {
-    cm[u] = u * NT + tid < s.nfull ? chunk_img<BF16>(cw[u]) : 0u;
-    lm = max(lm, cm[u]);
-  }
-  // 2. the bound, the larger of two: per wave, max over groups of GL lanes
-  //    then min over the wave's KMAX groups, and the largest of these over
-  //    the waves; and min over KMAX groups of NT / KMAX lanes spanning the
-  //    workgroup of the group maxima (much closer to the KMAX-th best value
-  //    of the slice, hence few candidates; the first stays positive where a
-  //    short slice leaves whole workgroup-wide groups empty)
   const uint32_t g = group_max_min<GL>(lm);
   const uint32_t g2 = group_max_min<GWL>(lm);  // GWL = 64: the wave's maximum
-  if (lane == 0) {
+  if ((tid & 63) == 0) {
     sh.tau[wave] = g;
     sh.tau2[wave] = g2;
   }
-  ptd::lds_barrier();
+}
+
+// Image of -inf.
+template <bool BF16>
+constexpr uint32_t kImgNegInf = BF16 ? 0x80u : 0x007FFFFFu;
+
+template <int NT>
+__device__ __forceinline__ void topk_append(TopkLds<NT>& sh, uint32_t bits, int v) {
+  const int pos = atomicAdd(&sh.cnt, 1);
+  if (pos < kCandCap) {
+    sh.cand[pos] = make_key(bits, static_cast<uint32_t>(v));
+    sh.bits[pos] = bits;
+  }
+}
+
+// Lists what reaches the bound, which is returned.
+template <int KMAX, bool BF16, int NT, int NL>
+__device__ __forceinline__ uint32_t topk_list(TopkLds<NT>& sh, const uint4 (&cw)[NL], const Slice& s, uint32_t bt, int tid) {
+  constexpr int NW = NT / PTD_WAVE;
+  constexpr int GW = NT / KMAX;
+  constexpr int WPG = GW < PTD_WAVE ? 1 : GW / PTD_WAVE;  // waves per workgroup-wide group
   uint32_t tau = 0;
 #pragma unroll
   for (int i = 0; i < NW; i += 4) {
@@ -299,20 +311,10 @@ __device__ __forceinline__ void topk_of_slice(TopkLds<NT>& sh, const uint4 (&cw)
     for (int w = 0; w < WPG; ++w) gm = max(gm, sh.tau2[j * WPG + w]);
     tau2 = min(tau2, gm);
   }
-  tau = max(tau, tau2);
-  const uint32_t tc = cmp_bound<BF16>(tau);
-
-  // 3. list the chunks that reach the bound, then examine them
-  auto append = [&](uint32_t bits, int v) {
-    const int pos = atomicAdd(&sh.cnt, 1);
-    if (pos < kCandCap) {
-      sh.cand[pos] = make_key(bits, static_cast<uint32_t>(v));
-      sh.bits[pos] = bits;
-    }
-  };
+  const uint32_t tc = max(cmp_bound<BF16>(max(tau, tau2)), kImgNegInf<BF16> + 1);
 #pragma unroll
   for (int u = 0; u < NL; ++u) {
-    if (cm[u] != 0 && cm[u] >= tc) {
+    if (u * NT + tid < s.nfull && chunk_img<BF16>(cw[u]) >= tc) {
       const int pos = atomicAdd(&sh.nlist, 1);
       if (pos < kListCap) {
         sh.ldata[pos] = cw[u];
@@ -320,84 +322,135 @@ __device__ __forceinline__ void topk_of_slice(TopkLds<NT>& sh, const uint4 (&cw)
       }
     }
   }
-  if (s.tail && elem_img<BF16>(bt) >= tc) append(bt, s.vt);
-  ptd::lds_barrier();
-  const int nl = sh.nlist;
-  if (nl <= kListCap) {  // uniform
-    for (int i0 = 0; i0 < nl; i0 += NT / E) {
-      const int i = i0 + tid / E;
-      if (i < nl) {
-        const int c = sh.list[i], e = tid & (E - 1);
-        const uint32_t bits = BF16 ? static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(sh.ldata + i)[e]) << 16
-                                   : reinterpret_cast<const uint32_t*>(sh.ldata + i)[e];
-        if (elem_img<BF16>(bits) >= tc) append(bits, s.vb + c * E + e);
+  if (s.tail && elem_img<BF16>(bt) >= tc) topk_append(sh, bt, s.vt);
+  return tc;
+}
+
+// The best key below `below` of a thread's elements, read anew.
+template <bool BF16, int NT>
+__device__ __forceinline__ uint64_t best_below(const char* rb, const Slice& s, int tid, uint64_t below) {
+  constexpr int E = BF16 ? 8 : 4;
+  uint64_t best = 0;
+  const uint4* src = reinterpret_cast<const uint4*>(rb + static_cast<size_t>(s.vb) * (BF16 ? 2 : 4));
+#pragma unroll 1
+  for (int c0 = tid; c0 < s.nfull; c0 += 4 * NT) {
+    uint4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = src[min(c0 + u * NT, s.nfull - 1)];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int c = c0 + u * NT;
+      if (c < s.nfull) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const uint64_t key = make_key(chunk_bits<BF16>(x[u], e), static_cast<uint32_t>(s.vb + c * E + e));
+          best = key < below && key > best ? key : best;
+        }
       }
     }
   }
-  __syncthreads();
-  const int n = sh.cnt;
+  if (s.tail) {
+    const uint64_t key = make_key(elem_bits<BF16>(rb, s.vt), static_cast<uint32_t>(s.vt));
+    best = key < below && key > best ? key : best;
+  }
+  return best;
+}
 
-  // 4. selection
+// The best keys of a slice to sh.out, one after the other: every thread looks for the best of its
+// own, the best of all is taken, and its owner looks for its next one.
+template <int KMAX, bool BF16, int NT>
+__device__ __forceinline__ void topk_in_turns(TopkLds<NT>& sh, const char* rb, const Slice& s, int tid) {
+  constexpr int NW = NT / PTD_WAVE;
+  uint64_t mine = 0, below = ~0ull;
+  bool look = true;
+#pragma unroll 1
+  for (int r = 0; r < KMAX; ++r) {
+    if (look) mine = best_below<BF16, NT>(rb, s, tid, below);
+    const uint64_t w = wave_max_u64(mine);
+    if (r == 0) __syncthreads();  // sh.cand of the lists is read
+    if ((tid & 63) == 0) sh.cand[(r & 1) * NW + (tid >> 6)] = w;
+    __syncthreads();
+    uint64_t best = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const uint64_t x = sh.cand[(r & 1) * NW + i];
+      best = x > best ? x : best;
+    }
+    look = best != 0 && mine == best;
+    below = best;
+    if (look || (best == 0 && tid == 0)) {
+      sh.out[r] = best;
+      sh.out_bits[r] = best ? elem_bits<BF16>(rb, key_index(best)) : 0u;
+    }
+  }
+}
+
+// The listed chunks' elements that reach the bound become candidates.
+template <bool BF16, int NT>
+__device__ __forceinline__ void topk_examine(TopkLds<NT>& sh, const Slice& s, uint32_t tc, int tid) {
+  constexpr int E = BF16 ? 8 : 4;  // elements per 16-byte chunk
+  const int nl = sh.nlist;
+  if (nl > kListCap) return;  // uniform
+  for (int i0 = 0; i0 < nl; i0 += NT / E) {
+    const int i = i0 + tid / E;
+    if (i < nl) {
+      const int c = sh.list[i], e = tid & (E - 1);
+      const uint32_t bits = BF16 ? static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(sh.ldata + i)[e]) << 16
+                                 : reinterpret_cast<const uint32_t*>(sh.ldata + i)[e];
+      if (elem_img<BF16>(bits) >= tc) topk_append(sh, bits, s.vb + c * E + e);
+    }
+  }
+}
+
+// put(rank, key, bits of the fp32 value) is called once for each rank < KMAX, by thread `rank`
+// (key 0: none).  overflow() leaves the keys and bits in sh.out where a list overflowed.
+template <int KMAX, bool BF16, int NT, typename Overflow, typename Put>
+__device__ __forceinline__ void topk_pick(TopkLds<NT>& sh, const char* rb, const Slice& s, int tid, Overflow overflow, Put put) {
+  const int nl = sh.nlist;
+  const int n = sh.cnt;
   if (nl <= kListCap && n <= kCandCap) {  // uniform over the workgroup
     int n2 = PTD_WAVE;  // candidates per part-set: a power of two >= n
     while (n2 < n) n2 <<= 1;
     const int parts = NT / n2;
     const int i = tid & (n2 - 1), p = tid / n2;  // p is uniform over a wave
-    const int len = (n + parts - 1) / parts;
-    const int j0 = p * len, j1 = min(n, j0 + len);
+    // (in steps of 8, whose reads are in flight together; a part's end and the next one's start
+    // are the same, and entries past the last are 0, above none.  256 candidates on 256 threads: 256
+    // reads one after the other took 6 us)
+    const int len = ((n + parts - 1) / parts + kCandPad - 1) & ~(kCandPad - 1);
+    const int j0 = p * len, j1 = min((n + kCandPad - 1) & ~(kCandPad - 1), j0 + len);
     const uint64_t mine = i < n ? sh.cand[i] : ~0ull;
     uint32_t above = 0;
-    for (int j = j0; j < j1; ++j) above += sh.cand[j] > mine ? 1u : 0u;
+#pragma unroll 1
+    for (int j = j0; j < j1; j += kCandPad) {
+      uint64_t x[kCandPad];
+#pragma unroll
+      for (int t = 0; t < kCandPad; ++t) x[t] = sh.cand[j + t];
+#pragma unroll
+      for (int t = 0; t < kCandPad; ++t) above += x[t] > mine ? 1u : 0u;
+    }
     if (above) atomicAdd(&sh.rank[i], above);
     __syncthreads();
-    if (tid < n) {
+    if (tid < n && sh.rank[tid] < static_cast<uint32_t>(KMAX)) {
       const uint32_t rank = sh.rank[tid];
-      const uint64_t key = sh.cand[tid];
-      if (rank < static_cast<uint32_t>(KMAX)) put(static_cast<int>(rank), key, sh.bits[tid]);
-    } else if (tid < KMAX) {  // fewer candidates than KMAX
-      put(tid, 0ull, 0u);
+      sh.out[rank] = sh.cand[tid];
+      sh.out_bits[rank] = sh.bits[tid];
     }
-    return;
-  }
-
-  // overflow: per-lane sorted lists of the lane's own elements that reach tau
-  uint64_t l[KMAX];
-#pragma unroll
-  for (int j = 0; j < KMAX; ++j) l[j] = 0;
-#pragma unroll
-  for (int u = 0; u < NL; ++u) {
-    const int c = u * NT + tid;
-    if (c < s.nfull) {
-      const int v = s.vb + c * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const uint32_t bits = chunk_bits<BF16>(cw[u], e);
-        const uint64_t key = make_key(bits, static_cast<uint32_t>(v + e));
-        if (elem_img<BF16>(bits) >= tc && key > l[KMAX - 1]) insert<KMAX>(l, key);
+    if (n < KMAX && tid < KMAX) {  // the rest: the first entries at -inf, then none
+      const int v = s.v0 + tid;
+      const bool out = v < s.v1 && elem_bits<BF16>(rb, v) == 0xFF800000u;
+      const uint64_t all = __ballot(out);
+      const int rank = n + __popcll(all & ((1ull << tid) - 1));
+      if (out && rank < KMAX) {
+        sh.out[rank] = make_key(0xFF800000u, static_cast<uint32_t>(v));
+        sh.out_bits[rank] = 0xFF800000u;
       }
+      if (tid >= n + __popcll(all)) sh.out[tid] = 0;
     }
-  }
-  if (s.tail) {
-    const uint64_t key = make_key(bt, static_cast<uint32_t>(s.vt));
-    if (key > l[KMAX - 1]) insert<KMAX>(l, key);
-  }
-  wave_merge<KMAX>(l);
-  if (lane < KMAX) {
-    uint64_t mine = 0;
-#pragma unroll
-    for (int r = 0; r < KMAX; ++r) mine = (lane == r) ? l[r] : mine;
-    sh.cand[wave * KMAX + lane] = mine;  // every wave is past its reads of sh.cand
+  } else {
+    overflow();
   }
   __syncthreads();
-  if (wave != 0) return;
-#pragma unroll
-  for (int j = 0; j < KMAX; ++j) l[j] = 0;
-  for (int i = lane; i < NW * KMAX; i += PTD_WAVE) insert<KMAX>(l, sh.cand[i]);
-  wave_merge<KMAX>(l);
-  uint64_t mine = 0;
-#pragma unroll
-  for (int r = 0; r < KMAX; ++r) mine = (lane == r) ? l[r] : mine;
-  if (lane < KMAX) put(lane, mine, mine ? elem_bits<BF16>(rb, key_index(mine)) : 0u);
+  if (tid < KMAX) put(tid, sh.out[tid], sh.out_bits[tid]);
 }
 
 }  // namespace ptd
