@@ -28,7 +28,7 @@ using namespace ptd;
 
 constexpr int kThreads = 256;       // of k_logp_row
 constexpr int kMergeThreads = 256;  // of k_logp_merge: the most (slices x best entries) of a row
-constexpr int kMergeSlices = 8;
+constexpr int kMergeSlices = 8;     // looked through at once
 constexpr int kMaxVocab = 262144;
 constexpr int kPartChunks = 4;      // k_logp_path: tokens of a lane at once
 
@@ -140,7 +140,7 @@ __device__ __forceinline__ void put_entry(const LogpArgs& a, int r, const Totals
 }
 __device__ __forceinline__ void put_best(const LogpArgs& a, int r, int rank, const Totals& t, uint64_t key, uint32_t bits) {
   const size_t at = static_cast<size_t>(r) * a.k + rank;
-  if (a.topk_idx) a.topk_idx[at] = static_cast<int32_t>(key_index(key));  // (no key: -1)
+  if (a.topk_idx) a.topk_idx[at] = key ? static_cast<int32_t>(key_index(key)) : -1;
   if (a.topk_val) a.topk_val[at] = key ? logprob_of(a, t, __uint_as_float(bits)) : NAN;
 }
 __device__ __forceinline__ void put_nothing(const LogpArgs& a, int r, int tid) {
@@ -390,7 +390,9 @@ __global__ void __launch_bounds__(kMergeThreads) k_logp_merge(LogpArgs a) {
     put_nothing(a, r, tid);
     return;
   }
-  if (KMAX > 0) s_key[tid] = key;  // (0: none)
+  if (KMAX > 0) {
+    s_key[tid] = key;  // (0: none)
+  }
   if (tid < PTD_WAVE) {
     const float xt = __shfl(s.token_logit, token >= 0 ? token / a.slice_len : 0, PTD_WAVE);
     // (a NaN maximum stays one)

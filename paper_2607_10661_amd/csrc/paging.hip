@@ -27,6 +27,9 @@ struct PlanParams {
 // their own, over the whole chip.  (A plan and its release, 16 sequences: of 1024 rows 10.1 us
 // and with a launch 13.1, of 2048 12.2 and 13.3, of 4096 16.7 and 13.1.)
 constexpr int kPlanRows = 2048;
+// Fewer where pages are shared, as held ones' counts are looked up.  (A plan and its release, 16 sequences of
+// 64 rows 13.3 us and with a launch 13.8, 32 of them 16.1 and 14.6.)
+constexpr int kPlanRowsShared = 1024;
 constexpr int kPlanSmall = 256, kPlanLarge = 1024;  // threads
 // Pages of the new rows from which on the planning workgroup is a large one.  (A plan and
 // the release of its pages by a call without rows, both with 256 threads and with 1024: of 32
@@ -215,7 +218,61 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
       }
     };
     long long freed = 0;
-    if (all.back > 0) {  // uniform
+    // a few surplus pages per thread stay in its registers
+    constexpr int kEach = 8;
+    int ids[kEach], seqs[kEach], give[kEach], m = 0;  // give: whether the thread puts the page on the list
+    const bool kept = ONE && all.back <= kEach * NT;
+    if (kept && all.back > 0) {  // uniform
+      s_back[tid] = static_cast<int>(at.back);
+      s_need[tid] = w.need;
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const int j = tid * kEach + u;
+        seqs[u] = j < all.back ? upper(s_back, B, j) : 0;
+        ids[u] = j < all.back ? table_of(p, seqs[u])[s_need[seqs[u]] + (j - s_back[seqs[u]])] : -1;
+      }
+      bool several = false;
+      int refs[kEach];
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        const bool ok = static_cast<uint32_t>(ids[u]) < static_cast<uint32_t>(p.s.num_pages);
+        refs[u] = ok ? p.refs[ids[u]] : 0;
+        if (tid * kEach + u < all.back && refs[u] <= 0) ptd::report(p.dev_status, PTD_ERR_PAGE);
+        several |= refs[u] > 1;
+        give[u] = refs[u] == 1;
+      }
+      // pages of one holder go back at once; else as below
+      if (__syncthreads_or(several)) {
+#pragma unroll
+        for (int u = 0; u < kEach; ++u)
+          if (refs[u] > 0) ptd::add_count(p.refs + ids[u], -1);
+        ptd::drained_barrier();
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+          const int v = refs[u] > 0 ? ptd::load_count(p.refs + ids[u]) : 1;
+          if (v == 0 || is_giver(v)) ptd::min_count(p.refs + ids[u], kGiver + seqs[u]);
+        }
+        ptd::drained_barrier();
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) give[u] = refs[u] > 0 && ptd::load_count(p.refs + ids[u]) == kGiver + seqs[u];
+      }
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) m += give[u];
+      Sums t;
+      int j = static_cast<int>(block_scan<NT>({m, 0, 0}, s_scan, &t).back);
+      freed = t.back;
+      const int count1 = count + static_cast<int>(min(freed, static_cast<long long>(p.s.num_pages - count)));
+#pragma unroll
+      for (int u = 0; u < kEach; ++u) {
+        if (give[u]) {
+          if (count1 - 1 - j >= count) p.s.free_pages[count1 - 1 - j] = ids[u];
+          p.refs[ids[u]] = 0;
+          ++j;
+        }
+      }
+      ptd::drained_barrier();
+    } else if (all.back > 0) {
       each([&](int, int id, bool ok, bool has) __attribute__((always_inline)) {
         if (ok ? ptd::add_count(p.refs + id, -1) <= 0 : has) ptd::report(p.dev_status, PTD_ERR_PAGE);
       });
@@ -235,7 +292,7 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
     }
     total = min(freed, static_cast<long long>(p.s.num_pages - count));
     long long done = 0;
-    if (freed > 0) {  // uniform
+    if (freed > 0 && !kept) {  // uniform
       const int count1 = count + static_cast<int>(total);
       each([&](int b, int id, bool ok, bool) __attribute__((always_inline)) {
         const bool mine = ok && ptd::load_count(p.refs + id) == kGiver + b;
@@ -275,6 +332,18 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
     }
     done += t.back;
     __syncthreads();
+  }
+  // whether a held page that gets rows is another sequence's too
+  __shared__ bool s_flag[SHARED && ONE ? NT : 1];
+  if constexpr (SHARED && ONE) {
+    bool flag = false;
+    if (tid < B && w.rows > 0) {
+      for (int k = w.kv >> p.page_shift; k < min(w.held, w.need) && !flag; ++k) {
+        const int id = table_of(p, tid)[k];
+        flag = static_cast<uint32_t>(id) >= static_cast<uint32_t>(p.s.num_pages) || ptd::load_count(p.refs + id) != 1;
+      }
+    }
+    s_flag[tid] = flag;
   }
   // ---- pages that are taken, in order while the list lasts; starts of the rows
   long long taken = 0, rows = 0;
@@ -345,7 +414,7 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
       if (rows > p.N) ptd::report(p.dev_status, PTD_ERR_ROWS);
     }
   }
-  if (p.N > kPlanRows) return;
+  if (p.N > (SHARED ? kPlanRowsShared : kPlanRows)) return;
   if (ONE) {
     // ids of pages that were held come from the table, of new ones from the free list
 #pragma unroll 4
@@ -363,7 +432,7 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
       const int pg = pos >> p.page_shift;
       const bool page = row && pg < s_need[b];
       const int32_t* from = pg < s_held[b] ? table_of(p, b) + pg : p.s.free_pages + (count1 - 1 - (s_off[b] + pg - s_held[b]));
-      put_row(p, i, !page ? -1 : pg < s_held[b] ? slot_in_held<SHARED>(p, *from, pos) : slot_at(p, *from, pos), row ? pos : -1);
+      put_row(p, i, !page ? -1 : SHARED && pg < s_held[b] && s_flag[b] ? slot_in_held<SHARED>(p, *from, pos) : slot_at(p, *from, pos), row ? pos : -1);
     }
   } else {
     if constexpr (SHARED) ptd::drained_barrier();
@@ -703,7 +772,7 @@ void launch_plan(const PlanParams& prm, hipStream_t st) {
   if (!large) hipLaunchKernelGGL((k_page_plan<true, kPlanSmall, SHARED>), dim3(1), dim3(kPlanSmall), 0, st, prm);
   else if (prm.s.B <= kPlanLarge) hipLaunchKernelGGL((k_page_plan<true, kPlanLarge, SHARED>), dim3(1), dim3(kPlanLarge), 0, st, prm);
   else hipLaunchKernelGGL((k_page_plan<false, kPlanLarge, SHARED>), dim3(1), dim3(kPlanLarge), 0, st, prm);
-  if (prm.N > kPlanRows) {
+  if (prm.N > (SHARED ? kPlanRowsShared : kPlanRows)) {
     const unsigned grid = static_cast<unsigned>((static_cast<long long>(prm.N) + kSlotRows - 1) / kSlotRows);
     hipLaunchKernelGGL((k_page_slots<SHARED>), dim3(grid), dim3(kSlotThreads), 0, st, prm);
   }

@@ -211,6 +211,146 @@ __global__ void __launch_bounds__(kThreads) k_page_fork(ForkArgs g) {
   }
 }
 
+// Last index x of [0, n) with a[x] <= v (a ascending, a[0] <= v).
+__device__ __forceinline__ int upper(const int* a, int n, int v) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a[mid] <= v) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// The same with a sequence per thread and the pages' counts in LDS: what is left in memory is four waits
+// one after the other (sequences, their sources, page ids, outputs), and nothing is changed
+// there before all checks are done.
+constexpr int kRound = 4 * kThreads;  // pages that the workgroup looks at in one turn
+template <int PAGES>
+__global__ void __launch_bounds__(kThreads) k_page_fork_lds(ForkArgs g) {
+  __shared__ int s_count[PAGES];
+  __shared__ int s_from[kThreads], s_whole[kThreads], s_off[kThreads], s_page[kThreads], s_free[kThreads];
+  __shared__ int s_scan[kWaves];
+  const int tid = threadIdx.x;
+  const int B = g.s.B, n = g.s.num_pages;
+  const int count = g.s.num_free[0];
+  int bad = count < 0 || count > n ? PTD_ERR_PAGE : 0;
+  Fork f = {-1, 0, 0};
+  int held = 0;
+  if (tid < B) {
+    f = fork_of(g, tid);
+    held = g.s.num_held[tid];
+    if (held < 0 || held > g.s.max_pages) bad = PTD_ERR_PAGE;
+    if (f.a < -1 || f.a >= B) bad = PTD_ERR_ROWS;
+    if (!bad && f.a >= 0) {
+      const int len = g.len[tid], have = g.s.num_held[f.a];
+      if (have < 0 || have > g.s.max_pages) bad = PTD_ERR_PAGE;
+      else if (len < 0 || len > static_cast<long long>(have) << g.page_shift) bad = PTD_ERR_KV_LEN;
+    }
+  }
+  if (tid < count && !bad) s_free[tid] = g.s.free_pages[count - 1 - tid];
+  for (int p = tid; p < n; p += kThreads) s_count[p] = 0;
+  if (bad) ptd::report(g.dev_status, bad);
+  bool refused = __syncthreads_or(bad != 0);
+  int copies = 0, at = 0, page = -1, mine = -1;
+  bool copy = false;
+  if (!refused) {
+    // ---- page ids: the whole ones are counted and go to the next table
+    int total;
+    const int off = block_scan(f.whole + (f.part > 0), s_scan, &total);
+    s_from[tid] = f.a, s_whole[tid] = f.whole, s_off[tid] = off;
+    __syncthreads();
+#pragma unroll 4
+    for (int e = tid; e < total; e += kThreads) {
+      const int b = upper(s_off, B, e), k = e - s_off[b];
+      const int id = table_of(g, s_from[b])[k];
+      if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(n)) bad = PTD_ERR_PAGE;
+      else if (k < s_whole[b]) atomicAdd(&s_count[id], 1);
+      if (k < s_whole[b]) g.table_next[static_cast<size_t>(b) * g.s.max_pages + k] = id;
+      else s_page[b] = id;
+    }
+    if (bad) ptd::report(g.dev_status, bad);
+    refused = __syncthreads_or(bad != 0);
+  }
+  if (!refused) {
+    // ---- who goes on in a page that nobody holds as a whole one: the lowest
+    const int me = kPart | (65535 - tid);
+    if (f.part > 0) {
+      page = s_page[tid];
+      const int v = s_count[page];
+      if ((v & kPart) || v == 0) atomicMax(&s_count[page], me);
+    }
+    __syncthreads();
+    copy = f.part > 0 && s_count[page] != me;
+    at = block_scan(copy, s_scan, &copies);
+    mine = page;
+    if (copies > count) {  // uniform
+      bad = PTD_ERR_NO_PAGES;
+      if (tid == 0) ptd::report(g.dev_status, bad);
+    } else if (copy) {
+      mine = s_free[at];
+      if (static_cast<uint32_t>(mine) >= static_cast<uint32_t>(n)) {
+        bad = PTD_ERR_PAGE;
+        ptd::report(g.dev_status, bad);
+      }
+    }
+    refused = __syncthreads_or(bad != 0);
+  }
+  if (refused) {  // nothing changes
+    for (int b = tid >> 6; b < B; b += kWaves) {
+      const int have = min(max(g.s.num_held[b], 0), g.s.max_pages);
+      for (int k = tid & 63; k < have; k += PTD_WAVE) g.table_next[static_cast<size_t>(b) * g.s.max_pages + k] = table_of(g, b)[k];
+    }
+    if (tid < B) {
+      g.held_next[tid] = held;
+      g.copy_src[tid] = g.copy_dst[tid] = -1;
+      g.copy_rows[tid] = 0;
+    }
+    return;
+  }
+  if (tid < B) {
+    if (copy) s_count[mine] = 1;
+    if (f.part > 0) g.table_next[static_cast<size_t>(tid) * g.s.max_pages + f.whole] = mine;
+    g.held_next[tid] = f.whole + (f.part > 0);
+    g.copy_src[tid] = copy ? page : -1;
+    g.copy_dst[tid] = copy ? mine : -1;
+    g.copy_rows[tid] = copy ? f.part : 0;
+  }
+  // ---- counts, and the pages that nobody holds any more, from the highest id down
+  int to = count - copies;
+  for (int p0 = (n - 1) / kRound * kRound; p0 >= 0; p0 -= kRound) {  // uniform
+    int old[4], gone[4], m = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int p = p0 + 4 * tid + u;
+      old[u] = p < n ? g.refs[p] : 0;
+    }
+    __syncthreads();  // (the fresh pages' counts)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int p = p0 + 4 * tid + u;
+      const int v = p < n ? s_count[p] : 0;
+      const int now = (v & kPart) ? 1 : v;
+      gone[u] = old[u] > 0 && now == 0;
+      m += gone[u];
+      if (p < n && now != old[u]) g.refs[p] = now;
+    }
+    int all;
+    int up = block_scan(m, s_scan, &all);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int j = to + all - 1 - up;
+      if (gone[u] && j < n) g.s.free_pages[j] = p0 + 4 * tid + u;
+      up += gone[u];
+    }
+    to += all;
+  }
+  if (tid == 0) {
+    if (to > n) ptd::report(g.dev_status, PTD_ERR_PAGE);  // pages that were held and free
+    g.s.num_free[0] = min(to, n);
+  }
+}
+
 struct CompactArgs {
   ptd_page_state s;
   int32_t* refs;
@@ -281,6 +421,102 @@ __global__ void __launch_bounds__(kThreads) k_page_compact(CompactArgs g) {
   for (int i = tid; i < movers; i += kThreads) g.refs[g.move_src[i]] = 0;
   for (int i = tid; i < n - live; i += kThreads) g.s.free_pages[i] = n - 1 - i;
   if (tid == 0) g.s.num_free[0] = n - live;
+}
+
+// The same with a sequence per thread, counts and moves in LDS.
+constexpr int kCompactPages = 8192;
+__global__ void __launch_bounds__(kThreads) k_page_compact_lds(CompactArgs g) {
+  __shared__ int s_ref[kCompactPages], s_src[kCompactPages / 2], s_dst[kCompactPages / 2];
+  __shared__ int s_off[kThreads];
+  __shared__ int s_scan[kWaves];
+  const int tid = threadIdx.x;
+  const int n = g.s.num_pages, B = g.s.B;
+  int held = tid < B ? g.s.num_held[tid] : 0;
+  if (held < 0 || held > g.s.max_pages) {
+    ptd::report(g.dev_status, PTD_ERR_PAGE);
+    held = 0;
+  }
+  int mine = 0, live, entries;
+#pragma unroll 4
+  for (int p = tid; p < n; p += kThreads) {
+    const int v = g.refs[p];
+    if (v < 0) {  // (no count: free)
+      g.refs[p] = 0;
+      ptd::report(g.dev_status, PTD_ERR_PAGE);
+    }
+    s_ref[p] = max(v, 0);
+    mine += v > 0;
+  }
+  s_off[tid] = block_scan(held, s_scan, &entries);
+  block_scan(mine, s_scan, &live);
+  // ids of the first entries, on their way while the moves are found
+  auto place = [&](int e) {
+    const int b = upper(s_off, B, e);
+    return g.s.page_table + static_cast<size_t>(b) * g.s.max_pages + (e - s_off[b]);
+  };
+  int32_t* where[4];
+  int id[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int e = tid + u * kThreads;
+    if (e < entries) where[u] = place(e), id[u] = *where[u];
+  }
+  int before = 0, movers = 0;  // live pages below the turn's first, movers among them
+  for (int p0 = 0; p0 < n; p0 += kRound) {  // uniform
+    int v[4], m = 0, all;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int p = p0 + 4 * tid + u;
+      v[u] = p < n ? s_ref[p] : 0;
+      m += v[u] > 0;
+    }
+    const int base = before + block_scan(m, s_scan, &all);
+    int at = base;  // live pages below p; of the free ones below `live` the p - at first come before p
+    int moving = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) moving += v[u] > 0 && p0 + 4 * tid + u >= live;
+    int some;
+    int j = movers + block_scan(moving, s_scan, &some);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int p = p0 + 4 * tid + u;
+      if (v[u] > 0) {
+        if (p >= live) s_src[j++] = p;
+        ++at;
+      } else if (p < live) {
+        s_dst[p - at] = p;
+      }
+    }
+    before += all;
+    movers += some;
+  }
+  __syncthreads();
+  for (int i = tid; i < n / 2; i += kThreads) {
+    const bool move = i < movers;
+    const int a = move ? s_src[i] : -1, b = move ? s_dst[i] : -1;
+    g.move_src[i] = a;
+    g.move_dst[i] = b;
+    if (move) {
+      g.refs[b] = s_ref[a];
+      g.refs[a] = 0;
+      s_ref[a] = -1 - b;
+    }
+  }
+  for (int i = tid; i < n - live; i += kThreads) g.s.free_pages[i] = n - 1 - i;
+  if (tid == 0) g.s.num_free[0] = n - live;
+  __syncthreads();
+  auto change = [&](int32_t* w, int x) {
+    if (static_cast<uint32_t>(x) >= static_cast<uint32_t>(n)) ptd::report(g.dev_status, PTD_ERR_PAGE);
+    else if (s_ref[x] < 0) *w = -1 - s_ref[x];
+  };
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    if (tid + u * kThreads < entries) change(where[u], id[u]);
+#pragma unroll 4
+  for (int e = tid + 4 * kThreads; e < entries; e += kThreads) {
+    int32_t* w = place(e);
+    change(w, *w);
+  }
 }
 
 // ===========================================================================
@@ -365,6 +601,11 @@ __global__ void __launch_bounds__(kCopyThreads) k_page_copy(CopyArgs g) {
   }
 }
 
+// A thread for every sequence, and all table entries counted in 31 bits.
+bool one_turn(const ptd_page_state& s) {
+  return s.B <= kThreads && static_cast<long long>(s.B) * s.max_pages <= 0x3FFFFFFFLL;
+}
+
 }  // namespace
 
 extern "C" int ptd_page_fork(const ptd_page_state* state, int32_t* refs, const int32_t* from, const int32_t* len,
@@ -385,7 +626,11 @@ extern "C" int ptd_page_fork(const ptd_page_state* state, int32_t* refs, const i
   g.copy_dst = copy_dst;
   g.copy_rows = copy_rows;
   g.dev_status = dev_status;
-  hipLaunchKernelGGL(k_page_fork, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), g);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool small = one_turn(*state);
+  if (small && state->num_pages <= 8192) hipLaunchKernelGGL((k_page_fork_lds<8192>), dim3(1), dim3(kThreads), 0, st, g);
+  else if (small && state->num_pages <= 32768) hipLaunchKernelGGL((k_page_fork_lds<32768>), dim3(1), dim3(kThreads), 0, st, g);
+  else hipLaunchKernelGGL(k_page_fork, dim3(1), dim3(kThreads), 0, st, g);
   return ptd_launch_status();
 }
 
@@ -401,7 +646,9 @@ extern "C" int ptd_page_compact(const ptd_page_state* state, int32_t* refs, int3
   g.move_src = move_src;
   g.move_dst = move_dst;
   g.dev_status = dev_status;
-  hipLaunchKernelGGL(k_page_compact, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), g);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (one_turn(*state) && state->num_pages <= kCompactPages) hipLaunchKernelGGL(k_page_compact_lds, dim3(1), dim3(kThreads), 0, st, g);
+  else hipLaunchKernelGGL(k_page_compact, dim3(1), dim3(kThreads), 0, st, g);
   return ptd_launch_status();
 }
 

@@ -82,6 +82,30 @@ def test_forks_and_plans_follow_the_lists(P, B, page, per):
     assert t.num_free.item() == num and (t.refs == 0).all()
 
 
+@pytest.mark.parametrize("num", [8192, 8193, 32768, 32769])
+def test_large_pools(P, num):
+    # (the kernels' counts move from one place to another at these sizes)
+    r = random.Random(num)
+    B, page, per = 7, 2, 3000
+    t, ref = P.PageTables(B, page, per, num, shared=True), R.SharedPages(B, page, per, num)
+    kv = [0] * B
+    for s in range(3):
+        new, left = [0] * B, len(ref.free)
+        for b in range(B):
+            if kv[b] < 100:
+                new[b] = r.randint(0, min(per * page - kv[b], max(0, left - 3) * page))
+                left -= -(-new[b] // page) + 1
+        plan(t, ref, kv, new)
+        kv = [a + n for a, n in zip(kv, new)]
+        frm = [r.choice([b, r.randrange(B), -1]) for b in range(B)]
+        kv = [0 if a < 0 else r.randint(0, kv[a]) for a in frm]
+        assert fork(t, ref, frm, kv)[3]
+        st = i32([0])
+        src, dst = t.compact(st)
+        assert st.item() == 0 and (src.tolist(), dst.tolist()) == ref.compact()
+        check_state(t, ref)
+
+
 def test_samples_of_one_prompt(P):
     # 100 rows of pages of 32: three shared pages, the last one each sample's own
     t, ref = P.PageTables(5, 32, 8, 40, shared=True), R.SharedPages(5, 32, 8, 40)
@@ -119,15 +143,15 @@ def test_rows_never_go_to_shared_pages(P):
 
 def test_pages_given_up_by_several_at_once(P):
     # all holders of shared pages end in one call, in rounds of sequences too
-    for B, page in ((7, 8), (700, 4), (1500, 4)):
-        t, ref = P.PageTables(B, page, 6, 6 * 40, shared=True), R.SharedPages(B, page, 6, 6 * 40)
-        lens = [page * 5 if b < 7 else 0 for b in range(B)]
+    for B, page, more in ((7, 8, 1), (200, 2, 100), (700, 4, 1), (1500, 4, 1), (300, 1, 1500)):
+        t, ref = P.PageTables(B, page, 6 * more, 6 * 40 * more, shared=True), R.SharedPages(B, page, 6 * more, 6 * 40 * more)
+        lens = [page * 5 * more if b < 7 else 0 for b in range(B)]
         plan(t, ref, [0] * B, lens)
-        fork(t, ref, [b % 7 for b in range(B)], [page * (1 + b % 5) for b in range(B)])
+        fork(t, ref, [b % 7 for b in range(B)], [page * (1 + b % 5) * (more if b < 20 else 1) for b in range(B)])
         plan(t, ref, [0 if b % 3 else page for b in range(B)], [0] * B)
         plan(t, ref, [0] * B, [page if b % 50 == 0 else 0 for b in range(B)])
         plan(t, ref, [0] * B, [0] * B)
-        assert t.num_free.item() == 240
+        assert t.num_free.item() == 240 * more
 
 
 def test_fork_refusals_change_nothing(P):
