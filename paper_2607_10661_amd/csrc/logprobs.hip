@@ -8,13 +8,20 @@
 // log1p of it.
 //
 // Kernels
-//   k_logp_row    one workgroup per (entry, slice of its row), the slice in registers: its
-//                 maximum first, so no sum is ever scaled anew, then one exponential per
-//                 element, then the selection of the best ones (topk_select.hpp).
+//   k_logp_row    one workgroup per (entry, slice of its row), the slice in registers (256 threads
+//                 x 16 chunks of 16 bytes, or 4).  One pass: a wave's terms are worked out relative to the
+//                 largest entry that it has seen, four chunks at a time, while others are on
+//                 their way; the sums of the waves are then brought to the slice's largest, and
+//                 the best entries are selected (topk_select.hpp).
+//   k_logp_path   the same for entries along accepted paths, few of which are there.
 //   k_logp_merge  one workgroup per entry joins the slices' sums, in their order, and ranks
-//                 their best entries by counting (rows of several slices).
-// Per element the sums take a subtraction, a product, the exponential, a sum, a bound and a
-// product-sum; terms are fp32, the sums of a wave are joined in fp64.
+//                 their best entries (rows of several slices).
+// An element costs its unpacking, a multiply-add, the exponential, a sum and a multiply-add, and 1.4
+// more for its chunk's largest: about 40 us of the vector units for 1040 rows x 128256, beside 51 of
+// HBM.  That takes 64 us in all with the 8 best entries and 52 without (a version that needed the
+// row's largest entry first took 77 and 58, 512 threads x 8 chunks 70); 97 rows x 32003 fp32 12
+// us, a single row 11, both the latency of two launches and of six barriers.
+// Terms and the sums of a wave are fp32, waves and slices are joined in fp64.
 #include <math.h>
 
 #include <algorithm>
@@ -174,45 +181,77 @@ struct RowLds {
   Totals totals;
 };
 
-template <bool BF16, int NL, typename Add>
-__device__ __forceinline__ void each_element(const uint4 (&cw)[NL], const Slice& sl, uint32_t bt, int tid, Add add) {
+// The sums with care, relative to the wave's largest entry: entries that equal m are counted and
+// left out, and what lies so far below that it has no weight (-inf; the type's lowest number
+// overflows to it) is raised to where it has none and the weighted sum stays a number.  The
+// elements are read again, so that the common way has their registers.
+template <bool BF16>
+__device__ __forceinline__ WaveSums careful_sums(const char* rb, const Slice& sl, uint32_t bt, int tid, float top, float m, float scale) {
+  constexpr int E = BF16 ? 8 : 4;
+  float r = 0.f, w = 0.f;
+  int n = 0;
+  bool nan = false;
+  const float c = top * scale;
+  const float none = -1.2e6f / scale;  // its exponent is -1.1e6 or less
+  auto add = [&](float x) __attribute__((always_inline)) {
+    nan |= x != x;
+    n += x == m ? 1 : 0;
+    const float arg = fmaf(x == m ? none : fmaxf(x, none), scale, -c);
+    const float e = __builtin_amdgcn_exp2f(arg);
+    r += e;
+    w = fmaf(e, arg, w);
+  };
+  const uint4* src = reinterpret_cast<const uint4*>(rb + static_cast<size_t>(sl.vb) * (BF16 ? 2 : 4));
+#pragma unroll 1
+  for (int c0 = tid; c0 < sl.nfull; c0 += 4 * kThreads) {
+    uint4 x[4];
 #pragma unroll
-  for (int u = 0; u < NL; ++u) {
-    if (u * kThreads + tid < sl.nfull) {
+    for (int u = 0; u < 4; ++u) x[u] = src[min(c0 + u * kThreads, sl.nfull - 1)];
 #pragma unroll
-      for (int e = 0; e < (BF16 ? 8 : 4); ++e) add(__uint_as_float(chunk_bits<BF16>(cw[u], e)));
+    for (int u = 0; u < 4; ++u) {
+      if (c0 + u * kThreads < sl.nfull) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) add(__uint_as_float(chunk_bits<BF16>(x[u], e)));
+      }
     }
   }
   if (sl.tail) add(__uint_as_float(bt));
+  // (where c is larger no entry but the largest has a weight: its distance is at least 2^-23 of c; and
+  // where the wave's is not the slice's largest, neither has that one)
+  if (!(fabsf(c) < 0x1p30f)) r = w = 0.f;
+  if (__any(nan) || !(fabsf(top) < INFINITY)) r = NAN;
+  return {c, wave_sum_dpp(r), wave_sum_dpp(w), top, wave_sum_dpp(static_cast<float>(n))};
 }
 
-// The sums with care, relative to the wave's largest entry: entries that equal m are counted and
-// left out, and so is what lies so far below it that it has no weight (-inf; the type's lowest
-// number overflows to it).
+// The wave's sums where its lane `at` alone holds entries that equal m, and these make up most of
+// them: what that lane has besides would be lost in its own sum, so the lane's elements are read
+// again, dealt out over the wave.
 template <bool BF16, int NL>
-__device__ __forceinline__ WaveSums careful_sums(uint4 (&cw)[NL], const Slice& sl, uint32_t bt, int tid, float top, float m, float scale) {
-  float r = 0.f, w = 0.f, n = 0.f;
-  const float c = top * scale;
-  const float none = __uint_as_float(__float_as_uint(-1.2e6f / scale) & 0xFFFF0000u);  // its exponent is -1.1e6 or less
-  // (where c is larger no entry but the largest has a weight: its distance is at least 2^-23 of c)
-  const bool near = fabsf(c) < 0x1p30f;
-  each_element<BF16, NL>(cw, sl, bt, tid, [&](float x) __attribute__((always_inline)) {
-    const float arg = fmaf(x < none ? none : x, scale, -c);
-    const float e = near ? __builtin_amdgcn_exp2f(arg) : x == top ? 1.f : 0.f;
-    const bool one = x == m;
-    n += one ? 1.f : 0.f;
-    r += one ? 0.f : e;
-    w += one || !near ? 0.f : e * arg;
-  });
-  if (!(fabsf(top) < INFINITY)) r = top - top;  // not a number
-  return {c, wave_sum_dpp(r), wave_sum_dpp(w), top, wave_sum_dpp(n)};
+__device__ __forceinline__ WaveSums without_top(const char* rb, const Slice& sl, uint32_t bt, int tid, int at, float m, float scale,
+                                                float c, float sum, float weighted, float top) {
+  constexpr int E = BF16 ? 8 : 4;
+  const int lane = tid & 63, chunk = lane / 4 * kThreads + (tid - lane) + at;
+  float r = lane == at ? 0.f : sum, w = lane == at ? 0.f : weighted;
+  int n = 0;
+  auto add = [&](float x) __attribute__((always_inline)) {
+    const float arg = fmaf(x, scale, -c);
+    const float e = __builtin_amdgcn_exp2f(arg);
+    n += x == m ? 1 : 0;
+    r += x == m ? 0.f : e;
+    w += x == m ? 0.f : e * arg;
+  };
+  if (lane / 4 < NL && chunk < sl.nfull) {
+    const uint32_t x = *reinterpret_cast<const uint32_t*>(rb + (static_cast<size_t>(sl.vb) + static_cast<size_t>(chunk) * E) * (BF16 ? 2 : 4) + lane % 4 * 4);
+    if constexpr (BF16) add(bf16_lo(x)), add(bf16_hi(x));
+    else add(__uint_as_float(x));
+  }
+  if (lane == at && sl.tail) add(__uint_as_float(bt));
+  return {c, wave_sum_dpp(r), wave_sum_dpp(w), top, wave_sum_dpp(static_cast<float>(n))};
 }
 
 // One slice of the row that entry r reads.  A wave's terms are relative to the largest entry of its
-// first chunks, so they are worked out while the other chunks are on their way; a wave whose
-// later entries lie far above, or whose weighted sum is no number (masked entries), takes
-// them once more with care.  So does the wave with the row's largest entry where that makes up most of
-// its sum.
+// first chunks, so they are worked out while others are on their way; where later ones hold one that is
+// 2^8 times as likely, the sums go on from there.
 template <int KMAX, bool BF16, int NL, bool ONE>
 __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, int r, int row, int token, int slice, int tid) {
   constexpr int NW = kThreads / PTD_WAVE;
@@ -226,26 +265,52 @@ __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, i
   const uint32_t bt = sl.tail ? elem_bits<BF16>(rb, sl.vt) : 0u;
   // (by every thread, or none: a wait less where it is needed)
   const float xt = token >= sl.v0 && token < sl.v1 ? __uint_as_float(elem_bits<BF16>(rb, token)) : 0.f;
-  // (short slices: the edge elements and the first chunk may be all that a wave has, or nothing)
-  const uint32_t first = max(tid < sl.nfull ? chunk_img<BF16>(cw[0]) : 0u, NL == 1 || sl.nfull < kThreads ? (sl.tail ? elem_img<BF16>(bt) : 0u) : 0u);
-  const float ref = image_value<BF16>(group_max_min<64>(first));
-  const float c = ref * a.scale;
-  float sum = 0.f, weighted = 0.f;
-  each_element<BF16, NL>(cw, sl, bt, tid, [&](float x) __attribute__((always_inline)) {
+  // the sums, four chunks at a time
+  uint32_t lm = sl.tail ? elem_img<BF16>(bt) : 0u, limit = 0;
+  float c = 0.f, sum = 0.f, weighted = 0.f;
+  auto add = [&](float x) __attribute__((always_inline)) {
     const float arg = fmaf(x, a.scale, -c);
     const float e = __builtin_amdgcn_exp2f(arg);
     sum += e;
     weighted = fmaf(e, arg, weighted);
-  });
-  uint32_t lm = sl.tail ? elem_img<BF16>(bt) : 0u;
+  };
+  static_assert(NL % 4 == 0, "groups of four chunks");
 #pragma unroll
-  for (int u = 0; u < NL; ++u) lm = max(lm, u * kThreads + tid < sl.nfull ? chunk_img<BF16>(cw[u]) : 0u);
+  for (int u0 = 0; u0 < NL; u0 += 4) {
+    uint32_t img = u0 == 0 ? lm : 0u;
+#pragma unroll
+    for (int u = u0; u < u0 + 4; ++u) img = max(img, u * kThreads + tid < sl.nfull ? chunk_img<BF16>(cw[u]) : 0u);
+    lm = max(lm, img);
+    if (__any(img > limit)) {
+      const uint32_t most = group_max_min<64>(img);
+      const float ref = image_value<BF16>(most);
+      const float next = ref > -INFINITY ? ref * a.scale : 0.f;  // (masked entries alone: any number)
+      const float f = __builtin_amdgcn_exp2f(c - next);
+      weighted = u0 == 0 ? 0.f : f * fmaf(c - next, sum, weighted);
+      sum = u0 == 0 ? 0.f : f * sum;
+      c = next;
+      limit = max(most, elem_img<BF16>(__float_as_uint(ref + 8.f / a.scale)));
+    }
+#pragma unroll
+    for (int u = u0; u < u0 + 4; ++u) {
+      if (u * kThreads + tid < sl.nfull) {
+#pragma unroll
+        for (int e = 0; e < (BF16 ? 8 : 4); ++e) add(__uint_as_float(chunk_bits<BF16>(cw[u], e)));
+      }
+    }
+  }
+  // (the compiler would keep the chunks' images for the lists: registers that it then spills the
+  // chunks from, 1040 rows x 128256 80 us and 64)
+  if constexpr (KMAX > 0) {
+#pragma unroll
+    for (int u = 0; u < NL; ++u) asm volatile("" : "+v"(cw[u].x), "+v"(cw[u].y), "+v"(cw[u].z), "+v"(cw[u].w));
+  }
+  if (sl.tail) add(__uint_as_float(bt));
   const uint32_t img = group_max_min<64>(lm);
   const float top = img ? image_value<BF16>(img) : -INFINITY;  // (a wave without an element)
-  sum = wave_sum_dpp(sum);
-  weighted = wave_sum_dpp(weighted);
-  bool care = !(weighted - weighted == 0.f) || !((top - ref) * a.scale <= 8.f) || !(fabsf(c) < 0x1p20f);
-  if (lane == 0) sh.sums[wave] = {c, sum, weighted, top, 0.f};
+  const float all = wave_sum_dpp(sum), all_weighted = wave_sum_dpp(weighted);
+  const bool care = !(all_weighted - all_weighted == 0.f) || !(fabsf(c) < 0x1p20f);
+  if (lane == 0) sh.sums[wave] = {c, all, all_weighted, top, 0.f};
   if constexpr (KMAX > 0) topk_groups<KMAX, kThreads>(sh.topk, lm, tid);
   lds_barrier();
   uint32_t tc = 0;
@@ -259,13 +324,16 @@ __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, i
     m = fmaxf(m, x);
   }
   if (nan) m = NAN;
-  // e of the largest entry is 2^(top * scale - c)
-  care |= top == m && !(sum >= 2.f * __builtin_amdgcn_exp2f(fmaf(top, a.scale, -c)));
   lds_barrier();  // sh.sums is read
   if (top == -INFINITY) {
     if (lane == 0) sh.sums[wave] = {0.f, 0.f, 0.f, top, 0.f};
   } else if (care) {
-    const WaveSums s = careful_sums<BF16, NL>(cw, sl, bt, tid, top, m, a.scale);
+    const WaveSums s = careful_sums<BF16>(rb, sl, bt, tid, top, m, a.scale);
+    if (lane == 0) sh.sums[wave] = s;
+  } else if (top == m && !(all >= 2.f * __builtin_amdgcn_exp2f(fmaf(top, a.scale, -c)))) {
+    // (e of the largest entry is 2^(top * scale - c); two lanes with one of it each are half of the sum)
+    const uint64_t who = __ballot(lm == img);
+    const WaveSums s = without_top<BF16, NL>(rb, sl, bt, tid, __builtin_ctzll(who), m, a.scale, c, sum, weighted, top);
     if (lane == 0) sh.sums[wave] = s;
   }
   if constexpr (KMAX > 0) topk_examine<BF16, kThreads>(sh.topk, sl, tc, tid);
@@ -338,29 +406,30 @@ __global__ void __launch_bounds__(kThreads, 4) k_logp_path(LogpArgs a) {
   const bool tell = way == 0 && slice == 0 && tid < PTD_WAVE;
   int seen = 0;
   for (int j0 = 0; j0 < n; j0 += kPartChunks * PTD_WAVE) {  // uniform: every wave reads the same tokens
-    int rows[kPartChunks], tokens[kPartChunks];
+    uint64_t there[kPartChunks];
 #pragma unroll
     for (int u = 0; u < kPartChunks; ++u) {
       const int j = j0 + u * PTD_WAVE + lane;
-      rows[u] = tokens[u] = -1;
-      if (j < n) rows[u] = entry_row(a, r0 + j, &tokens[u], tell);
+      int token;
+      const int row = j < n ? entry_row(a, r0 + j, &token, tell) : -1;
+      there[u] = __ballot(row >= 0);
       // (of several slices: k_logp_merge)
-      if (ONE && tell && j < n && rows[u] < 0) {
+      if (ONE && tell && j < n && row < 0) {
         for (int k = 0; k < max(a.k, 1); ++k) put_nothing(a, r0 + j, k);
       }
     }
 #pragma unroll 1
     for (int u = 0; u < kPartChunks; ++u) {
       static_assert(kPartChunks == 4, "four of them");
-      const int row = u == 0 ? rows[0] : u == 1 ? rows[1] : u == 2 ? rows[2] : rows[3];
-      const int token = u == 0 ? tokens[0] : u == 1 ? tokens[1] : u == 2 ? tokens[2] : tokens[3];
-      for (uint64_t live = __ballot(row >= 0); live; live &= live - 1) {
+      uint64_t live = u == 0 ? there[0] : u == 1 ? there[1] : u == 2 ? there[2] : there[3];
+      for (; live; live &= live - 1) {
         const bool mine = seen == way;
         seen = seen + 1 == a.ways ? 0 : seen + 1;
         if (!mine) continue;
-        const int at = __builtin_ctzll(live);
-        row_slice<KMAX, BF16, NL, ONE>(a, sh, r0 + j0 + u * PTD_WAVE + at, __builtin_amdgcn_readlane(row, at),
-                                       __builtin_amdgcn_readlane(token, at), slice, tid);
+        const int r = r0 + j0 + u * PTD_WAVE + __builtin_ctzll(live);
+        int token;
+        const int row = entry_row(a, r, &token, false);
+        row_slice<KMAX, BF16, NL, ONE>(a, sh, r, row, token, slice, tid);
         lds_barrier();
       }
     }
@@ -452,7 +521,10 @@ struct LogpPlan {
   size_t ws_bytes;
 };
 
-// path: the rows that are there are about four per sequence, whatever R.
+// Slices of 16 chunks a thread, or of 4 where workgroups would be fewer than two per CU: k = 5, bf16, 128256
+// entries, 4 / 16 chunks: a row 9.7 / 11.4 us, 64 rows 14.2 / 16.2, 128 rows 17.9 / 18.0, 256 rows 25.1 / 23.6, 1040
+// rows 74 / 63.  (The pairs of a row's slices have to fit the merge.)
+// path_seqs: entries lie along paths, and about four per sequence are there, whatever R.
 bool make_plan(int R, int V, int k, int elem_bytes, int path_seqs, LogpPlan* p) {
   if (R < 1 || V < 1 || V > kMaxVocab || k < 0 || k > PTD_MAX_K || k > V) return false;
   const int E = 16 / elem_bytes;
