@@ -314,7 +314,7 @@ __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, i
   if constexpr (KMAX > 0) topk_groups<KMAX, kThreads>(sh.topk, lm, tid);
   lds_barrier();
   uint32_t tc = 0;
-  if constexpr (KMAX > 0) tc = topk_list<KMAX, BF16, kThreads, NL>(sh.topk, cw, sl, bt, tid);
+  if constexpr (KMAX > 0) tc = topk_list<KMAX, BF16, kThreads, NL>(sh.topk, cw, sl, bt, tid, [&](int u) { return chunk_img<BF16>(cw[u]); });
   float m = sh.sums[0].top;
   bool nan = m != m;
 #pragma unroll

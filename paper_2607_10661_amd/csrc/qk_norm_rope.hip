@@ -38,7 +38,7 @@ struct QkArgs {
 };
 
 // cos and sin of a >= 0 (any size that a position can give), in fp64: a less its multiple of
-// pi / 2 (three parts of it: a position of 31 bits leaves 2^-50), then the series of both up to
+// pi / 2 (two doubles of it, which leave less than the rounding of the angle), then the series of both up to
 // the 16th power of |r| <= pi / 4 (what follows is below 2^-54).
 __device__ __forceinline__ float2 cos_sin(double a) {
   const double n = rint(a * 0x1.45f306dc9c883p-1);  // 2 / pi

@@ -222,14 +222,14 @@ __device__ __forceinline__ int upper(const int* a, int n, int v) {
   return lo;
 }
 
-// The same with a sequence per thread and the pages' counts in LDS: what is left in memory is four waits
+// The same as k_page_fork with a sequence per thread and the pages' counts in LDS: what is left in memory is four waits
 // one after the other (sequences, their sources, page ids, outputs), and nothing is changed
 // there before all checks are done.
 constexpr int kRound = 4 * kThreads;  // pages that the workgroup looks at in one turn
 template <int PAGES>
 __global__ void __launch_bounds__(kThreads) k_page_fork_lds(ForkArgs g) {
   __shared__ int s_count[PAGES];
-  __shared__ int s_from[kThreads], s_whole[kThreads], s_off[kThreads], s_page[kThreads], s_free[kThreads];
+  __shared__ int s_from[kThreads], s_whole[kThreads], s_part[kThreads], s_page[kThreads], s_free[kThreads];
   __shared__ int s_scan[kWaves];
   const int tid = threadIdx.x;
   const int B = g.s.B, n = g.s.num_pages;
@@ -255,19 +255,48 @@ __global__ void __launch_bounds__(kThreads) k_page_fork_lds(ForkArgs g) {
   int copies = 0, at = 0, page = -1, mine = -1;
   bool copy = false;
   if (!refused) {
-    // ---- page ids: the whole ones are counted and go to the next table
-    int total;
-    const int off = block_scan(f.whole + (f.part > 0), s_scan, &total);
-    s_from[tid] = f.a, s_whole[tid] = f.whole, s_off[tid] = off;
+    // ---- page ids: the whole ones are counted and go to the next table.  A wave has every 16th sequence
+    // (fewer than 16: a sequence several waves), 64 ids a step; those of four sequences are in flight
+    // together.  (The kernel with 64 beams of 80 pages 8.0 us, and 11.2 with a thread per entry that finds its
+    // sequence by halving)
+    s_from[tid] = f.a, s_whole[tid] = f.whole, s_part[tid] = f.part > 0;
     __syncthreads();
-#pragma unroll 4
-    for (int e = tid; e < total; e += kThreads) {
-      const int b = upper(s_off, B, e), k = e - s_off[b];
-      const int id = table_of(g, s_from[b])[k];
-      if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(n)) bad = PTD_ERR_PAGE;
-      else if (k < s_whole[b]) atomicAdd(&s_count[id], 1);
-      if (k < s_whole[b]) g.table_next[static_cast<size_t>(b) * g.s.max_pages + k] = id;
-      else s_page[b] = id;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int more = __builtin_clz(static_cast<unsigned>(min(B, kWaves))) - __builtin_clz(static_cast<unsigned>(kWaves));  // log2 of the waves of one
+    const int ways = 1 << more, units = B << more;
+    for (int u0 = wave; u0 < units; u0 += 4 * kWaves) {  // uniform
+      int most = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int b = min((u0 + u * kWaves) >> more, B - 1);
+        most = max(most, s_whole[b] + s_part[b]);
+      }
+      for (int c = 0; c < most; c += 2 * ways * PTD_WAVE) {
+        int id[4][2];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int unit = u0 + u * kWaves, b = min(unit >> more, B - 1), k = c + ((unit & (ways - 1)) * 2 + h) * PTD_WAVE + lane;
+            id[u][h] = -1;
+            if (unit < units && k < s_whole[b] + s_part[b]) id[u][h] = table_of(g, s_from[b])[k];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int unit = u0 + u * kWaves, b = min(unit >> more, B - 1), k = c + ((unit & (ways - 1)) * 2 + h) * PTD_WAVE + lane;
+            if (unit < units && k < s_whole[b] + s_part[b]) {
+              const int x = id[u][h];
+              if (static_cast<uint32_t>(x) >= static_cast<uint32_t>(n)) bad = PTD_ERR_PAGE;
+              else if (k < s_whole[b]) atomicAdd(&s_count[x], 1);
+              if (k < s_whole[b]) g.table_next[static_cast<size_t>(b) * g.s.max_pages + k] = x;
+              else s_page[b] = x;
+            }
+          }
+        }
+      }
     }
     if (bad) ptd::report(g.dev_status, bad);
     refused = __syncthreads_or(bad != 0);
@@ -564,40 +593,51 @@ __device__ __forceinline__ void copy_piece(const char* from, char* to, uint32_t 
   }
 }
 
-// One workgroup per (pair, piece of its page) in turn, an array of pages per grid row.  Bound by
-// HBM, reads and writes mixed.
+// One workgroup per (pair, piece of its page) in turn, an array of pages per grid row.  Each lane
+// looks up one of the workgroup's next 64 items, so lists that are mostly -1 (a compaction's) cost a wait per 64
+// (4096 pairs in 24 arrays, 10 of them there: 7 us, and 50 where each item was looked up by itself).
+// Bound by HBM, reads and writes mixed.
 __global__ void __launch_bounds__(kCopyThreads) k_page_copy(CopyArgs g) {
   const CopyArray a = g.arrays[blockIdx.y];
   const long long items = static_cast<long long>(g.n) * g.pieces;
   const uint32_t step = static_cast<uint32_t>(a.units) * a.unit_bytes / a.granule;  // of a head, in elements
   const long long page = static_cast<long long>(a.heads) * a.units * a.unit_bytes;
-  for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-    const int i = static_cast<int>(item / g.pieces);
-    const uint32_t first = static_cast<uint32_t>(item - static_cast<long long>(i) * g.pieces) * (kCopyThreads * kUnroll);
-    const int s = g.src[i], d = g.dst[i];
-    if (s == -1 || d == -1 || s == d) continue;
-    if (static_cast<uint32_t>(s) >= static_cast<uint32_t>(g.num_pages) || static_cast<uint32_t>(d) >= static_cast<uint32_t>(g.num_pages)) {
-      if (threadIdx.x == 0) ptd::report(g.dev_status, PTD_ERR_PAGE);
-      continue;
-    }
-    int units = a.units;
-    if (g.rows) {
-      const int r = g.rows[i];
-      if (r < 0 || r > static_cast<long long>(a.units) * a.unit_rows) {
-        if (threadIdx.x == 0) ptd::report(g.dev_status, PTD_ERR_ROWS);
-        continue;
+  const int lane = threadIdx.x & 63;
+  for (long long base = blockIdx.x; base < items; base += static_cast<long long>(PTD_WAVE) * gridDim.x) {  // uniform
+    const long long item = base + static_cast<long long>(lane) * gridDim.x;
+    int s = -1, d = -1, units = a.units;
+    uint32_t first = 0;
+    if (item < items) {
+      const int i = static_cast<int>(item / g.pieces);
+      first = static_cast<uint32_t>(item - static_cast<long long>(i) * g.pieces) * (kCopyThreads * kUnroll);
+      s = g.src[i], d = g.dst[i];
+      const int r = g.rows ? g.rows[i] : 0;
+      if (s == -1 || d == -1 || s == d) {
+        s = -1;
+      } else if (static_cast<uint32_t>(s) >= static_cast<uint32_t>(g.num_pages) || static_cast<uint32_t>(d) >= static_cast<uint32_t>(g.num_pages)) {
+        ptd::report(g.dev_status, PTD_ERR_PAGE);
+        s = -1;
+      } else if (g.rows) {
+        if (r < 0 || r > static_cast<long long>(a.units) * a.unit_rows) {
+          ptd::report(g.dev_status, PTD_ERR_ROWS);
+          s = -1;
+        }
+        units = static_cast<int>((static_cast<long long>(r) + a.unit_rows - 1) / a.unit_rows);
       }
-      units = static_cast<int>((static_cast<long long>(r) + a.unit_rows - 1) / a.unit_rows);
     }
-    const uint32_t run = static_cast<uint32_t>(units) * a.unit_bytes / a.granule, total = run * a.heads;
-    if (first >= total) continue;
-    const char* from = a.base + s * page;
-    char* to = a.base + d * page;
-    const uint32_t one = units == a.units ? total : run;
-    if (a.granule == 16) copy_piece<uint4>(from, to, total, one, step, first);
-    else if (a.granule == 4) copy_piece<uint32_t>(from, to, total, one, step, first);
-    else if (a.granule == 2) copy_piece<uint16_t>(from, to, total, one, step, first);
-    else copy_piece<uint8_t>(from, to, total, one, step, first);
+    const uint32_t run_of = static_cast<uint32_t>(units) * a.unit_bytes / a.granule;
+    for (uint64_t live = __ballot(s >= 0 && first < run_of * a.heads); live; live &= live - 1) {  // uniform
+      const int l = __builtin_ctzll(live);
+      const uint32_t run = __builtin_amdgcn_readlane(run_of, l), total = run * a.heads;
+      const char* from = a.base + __builtin_amdgcn_readlane(s, l) * page;
+      char* to = a.base + __builtin_amdgcn_readlane(d, l) * page;
+      const uint32_t at = __builtin_amdgcn_readlane(first, l);
+      const uint32_t one = run == step ? total : run;
+      if (a.granule == 16) copy_piece<uint4>(from, to, total, one, step, at);
+      else if (a.granule == 4) copy_piece<uint32_t>(from, to, total, one, step, at);
+      else if (a.granule == 2) copy_piece<uint16_t>(from, to, total, one, step, at);
+      else copy_piece<uint8_t>(from, to, total, one, step, at);
+    }
   }
 }
 

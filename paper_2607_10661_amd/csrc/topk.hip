@@ -72,11 +72,18 @@ k_topk_row(const void* __restrict__ logits, int V, long long ld, int slices, int
   load_chunks<BF16, NT, NL>(cw, rb, sl, tid);
   const uint32_t bt = sl.tail ? elem_bits<BF16>(rb, sl.vt) : 0u;
   uint32_t lm = sl.tail ? elem_img<BF16>(bt) : 0u;
+  uint32_t cm[NL];
 #pragma unroll
-  for (int u = 0; u < NL; ++u) lm = max(lm, u * NT + tid < sl.nfull ? chunk_img<BF16>(cw[u]) : 0u);
+  for (int u = 0; u < NL; ++u) {
+    cm[u] = chunk_img<BF16>(cw[u]);
+    // (the compiler would keep what an image is made of for the list: 72 registers, where up to 64 let a
+    // CU hold another workgroup)
+    asm volatile("" : "+v"(cm[u]));
+    lm = max(lm, u * NT + tid < sl.nfull ? cm[u] : 0u);
+  }
   topk_groups<KMAX, NT>(sh, lm, tid);
   lds_barrier();
-  const uint32_t tc = topk_list<KMAX, BF16, NT, NL>(sh, cw, sl, bt, tid);
+  const uint32_t tc = topk_list<KMAX, BF16, NT, NL>(sh, cw, sl, bt, tid, [&](int u) { return cm[u]; });
   lds_barrier();
   // a list that overflows (values tied at the top, or in order): every lane keeps a sorted list of
   // the best of its own elements that reach the bound, and the lists are merged (KMAX 16: its registers

@@ -222,7 +222,7 @@ struct TopkLds {
   uint16_t list[kListCap];
   __attribute__((aligned(16))) uint32_t tau[NT / PTD_WAVE];
   __attribute__((aligned(16))) uint32_t tau2[NT / PTD_WAVE];
-  uint64_t out[PTD_MAX_K];  // the best ones, in order
+  uint64_t out[PTD_MAX_K];  // the best ones, in order (a list that overflowed)
   uint32_t out_bits[PTD_MAX_K];
   int nlist, cnt;
 };
@@ -291,9 +291,9 @@ __device__ __forceinline__ void topk_append(TopkLds<NT>& sh, uint32_t bits, int 
   }
 }
 
-// Lists what reaches the bound, which is returned.
-template <int KMAX, bool BF16, int NT, int NL>
-__device__ __forceinline__ uint32_t topk_list(TopkLds<NT>& sh, const uint4 (&cw)[NL], const Slice& s, uint32_t bt, int tid) {
+// Lists what reaches the bound, which is returned.  img(u): the image of the thread's chunk u.
+template <int KMAX, bool BF16, int NT, int NL, typename Img>
+__device__ __forceinline__ uint32_t topk_list(TopkLds<NT>& sh, const uint4 (&cw)[NL], const Slice& s, uint32_t bt, int tid, Img img) {
   constexpr int NW = NT / PTD_WAVE;
   constexpr int GW = NT / KMAX;
   constexpr int WPG = GW < PTD_WAVE ? 1 : GW / PTD_WAVE;  // waves per workgroup-wide group
@@ -314,7 +314,7 @@ __device__ __forceinline__ uint32_t topk_list(TopkLds<NT>& sh, const uint4 (&cw)
   const uint32_t tc = max(cmp_bound<BF16>(max(tau, tau2)), kImgNegInf<BF16> + 1);
 #pragma unroll
   for (int u = 0; u < NL; ++u) {
-    if (u * NT + tid < s.nfull && chunk_img<BF16>(cw[u]) >= tc) {
+    if (u * NT + tid < s.nfull && img(u) >= tc) {
       const int pos = atomicAdd(&sh.nlist, 1);
       if (pos < kListCap) {
         sh.ldata[pos] = cw[u];
@@ -402,8 +402,8 @@ __device__ __forceinline__ void topk_examine(TopkLds<NT>& sh, const Slice& s, ui
   }
 }
 
-// put(rank, key, bits of the fp32 value) is called once for each rank < KMAX, by thread `rank`
-// (key 0: none).  overflow() leaves the keys and bits in sh.out where a list overflowed.
+// put(rank, key, bits of the fp32 value) is called once for each rank < KMAX (key 0: none), behind a
+// barrier of topk_pick's own.  overflow() leaves the keys and bits in sh.out where a list overflowed.
 template <int KMAX, bool BF16, int NT, typename Overflow, typename Put>
 __device__ __forceinline__ void topk_pick(TopkLds<NT>& sh, const char* rb, const Slice& s, int tid, Overflow overflow, Put put) {
   const int nl = sh.nlist;
@@ -430,27 +430,24 @@ __device__ __forceinline__ void topk_pick(TopkLds<NT>& sh, const char* rb, const
     }
     if (above) atomicAdd(&sh.rank[i], above);
     __syncthreads();
-    if (tid < n && sh.rank[tid] < static_cast<uint32_t>(KMAX)) {
-      const uint32_t rank = sh.rank[tid];
-      sh.out[rank] = sh.cand[tid];
-      sh.out_bits[rank] = sh.bits[tid];
+    if (tid < n) {
+      const uint32_t rank = sh.rank[tid], bits = sh.bits[tid];
+      const uint64_t key = sh.cand[tid];
+      if (rank < static_cast<uint32_t>(KMAX)) put(static_cast<int>(rank), key, bits);
     }
     if (n < KMAX && tid < KMAX) {  // the rest: the first entries at -inf, then none
       const int v = s.v0 + tid;
       const bool out = v < s.v1 && elem_bits<BF16>(rb, v) == 0xFF800000u;
       const uint64_t all = __ballot(out);
       const int rank = n + __popcll(all & ((1ull << tid) - 1));
-      if (out && rank < KMAX) {
-        sh.out[rank] = make_key(0xFF800000u, static_cast<uint32_t>(v));
-        sh.out_bits[rank] = 0xFF800000u;
-      }
-      if (tid >= n + __popcll(all)) sh.out[tid] = 0;
+      if (out && rank < KMAX) put(rank, make_key(0xFF800000u, static_cast<uint32_t>(v)), 0xFF800000u);
+      if (tid >= n + __popcll(all)) put(tid, 0, 0);
     }
   } else {
     overflow();
+    __syncthreads();
+    if (tid < KMAX) put(tid, sh.out[tid], sh.out_bits[tid]);
   }
-  __syncthreads();
-  if (tid < KMAX) put(tid, sh.out[tid], sh.out_bits[tid]);
 }
 
 }  // namespace ptd

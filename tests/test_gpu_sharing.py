@@ -282,6 +282,55 @@ def test_copies_of_block_scaled_pages(P):
         assert torch.equal(x.k_pages, k) and torch.equal(x.v_pages, v) and torch.equal(x.scales, s)
 
 
+@pytest.mark.parametrize("n", [1, 63, 65, 4099, 70000])
+@pytest.mark.parametrize("share", [0.0, 0.01, 1.0])
+def test_copies_of_long_lists(P, n, share):
+    # lists longer than the pairs that a workgroup looks up at once, most of them -1
+    r = random.Random(n)
+    num, Hkv, page = 600, 3, 5
+    x = torch.randint(0, 250, (num, Hkv, page, 16), dtype=torch.uint8, device="cuda")
+    src, dst, want = [-1] * n, [-1] * n, x.clone()
+    at = r.sample(range(n), min(n, 300, int(share * n) + 1))
+    for i, j in enumerate(at):
+        src[j], dst[j] = r.randrange(300), 300 + i
+        want[300 + i, :, :1 + j % page] = x[src[j], :, :1 + j % page]
+    st = i32([0])
+    P.page_copy(P.page_arrays(x), i32(src), i32(dst), i32([1 + j % page for j in range(n)]), st)
+    assert st.item() == 0 and torch.equal(x, want)
+    bad = src[:]
+    bad[n - 1], dst[n - 1] = num, 0  # (an id outside: nothing of that pair)
+    P.page_copy(P.page_arrays(x), i32(bad), i32(dst), i32([0] * n), st)
+    assert st.item() == 10 and torch.equal(x, want)
+
+
+@pytest.mark.parametrize("B", [1, 2, 3, 9, 15, 17, 65])
+def test_forks_of_long_tables(P, B):
+    # more pages than the waves of one step look at; the next tables against the old ones
+    page, per = 2, 700
+    r = random.Random(B)
+    held = [r.choice([0, 1, 63, 64, 65, 127, 129, 600, per]) if b else per for b in range(B)]
+    t = P.PageTables(B, page, per, sum(held) + 2 * B, shared=True)
+    t.plan(i32([0] * B), i32([page * h for h in held]), page * sum(held))
+    old = t.page_table.cpu().tolist()
+    frm = [r.randrange(B) for _ in range(B)]
+    ln = [r.randint(0, page * held[a]) for a in frm]
+    st = i32([0])
+    src, dst, rows = (v.tolist() for v in t.fork(i32(frm), i32(ln), st))
+    table, refs = t.page_table.cpu().tolist(), [0] * t.num_pages
+    assert st.item() == 0 and t.num_held.tolist() == [-(-x // page) for x in ln]
+    for b, a in enumerate(frm):
+        whole = ln[b] // page
+        assert table[b][:whole] == old[a][:whole]
+        if ln[b] % page:
+            last = old[a][whole]
+            assert (src[b], rows[b]) in ((last, ln[b] % page), (-1, 0)) and table[b][whole] == (last if src[b] < 0 else dst[b])
+        for p in table[b][:-(-ln[b] // page)]:
+            refs[p] += 1
+    assert t.refs.tolist() == refs
+    free = t.free_pages[:t.num_free.item()].tolist()
+    assert sorted(free) == [p for p in range(t.num_pages) if refs[p] == 0]
+
+
 def test_many_arrays_and_unaligned_ones(P):
     # more arrays than one launch takes; bases at odd addresses
     raw = torch.randint(0, 250, (200, 6 * 40 + 16), dtype=torch.uint8, device="cuda")
