@@ -446,7 +446,7 @@ int ptd_page_plan(const ptd_page_state* state, const int32_t* kv_len, const int3
 
 /* Rows of queries, keys and values (host struct, read during the call only). */
 typedef struct {
-  int32_t N;              /* rows */
+  int32_t N;              /* rows, at most 2^26 - 4 */
   int32_t Hq, Hkv;        /* heads; one of them may be 0 */
   int32_t D;              /* head dim: 64 or 128 */
   int32_t rot_dim;        /* leading dimensions that are turned: a multiple of 16, 0 .. D */
@@ -678,7 +678,7 @@ size_t ptd_token_logprobs_workspace_bytes(int32_t R, int32_t V, int32_t k);
  * entropy and the likeliest tokens with their log probabilities.
  *   logits      rows of V entries of dtype, ld elements apart, finite or -inf (masked entries:
  *               probability 0)
- *   R           entries of tokens and the outputs, >= 1
+ *   R           entries of tokens and the outputs, 1 .. 2^20 - 1 (up to 2^24 - 1 where V is at most 16384)
  *   V           1 .. 262144;  ld >= V
  *   tokens      int32 [R] or NULL: entry r's token.  -1: the entry stands for nothing, its
  *               row is not read, and its outputs are 0, 0, -1 (indices) and 0.  NULL: no

@@ -182,10 +182,15 @@ for _name, (_args, _res) in _SIGS.items():
     _f.restype = _res
 
 
+_Tensor = torch.Tensor
+
+
 def _ptr(x):
+    if type(x) is _Tensor:
+        return x.data_ptr()
     if x is None:
         return None
-    if isinstance(x, torch.Tensor):
+    if isinstance(x, _Tensor):
         return x.data_ptr()
     return int(x)
 

@@ -543,7 +543,7 @@ bool make_plan(int R, int V, int k, int elem_bytes, int path_seqs, LogpPlan* p) 
     cut(4);
     if (p->slices * std::max(p->kmax, 4) > kMergeThreads) cut(16);
   }
-  if (static_cast<long long>(R) * p->slices > 0x3FFFFFFFLL) return false;
+  if (static_cast<long long>(R) * p->slices >= (1 << 24)) return false;  // (a grid holds fewer than 2^32 threads)
   p->ws_bytes = p->slices > 1 ? static_cast<size_t>(R) * p->slices * (sizeof(Sums) + p->kmax * 16) : 0;
   return true;
 }
@@ -574,10 +574,11 @@ void dispatch(const LogpPlan& p, const LogpArgs& a, hipStream_t st) {
 
 extern "C" size_t ptd_token_logprobs_workspace_bytes(int32_t R, int32_t V, int32_t k) {
   // the dtype is not known here: size for the larger of the bf16 and fp32 plans;
-  // nor whether entries lie along paths, where a slice may be as small as with one row
+  // nor whether entries lie along paths, where slices may be those of fewer rows (the fewest: of the
+  // largest trees)
   size_t most = 0;
   for (int es = 2; es <= 4; es += 2) {
-    for (int seqs = 0; seqs < 2; ++seqs) {
+    for (int seqs : {0, std::max(1, R / (PTD_MAX_T + 1))}) {
       LogpPlan p;
       if (!make_plan(R, V, k, es, seqs, &p)) return 0;
       most = std::max(most, p.ws_bytes);

@@ -19,6 +19,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / PTD_WAVE;
 constexpr int kMaxHalf = 64;  // rot / 2 for D <= 128
+constexpr int kMaxRows = (1 << 26) - kWaves;  // a wave each: a grid holds fewer than 2^32 threads
 
 using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 
@@ -254,7 +255,7 @@ extern "C" int ptd_qk_norm_rope(const void* q, const void* k, const void* v, con
   const ptd_qk_shape& s = *shape;
   PTD_RETURN_IF((s.dtype != PTD_BF16 && s.dtype != PTD_F32) || (s.w_dtype != PTD_BF16 && s.w_dtype != PTD_F32),
                 PTD_ERR_DTYPE);
-  PTD_RETURN_IF(s.N < 0 || s.Hq < 0 || s.Hkv < 0 || s.Hq + static_cast<int64_t>(s.Hkv) < 1 || s.Hq > 65535 || s.Hkv > 65535 ||
+  PTD_RETURN_IF(s.N < 0 || s.N > kMaxRows || s.Hq < 0 || s.Hkv < 0 || s.Hq + static_cast<int64_t>(s.Hkv) < 1 || s.Hq > 65535 || s.Hkv > 65535 ||
                     (s.D != 64 && s.D != 128),
                 PTD_ERR_SHAPE);
   PTD_RETURN_IF(s.rot_dim < 0 || s.rot_dim > s.D || s.rot_dim % 16 != 0, PTD_ERR_SHAPE);

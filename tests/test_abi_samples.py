@@ -28,7 +28,7 @@ def test_qk_norm_rope_refusals():
         return _err(P.ptd_qk_norm_rope, q, k, v, wq, wk, pos, slots, qo, ko, store, shape or _qk(), inv)
 
     assert a(q=None) == a(k=None) == a(pos=None) == a(qo=None) == a(ko=None) == 1
-    for bad in (dict(N=-1), dict(Hq=-1), dict(Hkv=-1), dict(Hq=0, Hkv=0), dict(Hq=65536), dict(D=96), dict(D=256), dict(rot_dim=-16),
+    for bad in (dict(N=-1), dict(N=(1 << 26) - 3), dict(Hq=-1), dict(Hkv=-1), dict(Hq=0, Hkv=0), dict(Hq=65536), dict(D=96), dict(D=256), dict(rot_dim=-16),
                 dict(rot_dim=144), dict(rot_dim=8), dict(rot_dim=72), dict(D=64), dict(pairing=2), dict(pairing=-1), dict(norm=2),
                 dict(norm=-1), dict(norm=0), dict(eps=-1e-6), dict(eps=math.nan), dict(eps=math.inf), dict(theta=0.0), dict(theta=-1.0),
                 dict(theta=math.inf), dict(theta=math.nan), dict(ldq=1016), dict(ldk=248), dict(ldv=128), dict(ldqo=-1024), dict(ldko=8)):
@@ -61,7 +61,7 @@ def test_token_logprobs_refusals():
     assert a(x=None) == 1 and a(tok=None) == 1 and a(tok=None, lp=None, nodes=FAKE, T=4) == 1
     assert a(k=0, lp=None, ent=None, idx=None, val=None) == 1
     assert a(dt=2) == 3
-    for bad in (dict(R=0), dict(R=-1), dict(V=0), dict(V=262145, ld=262145), dict(ld=999), dict(k=-1), dict(k=17), dict(V=3, ld=3), dict(k=0),
+    for bad in (dict(R=0), dict(R=-1), dict(R=1 << 24), dict(R=1 << 20, V=262144, ld=262144, dt=P.PTD_F32), dict(V=0), dict(V=262145, ld=262145), dict(ld=999), dict(k=-1), dict(k=17), dict(V=3, ld=3), dict(k=0),
                 dict(idx=None, val=None), dict(tau=0.0), dict(tau=-1.0), dict(tau=math.nan), dict(tau=math.inf), dict(tau=1e-31), dict(tau=1e31),
                 dict(nodes=FAKE, T=0), dict(nodes=FAKE, T=3), dict(nodes=FAKE, T=1025)):
         assert a(**bad) == 2, bad
@@ -71,6 +71,8 @@ def test_token_logprobs_refusals():
     assert need > 0
     assert a(**big) == 5 and a(**big, ws=FAKE, n=16) == 5 and a(**big, ws=FAKE + 4, n=need) == 4
     assert P.ptd_token_logprobs_workspace_bytes(10, 1000, 4) == 0
+    assert P.ptd_token_logprobs_workspace_bytes(3 << 20, 32768, 4) == (3 << 20) * 2 * (32 + 8 * 16)  # fp32: two slices
+    assert P.ptd_token_logprobs_workspace_bytes((1 << 24) - 1, 16384, 4) == 0 and P.ptd_token_logprobs_workspace_bytes((1 << 20) - 1, 262144, 16) > 0
     for bad in ((0, 1000, 4), (10, 0, 0), (10, 262145, 4), (10, 1000, 17), (10, 3, 4), (10, 1000, -1)):
         assert P.ptd_token_logprobs_workspace_bytes(*bad) == 0
 
