@@ -28,10 +28,12 @@ def logprobs(row, temperature, token, k):
     """One row of logits: (log probability of the token, entropy, best k indices, their log
     probabilities, and bounds of the absolute errors of the first, the entropy and the last).
 
-    Bounds: a term e^d has a relative error of 3 * 2^-24 |d| / ln 2 * ln 2 from its argument (a
-    difference, a product, the rounded scale) and 2^-22 from the exponential; up to 65 terms
-    of a thread and 6 steps of a wave are added in fp32, 2^-24 each; the rest is fp64, and the result is
-    rounded to fp32."""
+    Bounds, with u = 2^-24: a term e^d has a relative error of 3 u |d| from its argument (a
+    difference, a product, the rounded scale), 6 u more where the argument is taken from a reference up to 8
+    doublings below the largest entry (8 ln 2 < 6), and 4 u from the exponential; up to 129
+    terms of a thread (16 chunks of 8, an edge) and 6 steps of a wave are added in fp32, u each; sums go on from
+    a larger reference up to 3 times, a factor (4 u) and a product each; the rest is fp64, and the result is rounded to
+    fp32."""
     x = row.double()
     V = x.numel()
     order = sorted(range(V), key=lambda i: (-x[i].item(), i))[:k] if V <= 2000 else \
@@ -47,7 +49,7 @@ def logprobs(row, temperature, token, k):
     dl = torch.where(live, d, 0.0)
     weighted = (e * dl).sum()
     u = 2.0 ** -24
-    term = 3 * u * dl.abs() + 4 * u + 71 * u
+    term = 3 * u * (dl.abs() + 6) + 4 * u + (129 + 6 + 3 * 5) * u
     rest = torch.where(x != m, e * term, 0.0).sum()  # absolute error of the sum
     e_lse = rest / total
     e_w = (e * dl.abs() * (term + 2 * u)).sum()

@@ -158,6 +158,20 @@ def test_ties_and_signed_zeros(P):
             check(P.token_logprobs(x, i32([1, 7, 0]), 16), x, [1, 7, 0], 16)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,N", [(1000, 1), (40000, 1), (40000, 300)])
+def test_rows_in_order(P, dtype, V, N):
+    # ascending and descending rows: the reference moves with every group of chunks, candidates fill their lists
+    up = torch.linspace(-90, 90, V, device="cuda").to(dtype)
+    steep = torch.linspace(-3000, 3000, V, device="cuda").to(dtype)
+    x = torch.stack([up, up.flip(0), steep, steep.flip(0)] * N)
+    tok = [V - 1, 0, V - 2, 3] * N
+    got = P.token_logprobs(x, i32(tok), 16)
+    check([t[:4] for t in got], x[:4], tok[:4], 16)
+    for t in got:
+        assert torch.equal(t.view(N, -1), t.view(N, -1)[:1].expand(N, -1))
+
+
 @pytest.mark.parametrize("tau", [1e-3, 0.05, 10.0, 1e6])
 def test_temperatures(P, tau):
     x = logits(3, 5000, torch.float32, 8, peak=10)
