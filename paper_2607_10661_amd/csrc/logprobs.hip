@@ -18,9 +18,10 @@
 //                 their best entries (rows of several slices).
 // An element costs its unpacking, a multiply-add, the exponential, a sum and a multiply-add, and 1.4
 // more for its chunk's largest: about 40 us of the vector units for 1040 rows x 128256, beside 51 of
-// HBM.  That takes 64 us in all with the 8 best entries and 52 without (a version that needed the
-// row's largest entry first took 77 and 58, 512 threads x 8 chunks 70); 97 rows x 32003 fp32 12
+// HBM.  That takes 64 us in all with the 8 best entries and 47 without (a version that needed the
+// row's largest entry first took 77 and 58, 512 threads x 8 chunks 70); 97 rows x 32003 fp32 11
 // us, a single row 11, both the latency of two launches and of six barriers.
+//   k_logp_wave   one wave per entry, for many rows that fit its registers (8 chunks of 16 bytes a lane, or 2).
 // Terms and the sums of a wave are fp32, waves and slices are joined in fp64.
 #include <math.h>
 
@@ -238,7 +239,7 @@ __device__ __forceinline__ WaveSums without_top(const char* rb, const Slice& sl,
     const float e = __builtin_amdgcn_exp2f(arg);
     n += x == m ? 1 : 0;
     r += x == m ? 0.f : e;
-    w += x == m ? 0.f : e * arg;
+    w += x == m ? 0.f : e * fmaxf(arg, -256.f);
   };
   if (lane / 4 < NL && chunk < sl.nfull) {
     const uint32_t x = *reinterpret_cast<const uint32_t*>(rb + (static_cast<size_t>(sl.vb) + static_cast<size_t>(chunk) * E) * (BF16 ? 2 : 4) + lane % 4 * 4);
@@ -268,11 +269,14 @@ __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, i
   // the sums, four chunks at a time
   uint32_t lm = sl.tail ? elem_img<BF16>(bt) : 0u, limit = 0;
   float c = 0.f, sum = 0.f, weighted = 0.f;
+  // (a masked entry's term is 0, times its exponent no number: the exponent of a term that is 0 may be any
+  // other.  1040 x 128256, 99 % of it masked, 62 us, and 115 where such waves were summed again with
+  // care; nothing masked 64 and 62)
   auto add = [&](float x) __attribute__((always_inline)) {
     const float arg = fmaf(x, a.scale, -c);
     const float e = __builtin_amdgcn_exp2f(arg);
     sum += e;
-    weighted = fmaf(e, arg, weighted);
+    weighted = fmaf(e, fmaxf(arg, -256.f), weighted);
   };
   static_assert(NL % 4 == 0, "groups of four chunks");
 #pragma unroll
@@ -285,7 +289,7 @@ __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, i
       const uint32_t most = group_max_min<64>(img);
       const float ref = image_value<BF16>(most);
       const float next = ref > -INFINITY ? ref * a.scale : 0.f;  // (masked entries alone: any number)
-      const float f = __builtin_amdgcn_exp2f(c - next);
+      const float f = __builtin_amdgcn_exp2f(fminf(c - next, 0.f));  // (above 0 only from masked entries, whose sums are 0)
       weighted = u0 == 0 ? 0.f : f * fmaf(c - next, sum, weighted);
       sum = u0 == 0 ? 0.f : f * sum;
       c = next;
@@ -392,6 +396,100 @@ __global__ void __launch_bounds__(kThreads, 4) k_logp_row(LogpArgs a) {
     return;
   }
   row_slice<KMAX, BF16, NL, ONE>(a, sh, r, row, token, slice, tid);
+}
+
+// One wave per entry, the whole row in its registers: the largest entry first, then the others' terms
+// relative to it, then the best entries one after the other -- the next best of the lane that had the
+// one before is found by the whole wave, an element each.
+template <bool TOPK, bool BF16, int NL>
+__global__ void __launch_bounds__(kThreads) k_logp_wave(LogpArgs a) {
+  constexpr int E = BF16 ? 8 : 4;
+  const int lane = threadIdx.x & 63;
+  const int r = blockIdx.x * (kThreads / PTD_WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (r >= a.R) return;  // whole wave
+  int token;
+  const int row = entry_row(a, r, &token, lane == 0);
+  if (row < 0) {  // uniform
+    put_nothing(a, r, lane);
+    return;
+  }
+  const char* rb = static_cast<const char*>(a.logits) + static_cast<size_t>(row) * a.ld * (BF16 ? 2 : 4);
+  const Slice sl = slice_at<BF16>(rb, 0, a.V, lane);
+  uint4 cw[NL];
+  load_chunks<BF16, PTD_WAVE, NL>(cw, rb, sl, lane);
+  const uint32_t bt = sl.tail ? elem_bits<BF16>(rb, sl.vt) : 0u;
+  const float xt = token >= 0 ? __uint_as_float(elem_bits<BF16>(rb, token)) : 0.f;
+  // every element of the lane, in order of its index but for the edge's
+  auto each = [&](auto&& f) __attribute__((always_inline)) {
+    if (sl.tail) f(bt, sl.vt);
+#pragma unroll
+    for (int u = 0; u < NL; ++u) {
+      const int c = u * PTD_WAVE + lane;
+      if (c < sl.nfull) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) f(chunk_bits<BF16>(cw[u], e), sl.vb + c * E + e);
+      }
+    }
+  };
+  uint32_t best = 0, at = 0;
+  bool nan = false;
+  each([&](uint32_t bits, int v) __attribute__((always_inline)) {
+    const float x = __uint_as_float(bits);
+    nan |= x != x;
+    const uint32_t o = ord_of(x);
+    const bool more = o > best || (o == best && static_cast<uint32_t>(v) < at);
+    best = more ? o : best;
+    at = more ? static_cast<uint32_t>(v) : at;
+  });
+  const uint32_t img = group_max_min<64>(best);
+  const float m = img ? image_value<false>(img) : NAN;
+  const float c = m * a.scale, none = -1.2e6f / a.scale;  // none: its exponent is -1.1e6 or less
+  float rest = 0.f, w = 0.f;
+  int n = 0;
+  each([&](uint32_t bits, int) __attribute__((always_inline)) {
+    const float x = __uint_as_float(bits);
+    n += x == m ? 1 : 0;
+    const float arg = fmaf(x == m ? none : fmaxf(x, none), a.scale, -c);
+    const float e = __builtin_amdgcn_exp2f(arg);
+    rest += e;
+    w = fmaf(e, arg, w);
+  });
+  if (!(fabsf(c) < 0x1p30f)) rest = w = 0.f;  // (as in careful_sums)
+  if (__any(nan) || m == INFINITY) rest = NAN;
+  rest = wave_sum_dpp(rest), w = wave_sum_dpp(w);
+  const float ones = wave_sum_dpp(static_cast<float>(n));
+  // (c is rounded: the terms are 2^d of what they stand for)
+  const double d = fabsf(c) < 0x1p30f ? static_cast<double>(c) - static_cast<double>(m) * a.scale : 0.0;
+  const double f = static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(d)));
+  const Sums s = {m, ones, f * rest, f * (w + d * rest) * a.unscale, xt};
+  const Totals tot = totals_of(s);
+  if (lane == 0) put_entry(a, r, tot, s.weighted, xt);
+  if constexpr (TOPK) {
+    for (int k = 0; k < a.k; ++k) {  // uniform
+      const uint32_t top = group_max_min<64>(best);
+      const uint32_t first = group_max_min<1>(best == top ? at : ~0u);
+      if (lane == 0) put_best(a, r, k, tot, top ? (static_cast<uint64_t>(top) << 32) | static_cast<uint32_t>(~first) : 0, __float_as_uint(image_value<false>(top)));
+      if (k + 1 == a.k) break;
+      const uint64_t who = __ballot(best == top && at == first);
+      if (!who) break;  // (never: the pair is some lane's)
+      const int owner = __builtin_ctzll(who);
+      // elements of the owner that come behind (top, first)
+      uint32_t o = 0, v = ~0u;
+      const int ch = lane / E * PTD_WAVE + owner;
+      if (lane / E < NL && ch < sl.nfull) {
+        v = static_cast<uint32_t>(sl.vb + ch * E + lane % E);
+        o = ord_of(__uint_as_float(elem_bits<BF16>(rb, v)));
+        if (!(o < top || (o == top && v > first))) o = 0;
+      }
+      if (lane == owner && sl.tail) {  // its edge, besides
+        const uint32_t eo = ord_of(__uint_as_float(bt)), ev = static_cast<uint32_t>(sl.vt);
+        if ((eo < top || (eo == top && ev > first)) && (eo > o || (eo == o && ev < v))) o = eo, v = ev;
+      }
+      const uint32_t next = group_max_min<64>(o);
+      const uint32_t place = group_max_min<1>(o == next ? v : ~0u);
+      if (lane == owner) best = next, at = place;
+    }
+  }
 }
 
 // Entries along paths: few of a sequence's T + 1 are there, and the host does not know which.
@@ -548,8 +646,27 @@ bool make_plan(int R, int V, int k, int elem_bytes, int path_seqs, LogpPlan* p) 
   return true;
 }
 
+// Whether rows go to k_logp_wave: those that fit, where there are many.  (bf16, a workgroup / a wave per
+// row: 1000 entries, k = 5, 64 rows 5.4 / 6.5 us, 1040 rows 11.3 / 7.1, 16384 rows 90 / 28; k = 16,
+// 1040 rows 13.3 / 13.5; 4000 entries, k = 5, 1040 rows 12.0 / 12.4, 16384 rows 98 / 58; k = 0, 1040
+// rows 6.8 / 9.8, 16384 rows 52 / 45; 100000 rows of 50 entries 538 / 122.)
+constexpr int kFewChunks = 2, kWaveChunks = 8;
+inline bool by_waves(const LogpArgs& a, int elems) {
+  if (a.V > PTD_WAVE * kWaveChunks * elems) return false;
+  const int rows = a.V <= PTD_WAVE * kFewChunks * elems ? 512 : a.k == 0 ? 8192 : 2048;
+  return a.R >= (a.k > 8 ? 2 * rows : rows);
+}
+
+template <bool TOPK, bool BF16>
+void launch_waves(const LogpArgs& a, hipStream_t st) {
+  const dim3 grid(ptd_cdiv(a.R, kThreads / PTD_WAVE));
+  if (a.V <= PTD_WAVE * kFewChunks * (BF16 ? 8 : 4)) hipLaunchKernelGGL((k_logp_wave<TOPK, BF16, kFewChunks>), grid, dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((k_logp_wave<TOPK, BF16, kWaveChunks>), grid, dim3(kThreads), 0, st, a);
+}
+
 template <int KMAX, bool BF16>
 void launch(const LogpPlan& p, const LogpArgs& a, hipStream_t st) {
+  if (by_waves(a, BF16 ? 8 : 4)) return launch_waves<(KMAX > 0), BF16>(a, st);
   const bool one = p.slices == 1;
   const unsigned n = (a.nodes ? static_cast<unsigned>(ptd_cdiv(a.R, a.part_rows)) * a.ways : static_cast<unsigned>(a.R)) * a.slices;
 #define PTD_LOGP(kernel_, nl_)                                                                                \

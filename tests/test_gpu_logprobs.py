@@ -172,6 +172,57 @@ def test_rows_in_order(P, dtype, V, N):
         assert torch.equal(t.view(N, -1), t.view(N, -1)[:1].expand(N, -1))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,N,k,odd", [(1, 600, 1, 0), (3, 600, 2, 1), (17, 1100, 16, 3), (50, 5000, 5, 0), (129, 700, 0, 1), (500, 520, 4, 5),
+                                       (511, 1030, 16, 1), (1024, 513, 8, 0), (1025, 2050, 3, 1), (2041, 4100, 9, 7), (2048, 2048, 5, 0),
+                                       (4096, 2048, 5, 0), (4091, 8200, 0, 0)])
+def test_many_short_rows(P, dtype, V, N, k, odd):
+    x = logits(N, V, dtype, V + N, odd=odd, peak=20.0, masked=0.2)
+    x[3] = -math.inf                               # nothing left
+    x[4] = 2.0                                     # ties
+    x[5, V // 2] = float("nan")
+    x[6, 0] = float("inf")
+    x[7] = torch.finfo(dtype).min                  # the type's lowest value throughout
+    x[8, ::2] = -0.0
+    x[8, 1::2] = 0.0
+    x[9] = torch.linspace(-50, 50, V).to(dtype)
+    x[10] = x[9].flip(0)
+    tok = torch.randint(0, V, (N,), generator=torch.Generator().manual_seed(V)).tolist()
+    tok[11] = -1
+    st = i32([0])
+    got = P.token_logprobs(x, i32(tok), k, dev_status=st)
+    assert st.item() == 0
+    some = [0, 1, 2, 3, 4, 7, 8, 9, 10, 11] + list(range(N - 30, N))
+    check([None if t is None else t[some] for t in got], x[some], [tok[r] for r in some], k)
+    assert got[0][5:7].isnan().all() and got[1][5:7].isnan().all()
+    # the workgroups' kernel, a few rows at a time
+    near = P.token_logprobs(x[100:200], i32(tok[100:200]), k)
+    if k:
+        assert torch.equal(near[2], got[2][100:200])
+    live = near[0] > -math.inf
+    assert torch.equal(live, got[0][100:200] > -math.inf)
+    assert ((near[0] - got[0][100:200])[live].abs() <= 2e-5 * (1 + near[0][live].abs())).all()
+
+
+def test_many_short_rows_along_paths(P):
+    B, T, V = 40, 64, 300
+    r = random.Random(5)
+    x = logits(B * (T + 1), V, torch.bfloat16, 9)
+    paths = [sorted(r.sample(range(T), r.choice([0, 1, 3, 9]))) for _ in range(B)]
+    tok, rows = [], []
+    for b, p in enumerate(paths):
+        tok += [r.randrange(V) if j <= len(p) else -1 for j in range(T + 1)]
+        rows += [b * (T + 1) + (p[j - 1] + 1 if 0 < j <= len(p) else 0) for j in range(T + 1)]
+    nodes = i32([p + [-1] * (T - len(p)) for p in paths])
+    st = i32([0])
+    check(P.token_logprobs(x, i32(tok), 5, nodes=nodes, dev_status=st), x, tok, 5, rows=rows)
+    assert st.item() == 0
+    tok[0], tok[T + 2] = V, 5
+    nodes[1, 0] = T
+    got = P.token_logprobs(x, i32(tok), 5, nodes=nodes, dev_status=st)
+    assert st.item() in (13, 14) and got[0][0] == 0 and got[0][T + 2] == 0 and (got[2][0] == -1).all()
+
+
 @pytest.mark.parametrize("tau", [1e-3, 0.05, 10.0, 1e6])
 def test_temperatures(P, tau):
     x = logits(3, 5000, torch.float32, 8, peak=10)
