@@ -16,12 +16,13 @@
 //   k_logp_path   the same for entries along accepted paths, few of which are there.
 //   k_logp_merge  one workgroup per entry joins the slices' sums, in their order, and ranks
 //                 their best entries (rows of several slices).
-// An element costs its unpacking, a multiply-add, the exponential, a sum and a multiply-add, and 1.4
-// more for its chunk's largest: about 40 us of the vector units for 1040 rows x 128256, beside 51 of
+//   k_logp_wave   one wave per entry, for many rows that fit its registers (8 chunks of 16 bytes a
+//                 lane, or 2).
+// An element costs its unpacking, a multiply-add, the exponential, a sum, a maximum and a multiply-add, and 1.4
+// more for its chunk's largest: about 45 us of the vector units for 1040 rows x 128256, beside 51 of
 // HBM.  That takes 64 us in all with the 8 best entries and 47 without (a version that needed the
 // row's largest entry first took 77 and 58, 512 threads x 8 chunks 70); 97 rows x 32003 fp32 11
 // us, a single row 11, both the latency of two launches and of six barriers.
-//   k_logp_wave   one wave per entry, for many rows that fit its registers (8 chunks of 16 bytes a lane, or 2).
 // Terms and the sums of a wave are fp32, waves and slices are joined in fp64.
 #include <math.h>
 

@@ -218,8 +218,10 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
       }
     };
     long long freed = 0;
-    // a few surplus pages per thread stay in its registers
-    constexpr int kEach = 8;
+    // a few surplus pages per thread stay in its registers, more come in turns.  (256 threads, a release and a take
+    // of 4096 pages 44 us, of 16384 154; with one page per thread and turn 80 and 300.  1024 threads spill
+    // with more than two: 16384 pages 82 us, with four 86, eight 107.)
+    constexpr int kEach = NT > kPlanSmall ? 2 : 8;
     int ids[kEach], seqs[kEach], give[kEach], m = 0;  // give: whether the thread puts the page on the list
     const bool kept = ONE && all.back <= kEach * NT;
     if (kept && all.back > 0) {  // uniform
@@ -272,6 +274,77 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
         }
       }
       ptd::drained_barrier();
+    } else if (ONE && all.back > 0) {
+      // the same in turns of as many, whose ids are loaded anew for each step
+      s_back[tid] = static_cast<int>(min(at.back, static_cast<long long>(0x7FFFFFFF)));
+      s_need[tid] = w.need;
+      __syncthreads();
+      // steps: 0 look at the counts; where a page has several holders, 1 count down, 2 claim, 3 count the claims;
+      // 4 put on the list
+      bool several = false;
+      long long done = 0;
+      for (int step = 0; step < 5; step = step == 0 && !several ? 4 : step + 1) {  // uniform
+        m = 0;
+        for (long long base = 0; base < all.back; base += kEach * NT) {
+#pragma unroll
+          for (int u = 0; u < kEach; ++u) {
+            const long long j = base + tid * kEach + u;
+            seqs[u] = j < all.back ? upper(s_back, B, j) : 0;
+            ids[u] = j < all.back ? table_of(p, seqs[u])[s_need[seqs[u]] + static_cast<int>(j - s_back[seqs[u]])] : -1;
+            if (step == 0 && j < all.back && static_cast<uint32_t>(ids[u]) >= static_cast<uint32_t>(p.s.num_pages))
+              ptd::report(p.dev_status, PTD_ERR_PAGE);
+            if (static_cast<uint32_t>(ids[u]) >= static_cast<uint32_t>(p.s.num_pages)) ids[u] = -1;
+          }
+          if (step == 1) {
+#pragma unroll
+            for (int u = 0; u < kEach; ++u)
+              if (ids[u] >= 0) ptd::add_count(p.refs + ids[u], -1);
+            continue;
+          }
+          int v[kEach];
+#pragma unroll
+          for (int u = 0; u < kEach; ++u) v[u] = ids[u] >= 0 ? ptd::load_count(p.refs + ids[u]) : 1;
+          if (step == 0) {
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+              if (v[u] <= 0) ptd::report(p.dev_status, PTD_ERR_PAGE);
+              several |= v[u] > 1;
+            }
+          } else if (step == 2) {
+#pragma unroll
+            for (int u = 0; u < kEach; ++u)
+              if (ids[u] >= 0 && (v[u] == 0 || is_giver(v[u]))) ptd::min_count(p.refs + ids[u], kGiver + seqs[u]);
+            continue;
+          }
+#pragma unroll
+          for (int u = 0; u < kEach; ++u) {
+            give[u] = ids[u] >= 0 && v[u] == (step >= 3 && several ? kGiver + seqs[u] : 1);
+            m += give[u];
+          }
+          if (step == 4) {
+            const int count1 = count + static_cast<int>(min(freed, static_cast<long long>(p.s.num_pages - count)));
+            Sums t;
+            long long j = done + block_scan<NT>({m, 0, 0}, s_scan, &t).back;
+            m = 0;
+#pragma unroll
+            for (int u = 0; u < kEach; ++u) {
+              if (give[u]) {
+                if (count1 - 1 - j >= count) p.s.free_pages[count1 - 1 - j] = ids[u];
+                p.refs[ids[u]] = 0;
+                ++j;
+              }
+            }
+            done += t.back;
+          }
+        }
+        ptd::drained_barrier();
+        if (step == 0) several = __syncthreads_or(several);
+        if (step == (several ? 3 : 0)) {
+          Sums t;
+          block_scan<NT>({m, 0, 0}, s_scan, &t);
+          freed = t.back;
+        }
+      }
     } else if (all.back > 0) {
       each([&](int, int id, bool ok, bool has) __attribute__((always_inline)) {
         if (ok ? ptd::add_count(p.refs + id, -1) <= 0 : has) ptd::report(p.dev_status, PTD_ERR_PAGE);
@@ -292,7 +365,7 @@ __global__ void __launch_bounds__(NT) k_page_plan(PlanParams p) {
     }
     total = min(freed, static_cast<long long>(p.s.num_pages - count));
     long long done = 0;
-    if (freed > 0 && !kept) {  // uniform
+    if (!ONE && freed > 0) {  // uniform
       const int count1 = count + static_cast<int>(total);
       each([&](int b, int id, bool ok, bool) __attribute__((always_inline)) {
         const bool mine = ok && ptd::load_count(p.refs + id) == kGiver + b;

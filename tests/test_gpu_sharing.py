@@ -154,6 +154,41 @@ def test_pages_given_up_by_several_at_once(P):
         assert t.num_free.item() == 240 * more
 
 
+@pytest.mark.parametrize("B,per,rows", [(6, 1500, 0), (6, 1500, 5000), (300, 40, 0)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_many_pages_given_up(P, B, per, rows, shared):
+    # more surplus pages than threads hold at once, of one holder or of several; with and without new rows
+    r = random.Random(B)
+    t, ref = P.PageTables(B, 1, per, B * per, shared=True), R.SharedPages(B, 1, per, B * per)
+    kv = [r.randint(per // 2, per) for _ in range(B)]
+    plan(t, ref, [0] * B, kv)
+    if shared:
+        frm = [b if b % 3 else 0 for b in range(B)]
+        kv = [kv[a] - (0 if a == b else r.randint(0, 9)) for b, a in enumerate(frm)]
+        assert fork(t, ref, frm, kv)[3]
+    keep = [r.choice([0, 0, 1, r.randint(0, n)]) for n in kv]
+    new = [0] * B
+    new[1] = min(rows, per - keep[1])
+    plan(t, ref, keep, new, N=rows)
+    plan(t, ref, [0] * B, [0] * B, N=0)
+    assert t.num_free.item() == B * per and (t.refs == 0).all()
+
+
+def test_pages_that_are_none(P):
+    # ids outside the pool and counts that are none among many surplus pages are reported, the others go back
+    B, per = 4, 1200
+    t = P.PageTables(B, 1, per, B * per, shared=True)
+    t.plan(i32([0] * B), i32([per] * B), 0)
+    t.page_table[1, 7], t.page_table[2, 8] = B * per, -5
+    lost = [t.page_table[3, 9].item()]
+    t.refs[lost[0]] = 0
+    st = i32([0])
+    before = set(range(B * per))
+    t.plan(i32([0] * B), i32([0] * B), 0, dev_status=st)
+    free = t.free_pages[:t.num_free.item()].tolist()
+    assert st.item() == 10 and len(set(free)) == len(free) == B * per - 3 and set(free) < before and lost[0] not in free
+
+
 def test_fork_refusals_change_nothing(P):
     def state():
         t = P.PageTables(4, 16, 4, 9, shared=True)
