@@ -695,7 +695,7 @@ size_t ptd_token_logprobs_workspace_bytes(int32_t R, int32_t V, int32_t k);
  *   workspace   >= ptd_token_logprobs_workspace_bytes(R, V, k), 8-byte aligned
  * At least one output.  A row whose entries are all -inf has no distribution: log
  * probabilities -inf, entropy 0, indices in order.  With a NaN or +inf in a row its own values are
- * NaN or unspecified.  Terms are fp32, sums fp64; what is left beside the row's largest
+ * NaN or unspecified.  Terms and the sums of 64 lanes are fp32, joined in fp64; what is left beside the row's largest
  * entries is summed apart, so log probabilities and entropies next to 0 keep their relative
  * precision.
  * dev_status: PTD_ERR_VALUE (a token outside [-1, V)), PTD_ERR_ROWS (a node outside [0, T) on a

@@ -123,7 +123,9 @@ __device__ __forceinline__ void load_weights(const void* w, int bf16, int d0, fl
   }
 }
 
-template <typename T, int D, bool INTERLEAVED>
+// MIXED: heads of queries, keys and values are taken one after the other, and a group of them may hold several
+// kinds; else a group is of one kind, which the whole wave then takes one way.
+template <typename T, int D, bool INTERLEAVED, bool MIXED>
 __global__ void __launch_bounds__(kThreads) k_qk_norm_rope(QkArgs a, int norm) {
   constexpr int G = D / 16;           // lanes of a head
   constexpr int H = PTD_WAVE / G;     // heads of a wave
@@ -150,17 +152,31 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_rope(QkArgs a, int norm) {
   const int d0 = 8 * (INTERLEAVED || !turn ? 2 * c : c);
   const int d1 = INTERLEAVED || !turn ? d0 + 8 : d0 + 8 * turned;
 
-  const int gq = (a.heads[0] + H - 1) / H, gk = (a.heads[1] + H - 1) / H;
-  const int groups = gq + gk + (slot >= 0 ? gk : 0);
+  const int hq = a.heads[0], hk = a.heads[1], total = hq + (slot >= 0 ? 2 : 1) * hk;
+  const int gq = (hq + H - 1) / H, gk = (hk + H - 1) / H;
+  const int groups = MIXED ? (total + H - 1) / H : gq + (slot >= 0 ? 2 : 1) * gk;
   const int page = slot >= 0 ? slot / a.page_size : 0;
   const int at = slot >= 0 ? slot - page * a.page_size : 0;
-  auto kind_of = [&](int u) { return u < gq ? 0 : u < gq + gk ? 1 : 2; };
-  auto head_of = [&](int u, int kind) { return (u - (kind == 0 ? 0 : kind == 1 ? gq : gq + gk)) * H + hl; };
+  struct Head {
+    int kind, h;
+    bool there;
+  };
+  auto head_of = [&](int u) __attribute__((always_inline)) {
+    if constexpr (MIXED) {
+      const int n = u * H + hl, kind = n < hq ? 0 : n < hq + hk ? 1 : 2;
+      return Head{kind, n - (kind == 0 ? 0 : kind == 1 ? hq : hq + hk), n < total};
+    } else {
+      const int kind = u < gq ? 0 : u < gq + gk ? 1 : 2;
+      const int h = (u - (kind == 0 ? 0 : kind == 1 ? gq : gq + gk)) * H + hl;
+      return Head{kind, h, u < groups && h < (kind == 0 ? hq : hk)};
+    }
+  };
   Chunk<T> x0, x1, n0, n1;
   auto load = [&](int u) __attribute__((always_inline)) {
-    const int kind = kind_of(u), h = head_of(u, kind);
-    if (u < groups && h < a.heads[kind > 0]) {
-      const T* src = static_cast<const T*>(a.in[kind]) + row * a.ld_in[kind] + static_cast<int64_t>(h) * D;
+    const auto [kind, h, there] = head_of(u);
+    if (there) {
+      const T* src = static_cast<const T*>(kind == 0 ? a.in[0] : kind == 1 ? a.in[1] : a.in[2]) +
+                     row * (kind == 0 ? a.ld_in[0] : kind == 1 ? a.ld_in[1] : a.ld_in[2]) + static_cast<int64_t>(h) * D;
       n0.load(src + d0);
       n1.load(src + d1);
     }
@@ -180,15 +196,15 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_rope(QkArgs a, int norm) {
   int have = -1;  // kind whose weights are in w0, w1
   float w0[8], w1[8];
   for (int u = sub; u < groups; u += a.waves_per_row) {
-    const int kind = kind_of(u), h = head_of(u, kind);
+    const auto [kind, h, there] = head_of(u);
     x0 = n0, x1 = n1;
     load(u + a.waves_per_row);
     if (norm && kind < 2 && kind != have) {
-      load_weights(a.w[kind], a.w_bf16, d0, w0);
-      load_weights(a.w[kind], a.w_bf16, d1, w1);
+      load_weights(kind == 0 ? a.w[0] : a.w[1], a.w_bf16, d0, w0);
+      load_weights(kind == 0 ? a.w[0] : a.w[1], a.w_bf16, d1, w1);
       have = kind;
     }
-    if (h >= a.heads[kind > 0]) continue;
+    if (!there) continue;
     if (kind < 2) {
       float x[8], y[8];
       x0.get(x);
@@ -223,25 +239,30 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_rope(QkArgs a, int norm) {
       }
       x0.set(x);
       x1.set(y);
-      if (a.out[kind]) {
-        T* dst = static_cast<T*>(a.out[kind]) + row * a.ld_out[kind] + static_cast<int64_t>(h) * D;
+      T* out = static_cast<T*>(kind == 0 ? a.out[0] : a.out[1]);
+      if (out) {
+        T* dst = out + row * (kind == 0 ? a.ld_out[0] : a.ld_out[1]) + static_cast<int64_t>(h) * D;
         x0.store(dst + d0);
         x1.store(dst + d1);
       }
     }
     if (kind > 0 && slot >= 0) {
-      T* dst = static_cast<T*>(a.pages[kind - 1]) +
-               ((static_cast<int64_t>(page) * a.heads[1] + h) * a.page_size + at) * D;
+      T* dst = static_cast<T*>(kind == 1 ? a.pages[0] : a.pages[1]) +
+               ((static_cast<int64_t>(page) * hk + h) * a.page_size + at) * D;
       x0.store(dst + d0);
       x1.store(dst + d1);
     }
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, bool MIXED>
 void launch(const QkArgs& a, int norm, bool inter, unsigned grid, hipStream_t st) {
-  if (inter) hipLaunchKernelGGL((k_qk_norm_rope<T, D, true>), dim3(grid), dim3(kThreads), 0, st, a, norm);
-  else hipLaunchKernelGGL((k_qk_norm_rope<T, D, false>), dim3(grid), dim3(kThreads), 0, st, a, norm);
+  if (inter) hipLaunchKernelGGL((k_qk_norm_rope<T, D, true, MIXED>), dim3(grid), dim3(kThreads), 0, st, a, norm);
+  else hipLaunchKernelGGL((k_qk_norm_rope<T, D, false, MIXED>), dim3(grid), dim3(kThreads), 0, st, a, norm);
+}
+template <typename T, int D>
+void launch(const QkArgs& a, int norm, bool inter, bool mixed, unsigned grid, hipStream_t st) {
+  mixed ? launch<T, D, true>(a, norm, inter, grid, st) : launch<T, D, false>(a, norm, inter, grid, st);
 }
 
 }  // namespace
@@ -310,13 +331,18 @@ extern "C" int ptd_qk_norm_rope(const void* q, const void* k, const void* v, con
   // A row's head groups over several waves while there are fewer than half of what the chip
   // holds.  (32/8 heads x 128, into pages: 1024 rows 10.2 us with a wave per row, 7.9 with four; 2048
   // rows 12.8 with four, 10.9 with two; 28000 rows 121 with one and 146 with six.)
-  const int per = s.D == 128 ? 8 : 16, groups = ptd_cdiv(s.Hq, per) + ptd_cdiv(s.Hkv, per) * (store ? 2 : 1);
+  const int per = s.D == 128 ? 8 : 16, kinds = store ? 2 : 1;
+  // Groups of several kinds where that makes fewer of them.  (70184 rows of 7/1 heads x 64 into pages, one
+  // group in place of three: 73 us and 97; 28700 rows of 32/8 x 128, as many groups: 122 and 119)
+  const int apart = ptd_cdiv(s.Hq, per) + kinds * ptd_cdiv(s.Hkv, per), together = ptd_cdiv(s.Hq + kinds * s.Hkv, per);
+  const bool mixed = together < apart;
+  const int groups = mixed ? together : apart;
   a.waves_per_row = std::max(1, std::min(groups, 4096 / s.N));
   const int64_t grid = (static_cast<int64_t>(s.N) * a.waves_per_row + kWaves - 1) / kWaves;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool il = s.pairing == PTD_ROPE_INTERLEAVED;
   const unsigned g = static_cast<unsigned>(grid);
-  if (s.dtype == PTD_BF16) s.D == 128 ? launch<uint16_t, 128>(a, s.norm, il, g, st) : launch<uint16_t, 64>(a, s.norm, il, g, st);
-  else s.D == 128 ? launch<float, 128>(a, s.norm, il, g, st) : launch<float, 64>(a, s.norm, il, g, st);
+  if (s.dtype == PTD_BF16) s.D == 128 ? launch<uint16_t, 128>(a, s.norm, il, mixed, g, st) : launch<uint16_t, 64>(a, s.norm, il, mixed, g, st);
+  else s.D == 128 ? launch<float, 128>(a, s.norm, il, mixed, g, st) : launch<float, 64>(a, s.norm, il, mixed, g, st);
   return ptd_launch_status();
 }
