@@ -172,8 +172,15 @@ struct NoLds {};
 // A wave's sums: of 2^(l * scale - c) and of that times the exponent, its largest entry, and
 // (ones > 0) how many entries equal to the slice's largest were taken out of them.
 struct WaveSums {
-  float c, sum, weighted, top, ones;
+  double c;
+  float sum, weighted, top, ones;
 };
+
+// The exponent of an entry's term relative to the row's or wave's largest entry.  The difference comes
+// before the scale, so entries of any size keep their distance, and what lies so far below that it has no
+// weight (-inf, a mask of any number, an overflow, the difference of two infinities) has a term of 0
+// and an exponent that is a number.
+__device__ __forceinline__ float exponent_below(float x, float top, float scale) { return fmaxf((x - top) * scale, -256.f); }
 
 // What a workgroup keeps of the entry that it works on.
 template <int KMAX>
@@ -183,23 +190,20 @@ struct RowLds {
   Totals totals;
 };
 
-// The sums with care, relative to the wave's largest entry: entries that equal m are counted and
-// left out, and what lies so far below that it has no weight (-inf; the type's lowest number
-// overflows to it) is raised to where it has none and the weighted sum stays a number.  The
-// elements are read again, so that the common way has their registers.
+// The sums with care, relative to the wave's largest entry itself, whatever its size: entries that
+// equal m are counted and left out.  The elements are read again, so that the common way has their
+// registers.
 template <bool BF16>
 __device__ __forceinline__ WaveSums careful_sums(const char* rb, const Slice& sl, uint32_t bt, int tid, float top, float m, float scale) {
   constexpr int E = BF16 ? 8 : 4;
   float r = 0.f, w = 0.f;
   int n = 0;
   bool nan = false;
-  const float c = top * scale;
-  const float none = -1.2e6f / scale;  // its exponent is -1.1e6 or less
   auto add = [&](float x) __attribute__((always_inline)) {
     nan |= x != x;
     n += x == m ? 1 : 0;
-    const float arg = fmaf(x == m ? none : fmaxf(x, none), scale, -c);
-    const float e = __builtin_amdgcn_exp2f(arg);
+    const float arg = exponent_below(x, top, scale);
+    const float e = x == m ? 0.f : __builtin_amdgcn_exp2f(arg);
     r += e;
     w = fmaf(e, arg, w);
   };
@@ -218,11 +222,8 @@ __device__ __forceinline__ WaveSums careful_sums(const char* rb, const Slice& sl
     }
   }
   if (sl.tail) add(__uint_as_float(bt));
-  // (where c is larger no entry but the largest has a weight: its distance is at least 2^-23 of c; and
-  // where the wave's is not the slice's largest, neither has that one)
-  if (!(fabsf(c) < 0x1p30f)) r = w = 0.f;
   if (__any(nan) || !(fabsf(top) < INFINITY)) r = NAN;
-  return {c, wave_sum_dpp(r), wave_sum_dpp(w), top, wave_sum_dpp(static_cast<float>(n))};
+  return {static_cast<double>(top) * scale, wave_sum_dpp(r), wave_sum_dpp(w), top, wave_sum_dpp(static_cast<float>(n))};
 }
 
 // The wave's sums where its lane `at` alone holds entries that equal m, and these make up most of
@@ -331,7 +332,7 @@ __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, i
   if (nan) m = NAN;
   lds_barrier();  // sh.sums is read
   if (top == -INFINITY) {
-    if (lane == 0) sh.sums[wave] = {0.f, 0.f, 0.f, top, 0.f};
+    if (lane == 0) sh.sums[wave] = {0.0, 0.f, 0.f, top, 0.f};
   } else if (care) {
     const WaveSums s = careful_sums<BF16>(rb, sl, bt, tid, top, m, a.scale);
     if (lane == 0) sh.sums[wave] = s;
@@ -347,7 +348,7 @@ __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, i
     // to the slice's largest entry: one lane per wave's sums
     const WaveSums s = sh.sums[min(lane, NW - 1)];
     const bool has = lane < NW && s.top != -INFINITY;
-    const double d = (fabsf(s.c) < 0x1p30f ? static_cast<double>(s.c) : static_cast<double>(s.top) * a.scale) - static_cast<double>(m) * a.scale;
+    const double d = s.c - static_cast<double>(m) * a.scale;  // (the product is exact)
     const double f = has ? static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(d))) : 0.0;
     double rest = has ? f * s.sum : 0.0, wt = has ? f * (s.weighted + d * s.sum) : 0.0;
     float ones = has ? s.ones : 0.f;
@@ -444,25 +445,20 @@ __global__ void __launch_bounds__(kThreads) k_logp_wave(LogpArgs a) {
   });
   const uint32_t img = group_max_min<64>(best);
   const float m = img ? image_value<false>(img) : NAN;
-  const float c = m * a.scale, none = -1.2e6f / a.scale;  // none: its exponent is -1.1e6 or less
   float rest = 0.f, w = 0.f;
   int n = 0;
   each([&](uint32_t bits, int) __attribute__((always_inline)) {
     const float x = __uint_as_float(bits);
     n += x == m ? 1 : 0;
-    const float arg = fmaf(x == m ? none : fmaxf(x, none), a.scale, -c);
-    const float e = __builtin_amdgcn_exp2f(arg);
+    const float arg = exponent_below(x, m, a.scale);
+    const float e = x == m ? 0.f : __builtin_amdgcn_exp2f(arg);
     rest += e;
     w = fmaf(e, arg, w);
   });
-  if (!(fabsf(c) < 0x1p30f)) rest = w = 0.f;  // (as in careful_sums)
   if (__any(nan) || m == INFINITY) rest = NAN;
   rest = wave_sum_dpp(rest), w = wave_sum_dpp(w);
   const float ones = wave_sum_dpp(static_cast<float>(n));
-  // (c is rounded: the terms are 2^d of what they stand for)
-  const double d = fabsf(c) < 0x1p30f ? static_cast<double>(c) - static_cast<double>(m) * a.scale : 0.0;
-  const double f = static_cast<double>(__builtin_amdgcn_exp2f(static_cast<float>(d)));
-  const Sums s = {m, ones, f * rest, f * (w + d * rest) * a.unscale, xt};
+  const Sums s = {m, ones, rest, w * a.unscale, xt};
   const Totals tot = totals_of(s);
   if (lane == 0) put_entry(a, r, tot, s.weighted, xt);
   if constexpr (TOPK) {

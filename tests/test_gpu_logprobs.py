@@ -336,3 +336,99 @@ def test_rows_past_32_bits(P):
     for i, r in enumerate(at):
         assert abs(lp[r].item() - want) <= 1e-6 and idx[r].item() == 1000 + i
     assert lp.count_nonzero().item() == 3 and (idx != -1).sum().item() == 3
+
+
+def check32(got, x, tokens, k, tau=1.0, rows=None):
+    """check(), of values that may leave fp32's range (their rounding is -inf) and of rows with several
+    largest entries.  Those stay in a wave's sums where they make up half of them or more: their terms are
+    rounded as the others' (ref64_samples.logprobs: 6 * 3 + 4 + 129 + 6 + 15 roundings), and so is
+    what they weigh in the entropy, whose exponents are then the rounding of a reference below 2^20."""
+    lp, ent, idx, val = [None if t is None else t.double().cpu() for t in got]
+    f32 = lambda v: torch.tensor(v, dtype=torch.float64).float().item()  # noqa: E731
+    x = x.cpu()
+    for r, t in enumerate(tokens):
+        if t < 0:
+            continue
+        w_lp, w_ent, order, top, e_lp, e_ent = R.logprobs(x[r if rows is None else rows[r]], tau, t, k)
+        d = (x[r if rows is None else rows[r]].double() - x[r if rows is None else rows[r]].double().max()) / tau
+        n = (d == 0).sum().item()
+        tops = n * 172 * 2.0 ** -24 / torch.exp(d).sum().item() if n > 1 else 0.0
+        e_lp, e_ent = e_lp + tops, e_ent + tops * (2 + w_ent)
+        assert lp[r] == f32(w_lp) or abs(lp[r] - w_lp) <= e_lp + 2.0 ** -24 * abs(w_lp), (r, lp[r], w_lp, e_lp)
+        assert abs(ent[r] - w_ent) <= e_ent, (r, ent[r], w_ent, e_ent)
+        if k:
+            assert idx[r].int().tolist() == order, (r, idx[r].tolist(), order)
+            for a, b in zip(val[r].tolist(), top):
+                assert a == f32(b) or abs(a - b) <= e_lp + 2.0 ** -24 * abs(b), (r, a, b, e_lp)
+
+
+def low_rows(V, dtype, what, seed):
+    """Rows whose logits, or most of them, lie far below 0: (row, temperature) of every kind of one test."""
+    g = torch.Generator("cuda").manual_seed(seed)
+    lowest = torch.finfo(dtype).min
+    ordinary = lambda: torch.randn(V, generator=g, device="cuda") * 2  # noqa: E731
+    got = []
+    if what == "masks":  # finite masks, a few tokens allowed
+        for mask in (-1e4, -65504.0, -1e5, -1e6, -1e7, -1e8, -7e8, -1e9, lowest):
+            for allowed in (1, 3, 50):
+                x = torch.full((V,), mask, device="cuda")
+                at = torch.randperm(V, generator=g, device="cuda")[:allowed]
+                x[at] = torch.randn(len(at), generator=g, device="cuda") * 2
+                got.append((x, 1.0))
+            x = ordinary()
+            x[: V // 2] = mask                  # whole slices
+            got.append((x, 1.0))
+            x = ordinary()
+            x[V - V // 8 - 1:] = mask           # a padded end of the vocabulary
+            got.append((x, 0.7))
+    elif what == "uniform":  # nothing allowed
+        for mask in (-65504.0, -1e6, -1e7, -1e8, -7e8, -1e9, lowest):
+            got.append((torch.full((V,), mask, device="cuda"), 1.0))
+        got += [(torch.full((V,), -65504.0, device="cuda"), t) for t in (0.07, 0.02, 1e-4)]
+    elif what == "low":  # all logits far below 0, near each other and not
+        for base in (-1e5, -1e6, -1e7, -1e8, -7e8, -1e9):
+            for spread in (2.0 ** -21, 2.0 ** -16, 2.0 ** -8, 1.0):
+                got.append((base * (1 + spread * torch.rand(V, generator=g, device="cuda")), 1.0))
+    else:  # low temperatures on negative logits
+        for tau in (0.05, 1e-3, 2e-5, 1e-5, 1e-6, 1e-7, 1e-30):
+            for top in (-0.01, -3.0, -20.0, -35.0):
+                got.append((top - torch.rand(V, generator=g, device="cuda") * 5, tau))
+            x = -3 - torch.rand(V, generator=g, device="cuda")
+            x[: min(V, 40)] = -3.0
+            got.append((x, tau))
+    return [(x.to(dtype), tau) for x, tau in got]
+
+
+# few rows: one slice, several; many of them: a wave per row
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("what", ["masks", "uniform", "low", "cold"])
+@pytest.mark.parametrize("V,N,k", [(300, 1, 8), (1000, 700, 8), (1000, 1, 0), (2100, 4200, 16), (20000, 1, 8), (66003, 1, 5)])
+def test_low_references(P, dtype, what, V, N, k):
+    rows = low_rows(V, dtype, what, V)
+    r = random.Random(V)
+    for tau in sorted({t for _, t in rows}):
+        x = torch.stack([y for y, t in rows if t == tau])
+        m = x.shape[0]
+        tok = [[y.argmax().item(), r.randrange(V), y.argmin().item()][i % 3] for i, y in enumerate(x)]
+        n = -(-N // m)
+        st = i32([0])
+        got = P.token_logprobs(x.repeat(n, 1), i32(tok * n), k, temperature=tau, dev_status=st)
+        assert st.item() == 0
+        check32([None if t is None else t[-m:] for t in got], x, tok, k, tau)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [500, 40000])
+def test_low_references_along_paths(P, dtype, V):
+    for what in ("masks", "uniform", "cold"):
+        for tau in (1.0, 1e-5):
+            rows = [y for y, t in low_rows(V, dtype, what, V + 1) if t == tau]
+            if not rows:
+                continue
+            T = 6
+            x = torch.stack((rows * (T + 1))[: 2 * (T + 1)])
+            nodes, n = [[0, 2, 5, -1, -1, -1], [1, -1, -1, -1, -1, -1]], [3, 1]
+            tok = [j * 7 if j <= n[b] else -1 for b in range(2) for j in range(T + 1)]
+            at = [b * (T + 1) + (nodes[b][j - 1] + 1 if 0 < j <= n[b] else 0) for b in range(2) for j in range(T + 1)]
+            got = P.token_logprobs(x.view(2, T + 1, V), i32(tok), 4, nodes=i32(nodes), temperature=tau)
+            check32(got, x, tok, 4, tau, rows=at)
