@@ -100,6 +100,14 @@ __device__ __forceinline__ float image_value(uint32_t img) {
   }
 }
 
+// The image of the largest element that is at most x: an image of bf16 leaves out the lower half of
+// a float, which takes negative numbers up.
+template <bool BF16>
+__device__ __forceinline__ uint32_t image_at_most(float x) {
+  const uint32_t bits = __float_as_uint(x);
+  return elem_img<BF16>(bits) - (BF16 && (bits & 0x80000000u) && (bits & 0xFFFFu) ? 1u : 0u);
+}
+
 __device__ __forceinline__ double reciprocal(double x) {
   const double r = __builtin_amdgcn_rcp(x);
   return fma(fma(-x, r, 1.0), r, r);
@@ -295,7 +303,7 @@ __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, i
       weighted = u0 == 0 ? 0.f : f * fmaf(c - next, sum, weighted);
       sum = u0 == 0 ? 0.f : f * sum;
       c = next;
-      limit = max(most, elem_img<BF16>(__float_as_uint(ref + 8.f / a.scale)));
+      limit = max(most, image_at_most<BF16>(ref + 8.f / a.scale));
     }
 #pragma unroll
     for (int u = u0; u < u0 + 4; ++u) {

@@ -432,3 +432,24 @@ def test_low_references_along_paths(P, dtype, V):
             at = [b * (T + 1) + (nodes[b][j - 1] + 1 if 0 < j <= n[b] else 0) for b in range(2) for j in range(T + 1)]
             got = P.token_logprobs(x.view(2, T + 1, V), i32(tok), 4, nodes=i32(nodes), temperature=tau)
             check32(got, x, tok, 4, tau, rows=at)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,N", [(1000, 1), (32768, 130)])
+def test_rows_in_order_far_below_zero(P, dtype, V, N):
+    # the reference moves with every group of chunks where the type's steps are many doublings
+    rows = []
+    for base, span in ((-1000.0, 200.0), (-5056.0, 700.0), (-20000.0, 3000.0), (-60000.0, 9000.0), (-300.0, 20.0)):
+        up = (base + torch.linspace(0, span, V, device="cuda")).to(dtype)
+        rows += [up, up.flip(0)]
+        x = torch.full((V,), -math.inf, dtype=dtype, device="cuda")  # one entry, and two at the end, a step of bf16 larger
+        x[0] = base
+        x[V - 2:] = torch.nextafter(torch.tensor(base, dtype=torch.bfloat16), torch.tensor(0.0, dtype=torch.bfloat16)).item()
+        rows.append(x)
+    x = torch.stack(rows * N)
+    tok = [0, V - 1, V - 2] * (len(rows) // 3)
+    for tau in (1.0, 0.6, 7.0):
+        got = P.token_logprobs(x, i32(tok * N), 8, temperature=tau)
+        check32([t[:len(rows)] for t in got], x[:len(rows)], tok, 8, tau)
+        for t in got:
+            assert torch.equal(t.view(N, -1), t.view(N, -1)[:1].expand(N, -1))
