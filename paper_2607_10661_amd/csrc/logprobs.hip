@@ -590,11 +590,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_logp_merge(LogpArgs a) {
     }
   }
   if constexpr (KMAX > 0) {
-    const int found = __syncthreads_count(tid < n && key != 0);
-    if (tid >= found && tid < a.k) {  // (entries that are no numbers: fewer than k in order)
-      if (a.topk_idx) a.topk_idx[static_cast<size_t>(r) * a.k + tid] = -1;
-      if (a.topk_val) a.topk_val[static_cast<size_t>(r) * a.k + tid] = NAN;
-    }
+    __syncthreads();
     // a slice's pairs are in order: the rank of one is its place plus, in every other slice, the number of
     // larger ones, found by halving (several slices at once: each step waits for LDS)
     int above = tid % KMAX;

@@ -248,7 +248,8 @@ struct TopkLds {
 //   4. The candidates are ranked by counting: the list is cut into parts,
 //      each thread counts the keys of one part above one candidate, and the
 //      counts are summed in LDS.  Where fewer than KMAX are above -inf, all others of the slice
-//      are at -inf, so the first of those in order are among its first KMAX entries.  If either list
+//      are at -inf (or NaN with the sign set, which count as such), so the first of those in order are
+//      among its first KMAX entries.  If either list
 //      overflows (many values tied at the top, or in order), the caller's overflow() finds them.
 // Only listed chunks pass through LDS, so the slice is read from memory once
 // and LDS carries a few KB.  The kernel's loops stay rolled, which keeps its
@@ -436,11 +437,13 @@ __device__ __forceinline__ void topk_pick(TopkLds<NT>& sh, const char* rb, const
       if (rank < static_cast<uint32_t>(KMAX)) put(static_cast<int>(rank), key, bits);
     }
     if (n < KMAX && tid < KMAX) {  // the rest: the first entries at -inf, then none
+      // (NaN with the sign set are in order with -inf: every rank below k is an entry of the row)
       const int v = s.v0 + tid;
-      const bool out = v < s.v1 && elem_bits<BF16>(rb, v) == 0xFF800000u;
+      const uint32_t bits = v < s.v1 ? elem_bits<BF16>(rb, v) : 0u;
+      const bool out = v < s.v1 && elem_img<BF16>(bits) <= kImgNegInf<BF16>;
       const uint64_t all = __ballot(out);
       const int rank = n + __popcll(all & ((1ull << tid) - 1));
-      if (out && rank < KMAX) put(rank, make_key(0xFF800000u, static_cast<uint32_t>(v)), 0xFF800000u);
+      if (out && rank < KMAX) put(rank, make_key(0xFF800000u, static_cast<uint32_t>(v)), bits);
       if (tid >= n + __popcll(all)) put(tid, 0, 0);
     }
   } else {

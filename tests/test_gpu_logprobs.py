@@ -453,3 +453,20 @@ def test_rows_in_order_far_below_zero(P, dtype, V, N):
         check32([t[:len(rows)] for t in got], x[:len(rows)], tok, 8, tau)
         for t in got:
             assert torch.equal(t.view(N, -1), t.view(N, -1)[:1].expand(N, -1))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,N", [(40, 1), (1000, 1), (20000, 1), (128256, 1), (700, 260)])
+def test_every_rank_of_rows_of_no_numbers(P, dtype, V, N):
+    # NaN with the sign set, a few numbers or -inf among them: indices of the row, each once, the numbers first
+    # (as a pattern: a conversion may lose a NaN's sign)
+    x = (torch.full((5, V), -0x40, dtype=torch.int16, device="cuda") if dtype == torch.bfloat16 else
+         torch.full((5, V), -0x400000, dtype=torch.int32, device="cuda")).view(dtype)
+    x[1, 7], x[1, V - 1] = 2.0, 3.0
+    x[2, ::2] = -math.inf
+    x[3, : V // 2] = -math.inf
+    x[4, V // 2:] = torch.linspace(-1, 1, V - V // 2, device="cuda")
+    _, _, idx, _ = P.token_logprobs(x.repeat(N, 1), None, 5)
+    assert torch.equal(idx.view(N, 5, 5), idx[:5].expand(N, 5, 5))
+    assert ((idx >= 0) & (idx < V)).all() and all(len(set(row)) == 5 for row in idx[:5].tolist())
+    assert idx[1, :2].tolist() == [V - 1, 7] and (idx[4] >= V // 2).all()
