@@ -102,14 +102,6 @@ __device__ __forceinline__ uint64_t shfl_xor_u64(uint64_t v, int o) {
   uint32_t hi = __shfl_xor(static_cast<uint32_t>(v >> 32), o, PTD_WAVE);
   return (static_cast<uint64_t>(hi) << 32) | lo;
 }
-__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    uint64_t w = shfl_xor_u64(v, o);
-    v = w > v ? w : v;
-  }
-  return v;
-}
 
 
 // Over a wave by DPP: shifts within rows of 16 lanes, then broadcasts of the rows' last

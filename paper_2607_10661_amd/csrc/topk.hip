@@ -87,7 +87,9 @@ k_topk_row(const void* __restrict__ logits, int V, long long ld, int slices, int
   lds_barrier();
   // a list that overflows (values tied at the top, or in order): every lane keeps a sorted list of
   // the best of its own elements that reach the bound, and the lists are merged (KMAX 16: its registers
-  // would halve the workgroups of a CU, so the best are taken one after the other)
+  // would halve the workgroups of a CU, so the best are taken one after the other.  1040 rows x 128256 bf16,
+  // k = 16, in turns / with lists: ordinary rows 50 / 146 us, 5 % tied at the top 146 / 648, in order
+  // 145 / 288, all but a few at one finite value 145 / 352; 65 x 32000 in order 33 / 31)
   auto overflow = [&]() {
     if constexpr (KMAX == 16) {
       topk_in_turns<KMAX, BF16, NT>(sh, rb, sl, tid);

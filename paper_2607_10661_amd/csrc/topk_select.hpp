@@ -212,6 +212,13 @@ __device__ __forceinline__ uint32_t group_max_min(uint32_t x) {
   return x;
 }
 
+// The wave's largest key, to every lane.
+__device__ __forceinline__ uint64_t wave_max_key(uint64_t key) {
+  const uint32_t hi = static_cast<uint32_t>(key >> 32);
+  const uint32_t top = group_max_min<64>(hi);
+  return (static_cast<uint64_t>(top) << 32) | group_max_min<64>(hi == top ? static_cast<uint32_t>(key) : 0u);
+}
+
 // LDS of the selection.
 template <int NT>
 struct TopkLds {
@@ -327,9 +334,9 @@ __device__ __forceinline__ uint32_t topk_list(TopkLds<NT>& sh, const uint4 (&cw)
   return tc;
 }
 
-// The best key below `below` of a thread's elements, read anew.
+// The best key of a thread's elements, read anew.
 template <bool BF16, int NT>
-__device__ __forceinline__ uint64_t best_below(const char* rb, const Slice& s, int tid, uint64_t below) {
+__device__ __forceinline__ uint64_t best_of(const char* rb, const Slice& s, int tid) {
   constexpr int E = BF16 ? 8 : 4;
   uint64_t best = 0;
   const uint4* src = reinterpret_cast<const uint4*>(rb + static_cast<size_t>(s.vb) * (BF16 ? 2 : 4));
@@ -345,29 +352,49 @@ __device__ __forceinline__ uint64_t best_below(const char* rb, const Slice& s, i
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const uint64_t key = make_key(chunk_bits<BF16>(x[u], e), static_cast<uint32_t>(s.vb + c * E + e));
-          best = key < below && key > best ? key : best;
+          best = key > best ? key : best;
         }
       }
     }
   }
   if (s.tail) {
     const uint64_t key = make_key(elem_bits<BF16>(rb, s.vt), static_cast<uint32_t>(s.vt));
-    best = key < below && key > best ? key : best;
+    best = key > best ? key : best;
   }
   return best;
 }
 
+// The best key below `below` of the elements of thread `owner` of the wave, which the wave reads anew,
+// one of them per lane (to every lane).
+template <bool BF16, int NT>
+__device__ __forceinline__ uint64_t next_of(const char* rb, const Slice& s, int tid, int owner, uint64_t below) {
+  constexpr int E = BF16 ? 8 : 4;
+  const int lane = tid & 63, first = tid - lane + owner;
+  uint64_t best = 0;
+  if (lane == owner && s.tail) {
+    const uint64_t key = make_key(elem_bits<BF16>(rb, s.vt), static_cast<uint32_t>(s.vt));
+    best = key < below ? key : 0;
+  }
+  for (int c0 = first; c0 < s.nfull; c0 += PTD_WAVE / E * NT) {  // uniform
+    const int c = c0 + lane / E * NT;
+    if (c < s.nfull) {
+      const int v = s.vb + c * E + lane % E;
+      const uint64_t key = make_key(elem_bits<BF16>(rb, v), static_cast<uint32_t>(v));
+      best = key < below && key > best ? key : best;
+    }
+  }
+  return wave_max_key(best);
+}
+
 // The best keys of a slice to sh.out, one after the other: every thread looks for the best of its
-// own, the best of all is taken, and its owner looks for its next one.
+// own, the best of all is taken, and its owner's wave looks for that thread's next one.
 template <int KMAX, bool BF16, int NT>
 __device__ __forceinline__ void topk_in_turns(TopkLds<NT>& sh, const char* rb, const Slice& s, int tid) {
   constexpr int NW = NT / PTD_WAVE;
-  uint64_t mine = 0, below = ~0ull;
-  bool look = true;
+  uint64_t mine = best_of<BF16, NT>(rb, s, tid);
 #pragma unroll 1
   for (int r = 0; r < KMAX; ++r) {
-    if (look) mine = best_below<BF16, NT>(rb, s, tid, below);
-    const uint64_t w = wave_max_u64(mine);
+    const uint64_t w = wave_max_key(mine);
     if (r == 0) __syncthreads();  // sh.cand of the lists is read
     if ((tid & 63) == 0) sh.cand[(r & 1) * NW + (tid >> 6)] = w;
     __syncthreads();
@@ -377,11 +404,18 @@ __device__ __forceinline__ void topk_in_turns(TopkLds<NT>& sh, const char* rb, c
       const uint64_t x = sh.cand[(r & 1) * NW + i];
       best = x > best ? x : best;
     }
-    look = best != 0 && mine == best;
-    below = best;
-    if (look || (best == 0 && tid == 0)) {
-      sh.out[r] = best;
-      sh.out_bits[r] = best ? elem_bits<BF16>(rb, key_index(best)) : 0u;
+    const uint64_t who = __ballot(best != 0 && mine == best);
+    if (who) {  // whole wave
+      const int owner = __builtin_ctzll(who);
+      if ((tid & 63) == owner) {
+        sh.out[r] = best;
+        sh.out_bits[r] = elem_bits<BF16>(rb, key_index(best));
+      }
+      const uint64_t next = next_of<BF16, NT>(rb, s, tid, owner, best);
+      if ((tid & 63) == owner) mine = next;
+    } else if (best == 0 && tid == 0) {
+      sh.out[r] = 0;
+      sh.out_bits[r] = 0u;
     }
   }
 }
