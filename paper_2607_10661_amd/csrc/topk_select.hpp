@@ -391,6 +391,8 @@ __device__ __forceinline__ uint64_t next_of(const char* rb, const Slice& s, int 
 template <int KMAX, bool BF16, int NT>
 __device__ __forceinline__ void topk_in_turns(TopkLds<NT>& sh, const char* rb, const Slice& s, int tid) {
   constexpr int NW = NT / PTD_WAVE;
+  // (what the lanes' numbers make would be worked out ahead, in registers of the common way)
+  asm volatile("" : "+v"(tid));
   uint64_t mine = best_of<BF16, NT>(rb, s, tid);
 #pragma unroll 1
   for (int r = 0; r < KMAX; ++r) {
