@@ -494,7 +494,8 @@ typedef struct {
  *   inv_freq   HOST double [rot_dim/2], at most 2^20 each, or NULL for those of theta
  * Sums, norm and rotation are fp32, angles and their sine and cosine fp64 (rounded to
  * fp32); each output is rounded once, to nearest even.  Heads whose sum of squares leaves fp32's range
- * (elements beyond 2^60), infinities and NaN give no numbers in their own head only.
+ * (elements beyond 2^60; with an eps below 2^-100 also heads of nothing but elements below 2^-56),
+ * infinities and NaN give no numbers, or ones that are off, in their own head only.
  * Data and weights 16-byte aligned.
  * dev_status: PTD_ERR_PAGE (a slot that is neither -1 nor in the pages: not stored).
  * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_DTYPE, PTD_ERR_ALIGN, PTD_ERR_HIP.
@@ -540,8 +541,9 @@ int ptd_page_plan_shared(const ptd_page_state* state, int32_t* refs, const int32
  * the stream may be the copy, as no page is both).  So the next row of every sequence goes to a page
  * of its own.  Pages that nobody holds any more go to the list's end, the highest id first.
  * The next tables then stand for the state with free_pages, num_free and refs, which are
- * changed in place; the old tables are spent.  All or nothing: after a device-reported
- * error the next tables are the old ones and nothing else has changed.
+ * changed in place; the old tables are spent.  refs is counted anew from the tables: a page that a
+ * program holds by a count of its own, and no sequence, goes back to the list.  All or nothing:
+ * after a device-reported error the next tables are the old ones and nothing else has changed.
  * dev_status: PTD_ERR_ROWS (from outside [-1, B)), PTD_ERR_KV_LEN (len), PTD_ERR_NO_PAGES,
  * PTD_ERR_PAGE (num_held, num_free or a page id out of range).
  * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_HIP.
@@ -652,7 +654,8 @@ size_t ptd_topk_workspace_bytes(int32_t R, int32_t V, int32_t k);
  *   topk_val  float [R][k]         (nullable) the selected entries' own values,
  *                                  widened exactly to fp32
  * Order: value descending; equal values by the lower index; -0.0 equals +0.0.
- * Logits are expected non-NaN (NaN ordering is unspecified); +-inf are ordered.
+ * Logits are expected non-NaN (NaN ordering is unspecified, but every index is one of the row and
+ * occurs once); +-inf are ordered.
  * A workspace is needed when a row is split over several workgroups, that is
  * when V exceeds one workgroup's slice (32768 bf16 or 16384 fp32 values, 1.5
  * times that when R times the slices of a row would exceed 256);
@@ -688,16 +691,17 @@ size_t ptd_token_logprobs_workspace_bytes(int32_t R, int32_t V, int32_t k);
  *               emitted token j, b * (T + 1) for j = 0, else b * (T + 1) + nodes[b][j - 1] + 1
  *   temperature 1e-30 .. 1e30
  *   k           0 .. PTD_MAX_K, k <= V; 0 with topk_idx and topk_logprob NULL
- *   logprob     float [R] or NULL (-inf for a masked token)
+ *   logprob     float [R] or NULL (-inf for a masked token, and below fp32's range)
  *   entropy     float [R] or NULL, in nats: -sum p log p
  *   topk_idx    int32 [R][k] or NULL, in the order of ptd_topk_argmax
  *   topk_logprob  float [R][k] or NULL
  *   workspace   >= ptd_token_logprobs_workspace_bytes(R, V, k), 8-byte aligned
  * At least one output.  A row whose entries are all -inf has no distribution: log
- * probabilities -inf, entropy 0, indices in order.  With a NaN or +inf in a row its own values are
+ * probabilities -inf, entropy 0, indices in order.  A finite mask is a logit like any other, whatever
+ * its size.  With a NaN or +inf in a row its own values are
  * NaN or unspecified.  Terms and the sums of 64 lanes are fp32, joined in fp64; what is left beside the row's largest
  * entries is summed apart, so log probabilities and entropies next to 0 keep their relative
- * precision.
+ * precision (5e-5 of themselves at worst, down to 1e-38).
  * dev_status: PTD_ERR_VALUE (a token outside [-1, V)), PTD_ERR_ROWS (a node outside [0, T) on a
  * path): that entry stands for nothing.
  * Errors: PTD_ERR_NULL, PTD_ERR_SHAPE, PTD_ERR_DTYPE, PTD_ERR_ALIGN, PTD_ERR_WORKSPACE,

@@ -1011,7 +1011,9 @@ class PageTables:
     def fork(self, from_, len_, dev_status=None):
         """Sequence b goes on from the first len_[b] rows of sequence from_[b] (-1: it ends);
         returns (copy_src, copy_dst, copy_rows) int32 [B] for page_copy, which has to follow before
-        rows are written.  page_table and num_held are new tensors afterwards."""
+        rows are written.  page_table and num_held are new tensors afterwards (so a captured fork goes
+        on from the tables of its capture: a graph that is replayed calls ptd_page_fork with two
+        tables of its own)."""
         self._need_shared()
         _need_i32(from_, len_, dev_status, self.page_table)
         if from_.numel() != self.B or len_.numel() != self.B:

@@ -20,7 +20,7 @@
 //                 lane, or 2).
 // An element costs its unpacking, a multiply-add, the exponential, a sum, a maximum and a multiply-add, and 1.4
 // more for its chunk's largest: about 45 us of the vector units for 1040 rows x 128256, beside 51 of
-// HBM.  That takes 64 us in all with the 8 best entries and 47 without (a version that needed the
+// HBM.  That takes 64 us in all with the 8 best entries and 52 without (a version that needed the
 // row's largest entry first took 77 and 58, 512 threads x 8 chunks 70); 97 rows x 32003 fp32 11
 // us, a single row 11, both the latency of two launches and of six barriers.
 // Terms and the sums of a wave are fp32, waves and slices are joined in fp64.
@@ -280,8 +280,8 @@ __device__ __forceinline__ void row_slice(const LogpArgs& a, RowLds<KMAX>& sh, i
   uint32_t lm = sl.tail ? elem_img<BF16>(bt) : 0u, limit = 0;
   float c = 0.f, sum = 0.f, weighted = 0.f;
   // (a masked entry's term is 0, times its exponent no number: the exponent of a term that is 0 may be any
-  // other.  1040 x 128256, 99 % of it masked, 62 us, and 115 where such waves were summed again with
-  // care; nothing masked 64 and 62)
+  // other.  1040 x 128256, 99 % of it masked, 65 us, and 115 where such waves were summed again with
+  // care; nothing masked 64)
   auto add = [&](float x) __attribute__((always_inline)) {
     const float arg = fmaf(x, a.scale, -c);
     const float e = __builtin_amdgcn_exp2f(arg);
@@ -648,9 +648,9 @@ bool make_plan(int R, int V, int k, int elem_bytes, int path_seqs, LogpPlan* p) 
 }
 
 // Whether rows go to k_logp_wave: those that fit, where there are many.  (bf16, a workgroup / a wave per
-// row: 1000 entries, k = 5, 64 rows 5.4 / 6.5 us, 1040 rows 11.3 / 7.1, 16384 rows 90 / 28; k = 16,
-// 1040 rows 13.3 / 13.5; 4000 entries, k = 5, 1040 rows 12.0 / 12.4, 16384 rows 98 / 58; k = 0, 1040
-// rows 6.8 / 9.8, 16384 rows 52 / 45; 100000 rows of 50 entries 538 / 122.)
+// row: 1000 entries, k = 5, 64 rows 5.1 / 6.4 us, 1040 rows 11.0 / 6.8, 16384 rows 91 / 27; k = 16,
+// 1040 rows 13.3 / 13.0; 4000 entries, k = 5, 1040 rows 11.6 / 12.1, 16384 rows 101 / 55; k = 0, 1040
+// rows 7.1 / 9.3, 16384 rows 56 / 44; 100000 rows of 50 entries 552 / 118.)
 constexpr int kFewChunks = 2, kWaveChunks = 8;
 inline bool by_waves(const LogpArgs& a, int elems) {
   if (a.V > PTD_WAVE * kWaveChunks * elems) return false;
